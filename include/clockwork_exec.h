@@ -63,9 +63,9 @@ enum {
     CW_ERR_TIMEOUT = -12        /* cw_worker_next_result: no result within the time given */
 };
 
-enum { CW_OP_CONV = 0, CW_OP_MAXPOOL = 1, CW_OP_GAVGPOOL = 2, CW_OP_FC = 3, CW_OP_SOFTMAX = 4, CW_OP_CONCAT = 5 };
+enum { CW_OP_CONV = 0, CW_OP_MAXPOOL = 1, CW_OP_GAVGPOOL = 2, CW_OP_FC = 3, CW_OP_SOFTMAX = 4, CW_OP_CONCAT = 5, CW_OP_FC4 = 6 };
 enum { CW_ACT_NONE = 0, CW_ACT_RELU = 1, CW_ACT_HSWISH = 2 };   /* values of cw_op.relu */
-enum { CW_DTYPE_FP16 = 0, CW_DTYPE_BF16 = 1 };
+enum { CW_DTYPE_FP16 = 0, CW_DTYPE_BF16 = 1, CW_DTYPE_FP32 = 2 };   /* a model's storage type is one of the first two */
 
 /* One operator of a model.  Ops form a DAG over earlier ops' outputs.
  * CONV:     cross-correlation, kh x kw, `stride`, zero padding, + bias[cout], then (if
@@ -81,6 +81,8 @@ enum { CW_DTYPE_FP16 = 0, CW_DTYPE_BF16 = 1 };
  * CONCAT:   the channels of op input_from followed by those of op residual_from (same spatial
  *           size; cin = channels of the first, cout = of both).  Where the producers allow it
  *           they write straight into their channel range of the result and nothing is copied.
+ * FC4:      FC over 4-bit weights (see cw_fc4) in the place of FC; `groups` inputs share a scale and a zero
+ *           point (a multiple of 32).  A quarter of the bytes to LOAD and to keep.
  * The operators beyond the ResNet set serve the other model families of the paper's Table 1
  * (DenseNet: concatenation; Inception v3: rectangular filters; MobileNet: depthwise, hard swish). */
 typedef struct {
@@ -92,7 +94,7 @@ typedef struct {
     int32_t residual_from; /* CONV: -1 or index of an earlier op to add; CONCAT: the second source */
     int32_t input_from;    /* -1 = the network input, else index of an earlier op */
     int32_t pad_w;         /* CONV with kh != kw: padding in width (`pad` is then the padding in height) */
-    int32_t groups;        /* CONV: 0 or 1 = dense, cin = depthwise */
+    int32_t groups;        /* CONV: 0 or 1 = dense, cin = depthwise; FC4: inputs of a group */
 } cw_op;
 
 typedef struct {
@@ -123,10 +125,10 @@ int32_t cw_destroy(cw_ctx *ctx);
  * variant, grid, split-K factor and workspace offsets are functions of (ops, input
  * size, batch) only.  Nothing is tuned or chosen at run time.
  * ops, batch_sizes: [host], copied.  The first op must read the network input
- * (in_c x in_h x in_w, NCHW fp32 at the boundary); the list must end FC, SOFTMAX.
+ * (in_c x in_h x in_w, NCHW fp32 at the boundary); the list must end FC, SOFTMAX or FC4, SOFTMAX.
  * Supported: CONV with cin % 32 == 0, cout % 32 == 0 and kh == kw <= 5 anywhere,
  * plus a first CONV with cin <= 4 and kh == kw <= 8; GAVGPOOL over a multiple of 64
- * channels; FC with cin % 256 == 0 reading the GAVGPOOL.  Returns CW_ERR_UNSUPPORTED otherwise,
+ * channels; FC with cin % 256 == 0, or FC4, reading the GAVGPOOL.  Returns CW_ERR_UNSUPPORTED otherwise,
  * CW_ERR_NO_MEMORY if a plan's workspace exceeds workspace_bytes. */
 int32_t cw_model_define(cw_ctx *ctx, const cw_op *ops, int32_t n_ops,
                         int32_t in_c, int32_t in_h, int32_t in_w,
@@ -147,6 +149,9 @@ size_t cw_model_workspace_bytes(cw_ctx *ctx, int32_t model_id, int32_t batch);
  * Canonical blob [host]: for every op that owns weights (CONV, FC), in op order,
  * W[cout][cin][kh][kw] in the model's storage type, back to back; zero padding to
  * a multiple of 4 bytes; then every bias[cout] as fp32 in the same op order.
+ * In W's place an FC4 has its weights q[cout][ceil(cin/2)] (bytes, the even input in the low four bits),
+ * the scales[cout][ceil(cin/groups)] in the storage type and the zero points [cout][ceil(cin/groups)]
+ * (bytes), each of the three padded with zeros to a multiple of 2 bytes.
  * The weight pool is a set of equal pages (section 5.1; cw_config.weight_page_bytes).  A
  * model's packed tensors were given places in cw_model_weight_pages() pages of its own when it
  * was defined, none straddling a page boundary; LOAD takes that many free pages of the pool,
@@ -229,6 +234,16 @@ size_t cw_exec_static_capacity(void);
  * only after these copies have completed.  CW_ERR_NO_INPUT if no EXEC ran. */
 int32_t cw_output(cw_ctx *ctx, int32_t slot, float *host_probs, float *host_logits,
                   void *stream);
+/* OUTPUT of the answer instead of the rows of probabilities (see cw_answer for what it holds): computed on
+ * `stream` behind the slot's EXEC from its logits and copied to host_answer [host], cw_answer_bytes(batch, top)
+ * bytes: logp fp32 [batch], rank int32 [batch], entropy fp32 [batch], top_id int32 [batch][top], top_logp fp32
+ * [batch][top], back to back.  host_given [host] int32 [batch] or NULL (nothing given).  Then releases the slot as
+ * cw_output does.  CW_ERR_NO_INPUT if no EXEC ran, CW_ERR_INVALID / CW_ERR_UNSUPPORTED for arguments that cw_answer
+ * refuses, CW_ERR_NO_MEMORY where the answer is larger than the slot's input and its probabilities; the slot then stays. */
+int32_t cw_output_answer(cw_ctx *ctx, int32_t slot, const int32_t *host_given, int32_t top, float scale,
+                         void *host_answer, void *stream);
+/* Bytes of that answer (0 for batch < 0 or top outside 0..CW_ANSWER_MOST_TOP). */
+size_t cw_answer_bytes(int32_t batch, int32_t top);
 /* Section 5.2, INFER: an action that is rejected after its INPUT (its window passed, its EXEC
  * failed) must give its IO-cache entry back without an OUTPUT.  Releases the slot without
  * copying anything out; the memory is reused only after its INPUT copy and its last EXEC have
@@ -258,6 +273,68 @@ int32_t cw_profile_measure(cw_ctx *ctx, int32_t model_id, int32_t batch, int32_t
                            uint32_t repeats, cw_profile *out, float *samples_us);
 /* Last measured profile; n == 0 if none was measured. */
 int32_t cw_profile_get(cw_ctx *ctx, int32_t model_id, int32_t batch, cw_profile *out);
+
+/* ---- single operators over the caller's device memory ------------------------------------------
+ * As cw_exec_static: every buffer is the caller's, on the context's GPU, and stays valid until the work is over; the call
+ * allocates nothing, enqueues kernel launches on `stream` and nothing else, and may be captured into a HIP graph.
+ * Inputs and outputs must not overlap.  Strides are in elements (bytes for 4-bit weights) from one row to
+ * the next; the elements of a row are contiguous.  Input rows may overlap (stride 0: one row for all), output
+ * rows not.  CW_ERR_INVALID for a null or misaligned pointer, a bad size, stride or type, CW_ERR_UNSUPPORTED for
+ * sizes the kernels do not run; nothing is enqueued then.  No row: CW_OK, nothing to do. */
+
+/* Fully connected layer over 4-bit weights with group scales:
+ *   y[m][n] = bias[n] + sum over k < cin of x[m][k] * (q[n][k] - zero[n][k / group]) * scale[n][k / group]
+ * Products and sums are exact to fp32; the result is rounded once, to y's type.  Activations of 16 bits are taken as they are;
+ * fp32 ones keep 22 bits of mantissa or more of a row's largest ones (what is below 2^-36 of the row's largest is lost). */
+typedef struct {
+    const void *x;          /* [rows][cin], x_dtype */
+    const uint8_t *q;       /* [cout][ceil(cin / 2)]: k even in the low, k odd in the high four bits */
+    const void *scales;     /* [cout][ceil(cin / group)], scale_dtype */
+    const uint8_t *zeros;   /* [cout][ceil(cin / group)], 0..15 (of larger values the low four bits), or NULL: 8 everywhere */
+    const float *bias;      /* [cout] or NULL */
+    void *y;                /* [rows][cout], y_dtype */
+    int64_t x_stride, q_stride, scale_stride, zero_stride, y_stride;
+    int32_t rows, cin, cout;
+    int32_t group;          /* inputs that share a scale: a multiple of 32 (the last group of a row may be short) */
+    int32_t x_dtype, scale_dtype, y_dtype;   /* CW_DTYPE_* */
+} cw_fc4_args;
+int32_t cw_fc4(cw_ctx *ctx, const cw_fc4_args *args, void *stream);
+
+/* The answer of every row of logits.  With d[i] = scale * (x[i] - max x) over the classes i with x[i] > -inf (a masked class
+ * has -inf) and S = sum exp d:
+ *   logp     d[given] - ln S; 0 for a negative `given` (nothing given), NaN for one >= classes, -inf for a masked class
+ *   rank     classes that come before the given one: larger logits, and equal ones of lower index (0: it is the first); -1 for
+ *            a `given` outside the classes
+ *   entropy  ln S - sum(d exp d) / S, in nats
+ *   top_id, top_logp  the `top` likeliest classes, equal ones by index, and d - ln S; behind the last class that is not masked -1
+ *            and -inf
+ * A row with nothing but -inf: logp -inf, entropy 0, no top classes.  A row with a NaN or +inf: logp, entropy and
+ * top_logp NaN, rank and top_id -1 (a negative `given` has logp 0 all the same).  The order is that of the logits as they are stored; sums are fp32.
+ * With few rows a row is shared by several workgroups, which meet in `workspace`: its first CW_ANSWER_COUNTERS bytes must be
+ * zero before the first call and are zero behind every call.  Calls that may overlap in time need a workspace each.
+ * Without one (NULL, or smaller than cw_answer_workspace_bytes) a workgroup takes a row; the answers are the same but for
+ * the order of the sums. */
+#define CW_ANSWER_MOST_TOP 64
+#define CW_ANSWER_COUNTERS 1024
+typedef struct {
+    const void *logits;     /* [rows][classes], dtype */
+    const int32_t *given;   /* [rows] or NULL */
+    float *logp;            /* [rows] or NULL; with `given` only */
+    int32_t *rank;          /* [rows] or NULL; with `given` only */
+    float *entropy;         /* [rows] or NULL */
+    int32_t *top_id;        /* [rows][top], NULL with top == 0 */
+    float *top_logp;        /* [rows][top], NULL with top == 0 */
+    void *workspace;        /* 16-byte aligned, or NULL */
+    size_t workspace_bytes;
+    int64_t stride;
+    int32_t rows, classes;
+    int32_t top;            /* 0..CW_ANSWER_MOST_TOP */
+    int32_t dtype;          /* CW_DTYPE_* */
+    float scale;            /* of the logits (1 / temperature): finite, > 0 */
+} cw_answer_args;
+int32_t cw_answer(cw_ctx *ctx, const cw_answer_args *args, void *stream);
+/* Workspace that serves every call (less than 1 MiB). */
+size_t cw_answer_workspace_bytes(void);
 
 /* Device ordinal the context was created on (-1: planning only). */
 int32_t cw_context_device(cw_ctx *ctx);

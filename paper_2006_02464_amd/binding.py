@@ -15,7 +15,9 @@ CW_ERR_INVALID, CW_ERR_HIP, CW_ERR_NO_MEMORY, CW_ERR_NOT_LOADED = -1, -2, -3, -4
 CW_ERR_ALREADY_LOADED, CW_ERR_NO_INPUT, CW_ERR_BAD_BATCH, CW_ERR_BUSY = -5, -6, -7, -8
 CW_ERR_UNSUPPORTED, CW_ERR_NO_SLOT, CW_ERR_TOO_LATE, CW_ERR_TIMEOUT = -9, -10, -11, -12
 CW_OP_CONV, CW_OP_MAXPOOL, CW_OP_GAVGPOOL, CW_OP_FC, CW_OP_SOFTMAX, CW_OP_CONCAT = 0, 1, 2, 3, 4, 5
-CW_DTYPE_FP16, CW_DTYPE_BF16 = 0, 1
+CW_OP_FC4 = 6
+CW_DTYPE_FP16, CW_DTYPE_BF16, CW_DTYPE_FP32 = 0, 1, 2
+CW_ANSWER_MOST_TOP, CW_ANSWER_COUNTERS = 64, 1024
 DTYPES = {"fp16": CW_DTYPE_FP16, "bf16": CW_DTYPE_BF16}
 CONV_TILES = {"128x128": 0, "128x64": 1, "64x64": 2, "64x32": 3, "32x64": 4, "32x32": 5,
               "128x64w2": 6, "64x128w2": 7, "256x64": 8, "128x128w8": 9,
@@ -33,6 +35,18 @@ class cw_op(Structure):
 class cw_config(Structure):
     _fields_ = [("device", c_int32), ("workspace_bytes", c_size_t), ("io_bytes", c_size_t),
                 ("weight_pool_bytes", c_size_t), ("load_staging_bytes", c_size_t), ("weight_page_bytes", c_size_t)]
+
+
+class cw_fc4_args(Structure):
+    _fields_ = [(n, c_void_p) for n in ("x", "q", "scales", "zeros", "bias", "y")] + \
+               [(n, c_int64) for n in ("x_stride", "q_stride", "scale_stride", "zero_stride", "y_stride")] + \
+               [(n, c_int32) for n in ("rows", "cin", "cout", "group", "x_dtype", "scale_dtype", "y_dtype")]
+
+
+class cw_answer_args(Structure):
+    _fields_ = [(n, c_void_p) for n in ("logits", "given", "logp", "rank", "entropy", "top_id", "top_logp", "workspace")] + \
+               [("workspace_bytes", c_size_t), ("stride", c_int64)] + \
+               [(n, c_int32) for n in ("rows", "classes", "top", "dtype")] + [("scale", c_float)]
 
 
 class cw_profile(Structure):
@@ -91,6 +105,11 @@ SIGNATURES = {
     "cw_exec_static": (c_int32, [c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]),
     "cw_exec_static_capacity": (c_size_t, []),
     "cw_output": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_void_p]),
+    "cw_output_answer": (c_int32, [c_void_p, c_int32, c_void_p, c_int32, c_float, c_void_p, c_void_p]),
+    "cw_answer_bytes": (c_size_t, [c_int32, c_int32]),
+    "cw_fc4": (c_int32, [c_void_p, POINTER(cw_fc4_args), c_void_p]),
+    "cw_answer": (c_int32, [c_void_p, POINTER(cw_answer_args), c_void_p]),
+    "cw_answer_workspace_bytes": (c_size_t, []),
     "cw_release": (c_int32, [c_void_p, c_int32]),
     "cw_exec_duration_ns": (c_int32, [c_void_p, c_int32, POINTER(c_uint64)]),
     "cw_profile_measure": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_uint32, POINTER(cw_profile), c_void_p]),
@@ -169,6 +188,44 @@ def _ptr(x):
     raise TypeError(type(x))
 
 
+_element_codes = {}
+
+
+def _element_code(dtype):
+    """CW_DTYPE_* of a torch dtype."""
+    if not _element_codes:
+        import torch
+        _element_codes.update({torch.float16: CW_DTYPE_FP16, torch.bfloat16: CW_DTYPE_BF16, torch.float32: CW_DTYPE_FP32})
+    try:
+        return _element_codes[dtype]
+    except KeyError:
+        raise TypeError("%s is no element type of this call" % dtype) from None
+
+
+def _matrix(t, what, device, shape=None):
+    """(address, row stride) of a matrix on GPU `device` whose rows are contiguous."""
+    have = t.shape
+    if t.get_device() != device:
+        raise ValueError("%s is not on the context's GPU" % what)
+    if len(have) != 2 or (shape is not None and tuple(have) != shape):
+        raise ValueError("%s is %s, not %s" % (what, tuple(have), shape or "a matrix"))
+    rows, step = t.stride()
+    if step != 1 and have[1] > 1:
+        raise ValueError("%s: elements of a row must be contiguous" % what)
+    return t.data_ptr(), rows
+
+
+def _vector(t, what, device, count, kind):
+    """Address of a contiguous tensor of `count` elements of the type `kind` there, or None."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError("%s is not on the context's GPU" % what)
+    if t.numel() != count or not t.is_contiguous() or str(t.dtype) != kind:
+        raise ValueError("%s must be %d contiguous elements of %s" % (what, count, kind))
+    return t.data_ptr()
+
+
 def _stream(s):
     if s is None:
         return None
@@ -189,6 +246,7 @@ class Context:
         if st != CW_OK:
             self._h = c_void_p()
             raise CwError(st, "cw_create: " + lib().cw_last_error(None).decode())
+        self._device = lib().cw_context_device(self._h)
 
     def _check(self, st):
         if st < 0:
@@ -286,6 +344,66 @@ class Context:
 
     def output(self, slot, host_probs, host_logits=None, stream=None):
         self._check(lib().cw_output(self._h, slot, _ptr(host_probs), _ptr(host_logits), _stream(stream)))
+
+    def output_answer(self, slot, host_answer, given=None, top=0, scale=1.0, stream=None):
+        """host_answer: answer_bytes(batch, top) bytes; split_answer() names their parts once `stream` has been synchronised."""
+        self._check(lib().cw_output_answer(self._h, slot, _ptr(given), top, scale, _ptr(host_answer), _stream(stream)))
+
+    @staticmethod
+    def answer_bytes(batch, top):
+        return lib().cw_answer_bytes(batch, top)
+
+    @staticmethod
+    def split_answer(host_answer, batch, top):
+        """The parts of an answer in host memory (a numpy array or a CPU tensor), as views."""
+        flat = host_answer if isinstance(host_answer, np.ndarray) else host_answer.numpy()
+        w = flat.reshape(-1).view(np.uint8)[:batch * (12 + 8 * top)].view(np.int32)
+        return {"logp": w[:batch].view(np.float32), "rank": w[batch:2 * batch], "entropy": w[2 * batch:3 * batch].view(np.float32),
+                "top_id": w[3 * batch:(3 + top) * batch].reshape(batch, top),
+                "top_logp": w[(3 + top) * batch:].view(np.float32).reshape(batch, top)}
+
+    # -- single operators over device tensors
+    def fc4(self, x, q, scales, y, group, zeros=None, bias=None, stream=None):
+        """y[rows][cout] = bias + x[rows][cin] times the 4-bit weights q[cout][ceil(cin / 2)] (uint8) with scales and zeros
+        [cout][ceil(cin / group)]: torch tensors on the context's GPU; y is written."""
+        rows, cin = x.shape
+        cout = y.shape[1] if len(y.shape) == 2 else -1
+        if group < 1:
+            raise ValueError("group must be positive")
+        parts = (cout, (cin + group - 1) // group)
+        on = self._device
+        xp, xs = _matrix(x, "x", on)
+        qp, qs = _matrix(q, "q", on, (cout, (cin + 1) // 2))
+        sp, ss = _matrix(scales, "scales", on, parts)
+        zp, zs = _matrix(zeros, "zeros", on, parts) if zeros is not None else (None, 0)
+        yp, ys = _matrix(y, "y", on, (rows, cout))
+        if q.element_size() != 1 or (zeros is not None and zeros.element_size() != 1):
+            raise TypeError("q and zeros hold bytes")
+        a = cw_fc4_args(xp, qp, sp, zp, _vector(bias, "bias", on, cout, "torch.float32"), yp, xs, qs, ss, zs, ys,
+                        rows, cin, cout, group, _element_code(x.dtype), _element_code(scales.dtype), _element_code(y.dtype))
+        self._check(lib().cw_fc4(self._h, byref(a), _stream(stream)))
+
+    def answer(self, logits, given=None, logp=None, rank=None, entropy=None, top_id=None, top_logp=None, scale=1.0, workspace=None,
+               stream=None):
+        """The answer of every row of logits[rows][classes]: torch tensors on the context's GPU, given and rank int32, the others
+        fp32; those that are not None are written, top_id and top_logp [rows][top].  workspace: uint8, zeros before its first call."""
+        rows, classes = logits.shape
+        on = self._device
+        lp, ls = _matrix(logits, "logits", on)
+        top = 0
+        if top_id is not None:
+            top = top_id.shape[1]
+        a = cw_answer_args(lp, _vector(given, "given", on, rows, "torch.int32"), _vector(logp, "logp", on, rows, "torch.float32"),
+                           _vector(rank, "rank", on, rows, "torch.int32"), _vector(entropy, "entropy", on, rows, "torch.float32"),
+                           _vector(top_id, "top_id", on, rows * top, "torch.int32"), _vector(top_logp, "top_logp", on, rows * top, "torch.float32"),
+                           None if workspace is None else _vector(workspace, "workspace", on, workspace.numel(), "torch.uint8"),
+                           0 if workspace is None else workspace.numel(), ls,
+                           rows, classes, top, _element_code(logits.dtype), scale)
+        self._check(lib().cw_answer(self._h, byref(a), _stream(stream)))
+
+    @staticmethod
+    def answer_workspace_bytes():
+        return lib().cw_answer_workspace_bytes()
 
     def release(self, slot):
         self._check(lib().cw_release(self._h, slot))

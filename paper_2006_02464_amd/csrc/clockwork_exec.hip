@@ -360,6 +360,18 @@ hipError_t issue(cw_ctx *c, const ModelRt *m, const Bases &s, const Launch &l, h
             }
             return launch_fc(dt, a, st);
         }
+        case K_FC4: {
+            Fc4Args a = l.fc4;
+            const Fc4Layout lay = fc4_layout(a.cin, a.cout, a.group);
+            const char *w = resolve(c, m, s, l.w);
+            a.x = resolve(c, m, s, l.x);
+            a.q = reinterpret_cast<const uint8_t *>(w);
+            a.scales = w + lay.scales;
+            a.zeros = reinterpret_cast<const uint8_t *>(w + lay.zeros);
+            a.bias = reinterpret_cast<const float *>(resolve(c, m, s, l.bias));
+            a.y = resolve(c, m, s, l.y);
+            return launch_fc4(a, st);
+        }
         case K_SOFTMAX: {
             SoftmaxArgs a = l.sm;
             a.z = reinterpret_cast<const float *>(resolve(c, m, s, l.x));
@@ -1041,6 +1053,7 @@ int32_t cw_load_weights_begin(cw_ctx *c, int32_t model_id, const void *host_blob
     std::vector<PackItem> items;
     items.reserve(m->m.wslots.size());
     for (const WeightSlot &ws : m->m.wslots) {
+        if (ws.group) continue;
         PackItem t{};
         t.src = reinterpret_cast<const uint16_t *>(c->staging + ws.blob_w_off);
         t.dst = reinterpret_cast<uint16_t *>(at(ws.packed_w_off));
@@ -1053,6 +1066,12 @@ int32_t cw_load_weights_begin(cw_ctx *c, int32_t model_id, const void *host_blob
         items.push_back(t);
     }
     if ((e = launch_pack_model(items.data(), (int)items.size(), st)) != hipSuccess) return bail(e, "pack_model");
+    for (const WeightSlot &ws : m->m.wslots)
+        if (ws.group) {
+            e = launch_pack_fc4(c->staging + ws.blob_w_off, at(ws.packed_w_off), reinterpret_cast<const float *>(c->staging + ws.blob_b_off),
+                                reinterpret_cast<float *>(at(ws.packed_b_off)), ws.cin, ws.cout, ws.group, st);
+            if (e != hipSuccess) return bail(e, "pack_fc4");
+        }
     for (const WeightSlot &ws : m->m.wslots)
         if (ws.wino_bytes) {
             e = launch_pack_winograd(m->m.dtype, c->staging + ws.blob_w_off, at(ws.wino_w_off), ws.cout, ws.cin, st);
@@ -1328,6 +1347,122 @@ int32_t cw_output(cw_ctx *c, int32_t slot, float *host_probs, float *host_logits
     }
     CW_HIP(c, hipEventRecord(s.released, st));
     free_slot(c, &s, true);
+    return CW_OK;
+}
+
+// What cw_answer and cw_output_answer refuse in common.
+static int32_t answer_checks(cw_ctx *c, int32_t top, float scale) {
+    if (top < 0 || top > kAnswerMostTop) return set_err(c, CW_ERR_UNSUPPORTED, "top must be 0..64");
+    if (!(scale > 0.f) || !std::isfinite(scale)) return set_err(c, CW_ERR_INVALID, "scale must be finite and positive");
+    return CW_OK;
+}
+
+size_t cw_answer_bytes(int32_t batch, int32_t top) {
+    return batch < 0 || top < 0 || top > kAnswerMostTop ? 0 : (size_t)batch * (12 + 8 * (size_t)top);
+}
+
+int32_t cw_output_answer(cw_ctx *c, int32_t slot, const int32_t *host_given, int32_t top, float scale, void *host_answer, void *stream) {
+    if (!c) return CW_ERR_INVALID;
+    if (!host_answer) return set_err(c, CW_ERR_INVALID, "null output buffer");
+    int32_t rc = answer_checks(c, top, scale);
+    if (rc != CW_OK) return rc;
+    if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
+    if (slot < 0 || slot >= kMaxSlots || c->slots[slot].state != SLOT_EXECUTED)
+        return set_err(c, CW_ERR_NO_INPUT, "slot holds no result");
+    Slot &s = c->slots[slot];
+    ModelRt *m = get_model(c, s.model);
+    // The answer is put together in the slot's own memory: its input, which nothing reads any more behind the EXEC, or its probabilities.
+    const size_t batch = (size_t)s.batch, bytes = cw_answer_bytes(s.batch, top), need = (bytes + 15) / 16 * 16 + batch * 4;
+    const size_t in_b = s.logits_off - s.in_off, probs_b = s.off + s.bytes - s.probs_off;
+    if (need > std::max(in_b, probs_b)) return set_err(c, CW_ERR_NO_MEMORY, "the answer does not fit the slot's memory");
+    char *dev = c->io + (in_b >= probs_b ? s.in_off : s.probs_off), *given = dev + (bytes + 15) / 16 * 16;
+    DeviceGuard g(c->device);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    wait_quietly(c, s, s.exec_end, st);
+    CW_HIP(c, hipStreamWaitEvent(st, s.exec_end, 0));
+    AnswerArgs a{};
+    a.x = c->io + s.logits_off;
+    a.stride = a.classes = m->m.classes;
+    a.rows = s.batch; a.top = top; a.dtype = DT_F32; a.scale = scale;
+    a.logp = reinterpret_cast<float *>(dev);
+    a.rank = reinterpret_cast<int32_t *>(dev + batch * 4);
+    a.entropy = reinterpret_cast<float *>(dev + batch * 8);
+    if (top) {
+        a.top_id = reinterpret_cast<int32_t *>(dev + batch * 12);
+        a.top_logp = reinterpret_cast<float *>(dev + batch * (12 + 4 * (size_t)top));
+    }
+    // From the first write on the slot holds no input and no result any more: a failure releases it too.
+    int32_t status = CW_OK;
+    auto step = [&](hipError_t e, const char *what) {
+        if (e != hipSuccess && status == CW_OK) status = hip_fail(c, e, what);
+        return e == hipSuccess;
+    };
+    if (host_given) {
+        a.given = reinterpret_cast<const int32_t *>(given);
+        step(hipMemcpyAsync(given, host_given, batch * 4, hipMemcpyHostToDevice, st), "copy of the given classes");
+    }
+    if (status == CW_OK && step(launch_answer(a, st), "answer")) {
+        char *view = device_view(host_answer, bytes);
+        if (view) step(launch_copy_out(view, dev, nullptr, nullptr, bytes, st), "copy_out");
+        else step(hipMemcpyAsync(host_answer, dev, bytes, hipMemcpyDeviceToHost, st), "copy of the answer");
+    }
+    if (hipEventRecord(s.released, st) != hipSuccess) (void)hipStreamSynchronize(st);
+    free_slot(c, &s, true);
+    return status;
+}
+
+static bool element_type(int32_t dtype) { return dtype >= DT_F16 && dtype <= DT_F32; }
+static bool aligned_to(const void *p, int32_t dtype) { return reinterpret_cast<uintptr_t>(p) % (dtype == DT_F32 ? 4 : 2) == 0; }
+
+int32_t cw_fc4(cw_ctx *c, const cw_fc4_args *r, void *stream) {
+    if (!c) return CW_ERR_INVALID;
+    if (!r) return set_err(c, CW_ERR_INVALID, "null arguments");
+    if (!element_type(r->x_dtype) || !element_type(r->scale_dtype) || !element_type(r->y_dtype)) return set_err(c, CW_ERR_INVALID, "bad dtype");
+    if (r->rows < 0 || r->cin < 1 || r->cout < 1) return set_err(c, CW_ERR_INVALID, "bad size");
+    if (r->rows > kFc4MostRows || r->cin > kFc4MostIn || r->cout > kFc4MostOut) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
+    if (r->group < 32 || r->group % 32 != 0) return set_err(c, CW_ERR_UNSUPPORTED, "a group holds a multiple of 32 inputs");
+    if (r->x_stride < 0 || r->q_stride < 0 || r->scale_stride < 0 || (r->zeros && r->zero_stride < 0) || (r->rows > 1 && r->y_stride < r->cout))
+        return set_err(c, CW_ERR_INVALID, "bad stride");
+    if (r->rows > 0) {
+        if (!r->x || !r->q || !r->scales || !r->y) return set_err(c, CW_ERR_INVALID, "null pointer");
+        if (!aligned_to(r->x, r->x_dtype) || !aligned_to(r->scales, r->scale_dtype) || !aligned_to(r->y, r->y_dtype) || !aligned_to(r->bias, DT_F32))
+            return set_err(c, CW_ERR_INVALID, "misaligned pointer");
+    }
+    if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
+    if (r->rows == 0) return CW_OK;
+    Fc4Args a{r->x, r->q, r->scales, r->zeros, r->bias, r->y, r->x_stride, r->q_stride, r->scale_stride, r->zero_stride, r->y_stride,
+              r->rows, r->cin, r->cout, r->group, (DType)r->x_dtype, (DType)r->scale_dtype, (DType)r->y_dtype};
+    DeviceGuard g(c->device);
+    if (!g.ok) return hip_fail(c, hipGetLastError(), "hipSetDevice");
+    CW_HIP(c, launch_fc4(a, static_cast<hipStream_t>(stream)));
+    return CW_OK;
+}
+
+size_t cw_answer_workspace_bytes(void) { return answer_workspace_bytes(); }
+
+int32_t cw_answer(cw_ctx *c, const cw_answer_args *r, void *stream) {
+    if (!c) return CW_ERR_INVALID;
+    if (!r) return set_err(c, CW_ERR_INVALID, "null arguments");
+    if (!element_type(r->dtype)) return set_err(c, CW_ERR_INVALID, "bad dtype");
+    if (r->rows < 0 || r->classes < 1) return set_err(c, CW_ERR_INVALID, "bad size");
+    if (r->classes > kAnswerMostClasses) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
+    const int32_t rc = answer_checks(c, r->top, r->scale);
+    if (rc != CW_OK) return rc;
+    if (r->stride < 0) return set_err(c, CW_ERR_INVALID, "bad stride");
+    if ((r->logp || r->rank) && !r->given && r->rows > 0) return set_err(c, CW_ERR_INVALID, "logp and rank need `given`");
+    if (r->rows > 0) {
+        if (!r->logits || (r->top > 0) != (r->top_id != nullptr) || (r->top > 0) != (r->top_logp != nullptr)) return set_err(c, CW_ERR_INVALID, "null pointer, or top classes without `top`");
+        if (!aligned_to(r->logits, r->dtype) || !aligned_to(r->given, DT_F32) || !aligned_to(r->logp, DT_F32) || !aligned_to(r->rank, DT_F32) ||
+            !aligned_to(r->entropy, DT_F32) || !aligned_to(r->top_id, DT_F32) || !aligned_to(r->top_logp, DT_F32) || reinterpret_cast<uintptr_t>(r->workspace) % 16 != 0)
+            return set_err(c, CW_ERR_INVALID, "misaligned pointer");
+    }
+    if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
+    if (r->rows == 0) return CW_OK;
+    AnswerArgs a{r->logits, r->given, r->logp, r->rank, r->entropy, r->top_id, r->top_logp,
+                 r->workspace_bytes >= answer_workspace_bytes() ? r->workspace : nullptr, r->stride, r->rows, r->classes, r->top, (DType)r->dtype, r->scale};
+    DeviceGuard g(c->device);
+    if (!g.ok) return hip_fail(c, hipGetLastError(), "hipSetDevice");
+    CW_HIP(c, launch_answer(a, static_cast<hipStream_t>(stream)));
     return CW_OK;
 }
 

@@ -10,7 +10,7 @@ namespace cw {
 typedef _Float16 f16;
 typedef __bf16 bf16;
 
-enum DType : int32_t { DT_F16 = 0, DT_BF16 = 1 };
+enum DType : int32_t { DT_F16 = 0, DT_BF16 = 1, DT_F32 = 2 };   // DT_F32: Fc4Args and AnswerArgs only
 
 // Kernel families (cw_launch_info.kind).
 enum Kind : int32_t {
@@ -24,6 +24,7 @@ enum Kind : int32_t {
     K_COPY_CHANNELS = 8,  // a tensor into a channel range of a wider one (CONCAT sources that cannot write there themselves)
     K_WINO_INPUT = 9,   // Winograd F(2x2, 3x3): input tiles -> 16 transformed matrices
     K_WINO_OUTPUT = 10, // ... 16 product matrices -> 2x2 output tiles, fused epilogue
+    K_FC4 = 12,         // fully connected over 4-bit weights
     K_RESIDENT = 11,    // a run of convolution layers as one launch of resident workgroups (kernels_resident.hip)
 };
 
@@ -303,6 +304,50 @@ struct SoftmaxArgs {
     const float *bias;
 };
 
+// Fully connected over 4-bit weights (kernels_fc4.hip); the fields are those of cw_fc4_args.
+struct Fc4Args {
+    const void *x;
+    const uint8_t *q;
+    const void *scales;
+    const uint8_t *zeros;
+    const float *bias;
+    void *y;
+    int64_t x_stride, q_stride, scale_stride, zero_stride, y_stride;
+    int32_t rows, cin, cout, group;
+    DType x_dtype, scale_dtype, y_dtype;
+};
+constexpr int kFc4MostIn = 1 << 24, kFc4MostOut = 1 << 24, kFc4MostRows = 1 << 20;
+// Parts of an FC4's packed weights (byte offsets): q rows, scales in the storage type, zero points.
+struct Fc4Layout {
+    size_t q_row, groups, scales, zeros, bytes;
+};
+inline Fc4Layout fc4_layout(int32_t cin, int32_t cout, int32_t group) {
+    Fc4Layout l;
+    l.q_row = ((size_t)cin + 1) / 2;
+    l.groups = ((size_t)cin + group - 1) / group;
+    l.scales = ((size_t)cout * l.q_row + 255) / 256 * 256;
+    l.zeros = (l.scales + (size_t)cout * l.groups * 2 + 255) / 256 * 256;
+    l.bytes = l.zeros + (size_t)cout * l.groups;
+    return l;
+}
+
+// The answer over rows of logits (kernels_answer.hip); the fields are those of cw_answer_args.
+struct AnswerArgs {
+    const void *x;
+    const int32_t *given;
+    float *logp;
+    int32_t *rank;
+    float *entropy;
+    int32_t *top_id;
+    float *top_logp;
+    void *workspace;
+    int64_t stride;
+    int32_t rows, classes, top;
+    DType dtype;
+    float scale;
+};
+constexpr int kAnswerMostTop = 64, kAnswerMostClasses = 1 << 24;
+
 // Tile shapes the conv kernel is instantiated for (fixed at plan time per layer).
 // (pixels x channels per workgroup; "wN" = N waves when not 4, each wave then owning 64x64;
 // "k128" = K slices of 128 instead of 64, for Cin % 128 == 0; "gN" = N groups of waves that split
@@ -460,6 +505,12 @@ struct PackArgs {
 };
 static_assert(sizeof(PackArgs) <= 4096, "kernel arguments");
 hipError_t launch_pack_model(PackItem *items, int n, hipStream_t s);
+// Canonical parts of an FC4's weights (q, scales, zero points: offsets in bytes from src, even) to the places of fc4_layout; and the bias.
+hipError_t launch_pack_fc4(const char *src, char *dst, const float *bias_src, float *bias_dst, int32_t cin, int32_t cout, int32_t group, hipStream_t s);
+hipError_t launch_fc4(const Fc4Args &a, hipStream_t s);
+void fc4_grid(const Fc4Args &a, dim3 *grid, int *block);   // of that launch
+hipError_t launch_answer(const AnswerArgs &a, hipStream_t s);
+size_t answer_workspace_bytes();
 // debug read-back: NHWC storage type (ld elements per pixel) -> fp32 NCHW
 hipError_t launch_nhwc_to_nchw_f32(DType dt, const void *src, float *dst, int B, int C, int H,
                                    int W, int ld, hipStream_t s);

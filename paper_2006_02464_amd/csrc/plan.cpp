@@ -127,8 +127,8 @@ int32_t model_init(Model *m, const cw_op *ops, int32_t n_ops, int32_t in_c, int3
     m->winograd = winograd;
     m->wslots.clear();
     m->op_wslot.assign(n_ops, -1);
-    if (ops[n_ops - 2].op != CW_OP_FC || ops[n_ops - 1].op != CW_OP_SOFTMAX)
-        return fail(err, CW_ERR_UNSUPPORTED, "op list must end with FC, SOFTMAX");
+    if ((ops[n_ops - 2].op != CW_OP_FC && ops[n_ops - 2].op != CW_OP_FC4) || ops[n_ops - 1].op != CW_OP_SOFTMAX)
+        return fail(err, CW_ERR_UNSUPPORTED, "op list must end with FC or FC4, SOFTMAX");
 
     size_t blob_w = 0;
     for (int i = 0; i < n_ops; ++i) {
@@ -200,13 +200,17 @@ int32_t model_init(Model *m, const cw_op *ops, int32_t n_ops, int32_t in_c, int3
                 if (i != n_ops - 2 || ops[o.input_from].op != CW_OP_GAVGPOOL || o.cin % 256 != 0 || o.cout < 1)
                     return fail(err, CW_ERR_UNSUPPORTED, "op %d: FC must follow the global average pool, cin %% 256 == 0", i);
                 break;
+            case CW_OP_FC4:
+                if (i != n_ops - 2 || ops[o.input_from].op != CW_OP_GAVGPOOL || o.cout < 1 || o.cout > kFc4MostOut || o.groups < 32 || o.groups % 32 != 0)
+                    return fail(err, CW_ERR_UNSUPPORTED, "op %d: FC4 must follow the global average pool, its groups hold a multiple of 32 inputs", i);
+                break;
             case CW_OP_SOFTMAX:
                 if (i != n_ops - 1 || o.input_from != n_ops - 2 || o.cout != o.cin)
                     return fail(err, CW_ERR_UNSUPPORTED, "op %d: SOFTMAX must be last and read the FC", i);
                 break;
             default: return fail(err, CW_ERR_INVALID, "op %d: unknown op code", i);
         }
-        if (o.op != CW_OP_FC && o.op != CW_OP_SOFTMAX && o.op != CW_OP_GAVGPOOL && i > 0) {
+        if (o.op != CW_OP_FC && o.op != CW_OP_FC4 && o.op != CW_OP_SOFTMAX && o.op != CW_OP_GAVGPOOL && i > 0) {
             const int src = ops[o.input_from].op;
             if (src != CW_OP_CONV && src != CW_OP_MAXPOOL && src != CW_OP_CONCAT)
                 return fail(err, CW_ERR_UNSUPPORTED, "op %d: spatial op needs a spatial input", i);
@@ -217,6 +221,19 @@ int32_t model_init(Model *m, const cw_op *ops, int32_t n_ops, int32_t in_c, int3
                 return fail(err, CW_ERR_UNSUPPORTED, "op %d: average pool needs a spatial input", i);
         }
         m->shapes[i] = out;
+        if (o.op == CW_OP_FC4) {
+            WeightSlot ws{};
+            ws.op_index = i;
+            ws.cout = o.cout; ws.cin = ws.cinp = o.cin;
+            ws.kh = ws.kw = ws.khp = ws.kwp = 1;
+            ws.group = o.groups;
+            ws.blob_w_off = blob_w;
+            const Fc4Layout lay = fc4_layout(o.cin, o.cout, o.groups);
+            ws.packed_w_bytes = lay.bytes;
+            blob_w += align_up(o.cout * lay.q_row, 2) + o.cout * lay.groups * 2 + align_up(o.cout * lay.groups, 2);
+            m->op_wslot[i] = (int)m->wslots.size();
+            m->wslots.push_back(ws);
+        }
         if (o.op == CW_OP_CONV || o.op == CW_OP_FC) {
             WeightSlot ws{};
             ws.op_index = i;
@@ -254,7 +271,7 @@ int32_t model_init(Model *m, const cw_op *ops, int32_t n_ops, int32_t in_c, int3
     for (WeightSlot &ws : m->wslots) {
         ws.blob_b_off = blob_b;
         blob_b += (size_t)ws.cout * 4;
-        ws.packed_w_bytes = (size_t)ws.cout * ws.khp * ws.kwp * ws.cinp * 2;
+        if (!ws.group) ws.packed_w_bytes = (size_t)ws.cout * ws.khp * ws.kwp * ws.cinp * 2;
         ws.packed_w_off = place(ws.packed_w_bytes);
     }
     for (WeightSlot &ws : m->wslots) ws.packed_b_off = place((size_t)ws.cout * 4);
@@ -1221,6 +1238,28 @@ int32_t plan_build(const Model &m, int32_t batch, const PlanOverride &ov, Plan *
                 p.launches.push_back(l);
                 break;
             }
+            case CW_OP_FC4: {
+                const WeightSlot &ws = m.wslots[m.op_wslot[i]];
+                const Fc4Layout lay = fc4_layout(o.cin, o.cout, o.groups);
+                p.op_out[i] = Ref{SP_SLOT_LOGITS, 0};
+                Launch l{};
+                l.kind = K_FC4;
+                l.op_index = i;
+                l.fc4.rows = batch; l.fc4.cin = o.cin; l.fc4.cout = o.cout; l.fc4.group = o.groups;
+                l.fc4.x_stride = o.cin; l.fc4.q_stride = (int64_t)lay.q_row;
+                l.fc4.scale_stride = l.fc4.zero_stride = (int64_t)lay.groups; l.fc4.y_stride = o.cout;
+                l.fc4.x_dtype = l.fc4.y_dtype = DT_F32; l.fc4.scale_dtype = m.dtype;
+                l.x = src;
+                l.w = Ref{SP_WEIGHTS, ws.packed_w_off};
+                l.bias = Ref{SP_WEIGHTS, ws.packed_b_off};
+                l.y = p.op_out[i];
+                l.info.gemm_m = batch; l.info.gemm_n = o.cout; l.info.gemm_k = o.cin;
+                l.info.flops = 2 * (int64_t)batch * o.cout * o.cin;
+                l.info.bytes = (int64_t)batch * o.cin * 4 + (int64_t)o.cout * (int64_t)(lay.q_row + 3 * lay.groups) + o.cout * 4 + (int64_t)batch * o.cout * 4;
+                snprintf(l.info.name, sizeof l.info.name, "fc4");
+                p.launches.push_back(l);
+                break;
+            }
             case CW_OP_SOFTMAX: {
                 p.op_out[i] = Ref{SP_SLOT_PROBS, 0};
                 if (!p.launches.empty() && p.launches.back().kind == K_FC && p.launches.back().probs.space == SP_SLOT_PROBS) {
@@ -1519,6 +1558,7 @@ int32_t plan_build(const Model &m, int32_t batch, const PlanOverride &ov, Plan *
                 else if (l.partial.space != SP_NONE) { g = dim3((l.fc.Out + 15) / 16, (l.fc.B + 15) / 16, kFcWaves); b = 64; }
                 else { g = dim3((l.fc.Out + 15) / 16, (l.fc.B + 15) / 16); b = 512; }
                 break;
+            case K_FC4: fc4_grid(l.fc4, &g, &b); break;
             case K_SOFTMAX: g = dim3(l.sm.B); b = 256; break;
             case K_DWCONV:
                 if (l.dw_fused) {

@@ -35,6 +35,7 @@ struct Launch {
     CastArgs cast{};
     PoolArgs pool{};
     FcArgs fc{};
+    Fc4Args fc4{};
     SoftmaxArgs sm{};
     DwArgs dw{};
     CopyArgs copy{};
@@ -100,6 +101,7 @@ struct WeightSlot {        // one op that owns weights
     size_t packed_w_bytes;
     int32_t cout, cin, kh, kw, khp, kwp, cinp;   // cin: input channels per filter (1 for a depthwise convolution)
     bool depthwise;
+    int32_t group;         // FC4: inputs of a group (packed_w_off is the start of fc4_layout's parts), else 0
     size_t wino_w_off;     // Winograd-transformed weights U[16][cout][cin] (0 bytes: none)
     size_t wino_bytes;
 };
