@@ -1,100 +1,305 @@
 // The answer of a row of logits: log probability and rank of a given class, entropy, the likeliest classes (cw_answer has the definitions).
 #include <cmath>
 
-#include "common.h"
+#include "conv_common.h"
 
 namespace cw {
 
-__device__ static inline float logit(const AnswerArgs &a, int64_t i) {
-    return a.dtype == DT_F32 ? static_cast<const float *>(a.x)[i] : a.dtype == DT_F16 ? (float)static_cast<const f16 *>(a.x)[i] : (float)static_cast<const bf16 *>(a.x)[i];
+// One pass.  A workgroup takes a row, or a run of its segments, 8192 logits at a time in registers, 16 bytes a load.  Every thread keeps a
+// maximum m, S = sum 2^d and T = sum d 2^d with d = (x - m) scale / ln 2 of its own (a new maximum rescales both once a segment), the
+// threads meet at the end.  For the top classes a segment gives those of its logits that can still be among them to a list in LDS.
+constexpr int kThreads = 256, kEach = 32, kSegment = kThreads * kEach;
+constexpr int kParts = 32;                         // workgroups a row at most
+constexpr int kRecords = 1024;                     // of rows that are shared
+constexpr int kRecordBytes = 16 + 8 * kAnswerMostTop;
+constexpr int kCounterSlots = 256;                 // rows that can be shared
+// Logits above the k-th largest of the threads' maxima lie with fewer than k threads; those equal to it are taken 2048 at a time.
+constexpr int kList = kAnswerMostTop + (kAnswerMostTop - 1) * kEach + kAnswerMostTop + kThreads * 8;
+
+template <typename T>
+struct Vec { static constexpr int N = 16 / sizeof(T); };
+
+// Of all 64 lanes, in all of them.
+template <typename V, typename F>
+__device__ static inline V wave_all(V v, F f) {
+    static_assert(sizeof(V) == 4, "a register");
+    auto dpp = [](V x, auto control) {
+        return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(control)::value, 0xf, 0xf, false));
+    };
+    v = f(v, dpp(v, std::integral_constant<int, 0xB1>{}));    // lanes 1 0 3 2
+    v = f(v, dpp(v, std::integral_constant<int, 0x4E>{}));    // lanes 2 3 0 1
+    v = f(v, dpp(v, std::integral_constant<int, 0x141>{}));   // mirrored in 8
+    v = f(v, dpp(v, std::integral_constant<int, 0x140>{}));   // mirrored in 16
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    v = f(__builtin_bit_cast(V, (unsigned)r[0]), __builtin_bit_cast(V, (unsigned)r[1]));
+    const unsigned w = __builtin_bit_cast(unsigned, v);
+    r = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return f(__builtin_bit_cast(V, (unsigned)r[0]), __builtin_bit_cast(V, (unsigned)r[1]));
 }
 
-// The larger logit, and of equal ones the lower index, comes first.
-__device__ static inline bool before(float x, int i, float y, int j) { return x > y || (x == y && i < j); }
+// Larger numbers for larger floats (the zeros are equal).
+__device__ static inline unsigned order_of(float x) {
+    const unsigned u = __builtin_bit_cast(unsigned, x + 0.f);
+    return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ static inline float of_order(unsigned o) { return __builtin_bit_cast(float, o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)); }
+// Larger for what comes first: the larger logit, of equal ones the lower class.
+__device__ static inline uint64_t key_of(float x, int i) { return (uint64_t)order_of(x) << 32 | (unsigned)~i; }
 
-// One workgroup a row, a pass for each question.
-__global__ __launch_bounds__(256) void answer_kernel(const AnswerArgs a) {
-    __shared__ float fs[256];
-    __shared__ int is[256];
+// m, S and T of two sets of logits.
+struct Soft { float m, s, t; };
+__device__ static inline Soft join(const Soft &a, const Soft &b, float c2) {
+    const float m = fmaxf(a.m, b.m), base = m == -INFINITY ? 0.f : m;
+    const float da = fmaxf((a.m - base) * c2, -1e30f), db = fmaxf((b.m - base) * c2, -1e30f);   // -inf times 0 is no number
+    const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
+    return {m, a.s * ea + b.s * eb, (a.t + a.s * da) * ea + (b.t + b.s * db) * eb};
+}
+
+struct AnswerLds {
+    uint64_t list[kList], best[kAnswerMostTop];
+    unsigned order[kThreads];
+    float m[4], s[4], t[4];
+    int rank[4];
+    int n, last;
+};
+
+// The k first of list[0..n) in order; returns how many there are.  All threads.
+__device__ static inline int first_of(AnswerLds &l, int n, int k) {
     const int t = threadIdx.x;
-    const int64_t row = blockIdx.x, base = row * a.stride;
-    float m = -INFINITY;
-    int bad = 0;
-    for (int i = t; i < a.classes; i += 256) {
-        const float x = logit(a, base + i);
-        bad |= !(x < INFINITY);
-        m = fmaxf(m, x);
+    for (int at = t; at < n; at += kThreads) {
+        const uint64_t mine = l.list[at];
+        int rank = 0;
+        for (int o = 0; o < n; ++o) rank += l.list[o] > mine;
+        if (rank < k) l.best[rank] = mine;
     }
-    auto sum = [&](float v) {
-        __syncthreads();
-        fs[t] = v;
-        __syncthreads();
-        for (int n = 128; n; n >>= 1) {
-            if (t < n) fs[t] += fs[t + n];
-            __syncthreads();
-        }
-        return fs[0];
-    };
-    fs[t] = m; is[t] = bad;
     __syncthreads();
-    for (int n = 128; n; n >>= 1) {
-        if (t < n) { fs[t] = fmaxf(fs[t], fs[t + n]); is[t] |= is[t + n]; }
-        __syncthreads();
-    }
-    m = fs[0]; bad = is[0];
+    const int have = n < k ? n : k;
+    if (t < have) l.list[t] = l.best[t];
+    __syncthreads();
+    return have;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, int parts) {
+    constexpr int N = Vec<T>::N, CHUNKS = kEach / N, CHUNK = kThreads * N;
+    __shared__ AnswerLds l;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int row = blockIdx.x / parts, part = blockIdx.x - row * parts, k = a.top;
+    const T *x = static_cast<const T *>(a.x) + row * a.stride;
+    const int segments = (a.classes + kSegment - 1) / kSegment;
+    const int seg0 = (int)((int64_t)segments * part / parts), seg1 = (int)((int64_t)segments * (part + 1) / parts);
+    const float c2 = a.scale * 1.44269504f;
     const int g = a.given ? a.given[row] : -1;
     const bool inside = g >= 0 && g < a.classes;
-    const float xg = inside ? logit(a, base + g) : 0.f;
-    float S = 0.f, T = 0.f, R = 0.f;
-    for (int i = t; i < a.classes; i += 256) {
-        const float x = logit(a, base + i);
-        if (x > -INFINITY) {
-            const float d = (x - m) * a.scale, e = expf(d);
-            S += e;
-            if (e > 0.f) T += e * d;
+    const float xg = inside ? (float)x[g] : INFINITY;
+
+    Soft soft{-INFINITY, 0.f, 0.f};
+    int before = 0;       // logits that come before the given one
+    int have = 0;         // classes in the list, the first `have` of it in order
+    float bar = -INFINITY;   // the k-th of them: later ones have to be larger
+    for (int seg = seg0; seg < seg1; ++seg) {
+        float v[kEach];
+        const int base = seg * kSegment, count = a.classes - base < kSegment ? a.classes - base : kSegment;
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            const int at = j * CHUNK + t * N;
+            if (at + N <= count) {
+                typedef T TN __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+                const TN raw = *reinterpret_cast<const TN *>(x + base + at);
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[j * N + e] = (float)raw[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[j * N + e] = at + e < count ? (float)x[base + at + e] : -INFINITY;
+            }
         }
-        R += before(x, i, xg, g);   // exact: at most 2^24
+        float most = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) most = fmaxf(most, v[i]);
+        {
+            const float m = fmaxf(soft.m, most), ref = m == -INFINITY ? 0.f : m;
+            const float d0 = fmaxf((soft.m - ref) * c2, -1e30f), e0 = __builtin_amdgcn_exp2f(d0);
+            soft.t = (soft.t + soft.s * d0) * e0;
+            soft.s *= e0;
+            soft.m = m;
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j) {
+                if (j * CHUNK >= count) break;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float d = (v[j * N + e] - ref) * c2, p = __builtin_amdgcn_exp2f(d);
+                    soft.s += p;
+                    soft.t = fmaf(p, fmaxf(d, -1000.f), soft.t);   // p is 0 long before
+                }
+            }
+        }
+        if (inside) {
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j) {
+                const int from = base + j * CHUNK + t * N;
+                if (from + N <= g) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) before += v[j * N + e] >= xg;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) before += v[j * N + e] > xg;
+                    if (from < g) {
+#pragma unroll
+                        for (int e = 0; e < N; ++e) before += from + e < g && v[j * N + e] == xg;
+                    }
+                }
+            }
+        }
+        if (k > 0) {
+            // What is above the bar, if it is not too much.
+            int above = 0;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) above += v[i] > bar;
+            l.order[t] = order_of(most);
+            if (t == 0) l.n = have;
+            above = wave_all(above, [](int p, int q) { return p + q; });
+            if (lane == 0) l.rank[wave] = above;
+            __syncthreads();
+            above = l.rank[0] + l.rank[1] + l.rank[2] + l.rank[3];
+            if (above == 0) { __syncthreads(); continue; }
+            float from = bar;     // candidates are above it ...
+            bool equal = false;   // ... or, with `equal`, those equal to it too, as far as they are needed
+            if (above > 256) {
+                // The k-th largest of the threads' maxima, bit by bit: at least k logits are as large.
+                unsigned o[4], tau = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = l.order[i * 64 + lane];
+                for (int bit = 31; bit >= 0; --bit) {
+                    const unsigned q = tau | 1u << bit;
+                    int c = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) c += __popcll(__ballot(o[i] >= q));
+                    if (c >= k) tau = q;
+                    if (c == k) break;
+                }
+                const float edge = of_order(tau);
+                if (edge > bar) { from = edge; equal = true; }
+            }
+            auto put = [&](float value, int i) { l.list[atomicAdd(&l.n, 1)] = key_of(value, base + i); };
+            if (most >= from) {
+#pragma unroll
+                for (int i = 0; i < kEach; ++i)
+                    if (v[i] > from) put(v[i], (i / N) * CHUNK + t * N + i % N);
+            }
+            if (equal) {
+                // At least k logits are as large as `from`: of those equal to it the first ones are needed, chunk by chunk.
+                for (int j = 0; j < CHUNKS; ++j) {
+                    __syncthreads();
+                    const int n = l.n;
+                    if (n - have >= k) break;
+                    __syncthreads();
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i)
+                        if (i / N == j && v[i] == from) put(v[i], (i / N) * CHUNK + t * N + i % N);
+                }
+            }
+            __syncthreads();
+            have = first_of(l, l.n, k);
+            if (have == k) bar = of_order((unsigned)(l.list[k - 1] >> 32));
+        }
     }
-    S = sum(S); T = sum(T); R = sum(R);
-    const bool empty = m == -INFINITY;
-    const float ls = logf(S);
+
+    // The threads meet.
+    const float m = wave_all(soft.m, [](float p, float q) { return fmaxf(p, q); });
+    {
+        const float ref = m == -INFINITY ? 0.f : m, d = fmaxf((soft.m - ref) * c2, -1e30f), e = __builtin_amdgcn_exp2f(d);
+        soft.t = (soft.t + soft.s * d) * e;
+        soft.s *= e;
+    }
+    const auto plus = [](auto p, auto q) { return p + q; };
+    soft.s = wave_all(soft.s, plus);
+    soft.t = wave_all(soft.t, plus);
+    before = wave_all(before, plus);
+    if (lane == 0) { l.m[wave] = m; l.s[wave] = soft.s; l.t[wave] = soft.t; l.rank[wave] = before; }
+    __syncthreads();
+    Soft all = join(join({l.m[0], l.s[0], l.t[0]}, {l.m[1], l.s[1], l.t[1]}, c2), join({l.m[2], l.s[2], l.t[2]}, {l.m[3], l.s[3], l.t[3]}, c2), c2);
+    before = l.rank[0] + l.rank[1] + l.rank[2] + l.rank[3];
+
+    if (parts > 1) {
+        // This part's record to memory, past the XCD's own L2; the last workgroup of the row to arrive joins them, in the parts' order.
+        int *counter = static_cast<int *>(a.workspace) + row;
+        char *records = static_cast<char *>(a.workspace) + kCounterSlots * 4 + (int64_t)row * parts * kRecordBytes;
+        {
+            int *w = reinterpret_cast<int *>(records + part * kRecordBytes);
+            auto put = [&](int i, int value) { __hip_atomic_store(w + i, value, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+            if (t == 0) {
+                put(0, __builtin_bit_cast(int, all.m));
+                put(1, __builtin_bit_cast(int, all.s));
+                put(2, __builtin_bit_cast(int, all.t));
+                put(3, before);
+            }
+            for (int i = t; i < k; i += kThreads) {
+                const uint64_t key = i < have ? l.list[i] : 0;
+                put(4 + 2 * i, (int)(unsigned)key);
+                put(5 + 2 * i, (int)(unsigned)(key >> 32));
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0);   // this thread's stores have been made
+        __syncthreads();
+        if (t == 0) l.last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+        __syncthreads();
+        if (!l.last) return;
+        if (t == 0) {
+            __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            l.n = 0;
+        }
+        auto get = [&](int p, int i) { return __hip_atomic_load(reinterpret_cast<int *>(records + p * kRecordBytes) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+        all = {-INFINITY, 0.f, 0.f};
+        before = 0;
+        for (int p = 0; p < parts; ++p) {
+            all = join(all, {__builtin_bit_cast(float, get(p, 0)), __builtin_bit_cast(float, get(p, 1)), __builtin_bit_cast(float, get(p, 2))}, c2);
+            before += get(p, 3);
+        }
+        __syncthreads();
+        if (k > 0) {
+            for (int i = t; i < parts * k; i += kThreads) {
+                const int p = i / k, j = i - p * k;
+                const uint64_t key = (uint64_t)(unsigned)get(p, 5 + 2 * j) << 32 | (unsigned)get(p, 4 + 2 * j);
+                if (key) l.list[atomicAdd(&l.n, 1)] = key;
+            }
+            __syncthreads();
+            have = first_of(l, l.n, k);
+        }
+    }
+
+    const bool bad = !(all.s < INFINITY) || all.m == INFINITY, empty = all.m == -INFINITY;
+    const float ls = logf(all.s);
     if (t == 0) {
-        float lp = bad ? NAN : !inside ? NAN : empty ? -INFINITY : (xg - m) * a.scale - ls;
+        float lp = bad || !inside ? NAN : empty ? -INFINITY : (xg - all.m) * a.scale - ls;
         if (g < 0) lp = 0.f;
         if (a.logp) a.logp[row] = lp;
-        if (a.rank) a.rank[row] = bad || !inside ? -1 : (int)R;
-        if (a.entropy) a.entropy[row] = bad ? NAN : empty ? 0.f : ls - T / S;
+        if (a.rank) a.rank[row] = bad || !inside ? -1 : before;
+        if (a.entropy) a.entropy[row] = bad ? NAN : empty ? 0.f : ls - all.t * 0.693147181f / all.s;
     }
-    float lx = INFINITY;
-    int li = -1;
-    for (int k = 0; k < a.top; ++k) {   // the first class behind the last one
-        float bx = -INFINITY;
-        int bi = 0x7fffffff;
-        for (int i = t; i < a.classes; i += 256) {
-            const float x = logit(a, base + i);
-            if (before(lx, li, x, i) && before(x, i, bx, bi)) { bx = x; bi = i; }
-        }
-        __syncthreads();
-        fs[t] = bx; is[t] = bi;
-        __syncthreads();
-        for (int n = 128; n; n >>= 1) {
-            if (t < n && before(fs[t + n], is[t + n], fs[t], is[t])) { fs[t] = fs[t + n]; is[t] = is[t + n]; }
-            __syncthreads();
-        }
-        lx = fs[0]; li = is[0];
-        if (t == 0) {
-            const bool none = bad || !(lx > -INFINITY);
-            a.top_id[row * a.top + k] = none ? -1 : li;
-            a.top_logp[row * a.top + k] = bad ? NAN : none ? -INFINITY : (lx - m) * a.scale - ls;
-        }
+    if (t < k) {
+        const bool some = t < have && !bad;
+        const uint64_t key = some ? l.list[t] : 0;
+        a.top_id[(int64_t)row * k + t] = some ? (int)~(unsigned)key : -1;
+        a.top_logp[(int64_t)row * k + t] = bad ? NAN : some ? (of_order((unsigned)(key >> 32)) - all.m) * a.scale - ls : -INFINITY;
     }
 }
 
-size_t answer_workspace_bytes() { return 1024; }
+size_t answer_workspace_bytes() { return kCounterSlots * 4 + (size_t)kRecords * kRecordBytes; }
 
 hipError_t launch_answer(const AnswerArgs &a, hipStream_t s) {
     if (a.rows < 1 || a.classes < 1 || a.classes > kAnswerMostClasses || a.top < 0 || a.top > kAnswerMostTop || (a.top > 0 && (!a.top_id || !a.top_logp))) return hipErrorInvalidValue;
-    answer_kernel<<<dim3(a.rows), 256, 0, s>>>(a);
+    const int segments = (a.classes + kSegment - 1) / kSegment;
+    int parts = 1;
+    if (a.workspace && a.rows <= kCounterSlots) {
+        parts = kRecords / a.rows;
+        parts = parts < kParts ? parts : kParts;
+        parts = parts < segments ? parts : segments;
+    }
+    const dim3 grid((unsigned)a.rows * parts);
+    if (a.dtype == DT_F32) answer_kernel<float><<<grid, kThreads, 0, s>>>(a, parts);
+    else if (a.dtype == DT_F16) answer_kernel<f16><<<grid, kThreads, 0, s>>>(a, parts);
+    else answer_kernel<bf16><<<grid, kThreads, 0, s>>>(a, parts);
     return hipGetLastError();
 }
 
