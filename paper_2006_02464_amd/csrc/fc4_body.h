@@ -1,0 +1,638 @@
+// Fully connected layer over 4-bit weights with group scales:
+//   y[m][n] = bias[n] + sum_k x[m][k] * (q[n][k] - z[n][k / group]) * s[n][k / group]
+#pragma once
+#include "conv_common.h"
+
+namespace cw {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(1)));     // a 16-byte load from any address (global memory takes them)
+
+constexpr int kBlock = 128;   // inputs that a wave takes at a time: 16 bytes of weights a lane, four lanes a row
+
+// How x becomes fp16 operands: as it is; bf16 and fp32 scaled by a power of two to each row's and block's largest value,
+// fp32 in two parts.
+enum XForm { X_F16, X_BF16, X_F32 };
+constexpr int kShortIn = 32;   // rows of fewer inputs have fewer bytes than a load: a kernel of their own
+
+struct Fc4Kernel {
+    Fc4Args a;
+    FastDiv group_div;   // of an input's number by `group`
+    FastDiv lots_div;    // by a row's groups in sixteens
+};
+
+__device__ static inline void fc4_store(void *p, int64_t i, DType t, float v) {
+    if (t == DT_F32) static_cast<float *>(p)[i] = v;
+    else if (t == DT_F16) static_cast<f16 *>(p)[i] = (f16)v;
+    else static_cast<bf16 *>(p)[i] = (bf16)v;
+}
+
+// v[0..N) as one number, shifted down by `bits` (a multiple of 8, less than 32 N; of 32 N and more: zero).
+template <int N>
+__device__ static inline void fc4_shift_down(u32x4 (&v)[N / 4], unsigned bits) {
+    auto at = [&](int i) -> unsigned { return i < N ? v[i / 4][i % 4] : 0u; };
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i / 4][i % 4] = __builtin_amdgcn_alignbit(at(i + 1), at(i), bits & 31);
+#pragma unroll
+    for (int s = 1; s < N; s *= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i / 4][i % 4] = bits & (32 * s) ? at(i + s) : at(i);
+    if (bits >= 32 * N)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i / 4][i % 4] = 0;
+}
+
+// What a lane reads of the weights: 32 nibbles a block of each of NT rows.  No load stands in a branch: the wait for earlier loads behind it would be for all
+// of them.
+template <int NT>
+struct Fc4Weights {
+    u32x4 w[NT];
+    // The sixteen bytes of a lane, or where the row ends among them or before, its last sixteen (see shift).
+    __device__ void load(const Fc4Kernel &f, const uint8_t *const (&q)[NT], int block, int kq) {
+        const int at = block * (kBlock / 2) + kq * 16, last = ((f.a.cin + 1) >> 1) - 16, from = at < last ? at : last;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) w[i] = *reinterpret_cast<const u32x4_any *>(q[i] + from);
+    }
+    // The last block, where it is not whole: bytes to their places (what then stands behind the row is multiplied by zeros).
+    __device__ void shift(const Fc4Kernel &f, int block, int kq) {
+        const int at = block * (kBlock / 2) + kq * 16, last = ((f.a.cin + 1) >> 1) - 16;
+        const unsigned bits = at > last ? (unsigned)(at - last) * 8 : 0;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            u32x4 v[1] = {w[i]};
+            fc4_shift_down<4>(v, bits);
+            w[i] = v[0];
+        }
+    }
+};
+template <int NT>
+__device__ static inline void fc4_rows(const uint8_t *(&q)[NT], const Fc4Args &a, int n0, int c) {   // rows behind the last: the last
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        const int n = n0 + i * 16 + c < a.cout ? n0 + i * 16 + c : a.cout - 1;
+        q[i] = a.q + n * a.q_stride;
+    }
+}
+
+// Scales and zero points in LDS, as fp32 [tile][group][ROWS] and bytes [tile][group][ROWS], of groups j0 .. j0 + groups of `count` tiles of ROWS weight rows,
+// every wgs-th from `tile` on: read from memory by the lanes that need them, a scale of each of sixteen rows would bring a line of each of them from the XCD's
+// L2 to the CU for every use.
+template <int ROWS, int THREADS, bool Z>
+__device__ static inline void fc4_scales(const Fc4Kernel &f, int tile, int wgs, int count, int j0, int groups, float *scale, uint8_t *zero, int t) {
+    const Fc4Args &a = f.a;
+    constexpr int U = 4;   // loads of a thread under way
+    const int lots = (groups + 15) / 16, total = count * lots * (16 * ROWS);   // sixteen groups of each row
+    struct Place { int tile, row, j; };
+    auto place = [&](int i) {
+        i = i < total ? i : total - 1;
+        const int lot = i / (16 * ROWS), mine = count == 1 ? 0 : (int)fast_div(lot, f.lots_div);
+        return Place{mine, i / 16 % ROWS, (lot - mine * lots) * 16 + i % 16};
+    };
+    auto take = [&](auto *p) {
+        typedef typename std::remove_const<typename std::remove_pointer<decltype(p)>::type>::type S;
+        for (int base = 0; base < total; base += U * THREADS) {
+            S v[U];
+            uint8_t z[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (base + u * THREADS >= total) break;
+                const Place to = place(base + u * THREADS + t);
+                const int at = (tile + to.tile * wgs) * ROWS + to.row, n = at < a.cout ? at : a.cout - 1, j = j0 + (to.j < groups ? to.j : groups - 1);
+                v[u] = p[n * a.scale_stride + j];
+                if (Z) z[u] = a.zeros[n * a.zero_stride + j];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = base + u * THREADS + t;
+                const Place at = place(i);
+                if (i >= total) break;
+                if (at.j >= groups) continue;
+                const int to = (at.tile * groups + at.j) * ROWS + at.row;
+                scale[to] = (float)v[u];
+                if (Z) zero[to] = z[u];
+            }
+        }
+    };
+    if (a.scale_dtype == DT_F32) take(static_cast<const float *>(a.scales));
+    else if (a.scale_dtype == DT_F16) take(static_cast<const f16 *>(a.scales));
+    else take(static_cast<const bf16 *>(a.scales));
+}
+
+// A lane has 32 inputs of its row, 8 a word; a matrix step takes 8 inputs of each of the four lanes of a row.  Word j of lane group kq becomes word kq of
+// lane group j: step j then has inputs 32 j + 8 kq + 0..7, and all of a step are of one group.
+__device__ static inline void fc4_turn(u32x4 &v) {
+    auto r = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+    v[0] = r[0]; v[2] = r[1];
+    r = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+    v[1] = r[0]; v[3] = r[1];
+    r = __builtin_amdgcn_permlane16_swap(v[0], v[1], false, false);
+    v[0] = r[0]; v[1] = r[1];
+    r = __builtin_amdgcn_permlane16_swap(v[2], v[3], false, false);
+    v[2] = r[0]; v[3] = r[1];
+}
+
+// The eight weights of a word, less their zero point, in the order (0 4) (1 5) (2 6) (3 7).  Nibbles as the low bits of fp16 numbers of exponent 10 are
+// 1024 + q and 1024 + 16 q, from which q - z follows exactly.
+template <bool Z>
+__device__ static inline f16x8 fc4_operand(unsigned v, unsigned z, unsigned magic) {
+    unsigned zlo = 0xE408E408u, zhi = 0xD480D480u;   // -(1024 + 8), -(64 + 8)
+    if (Z) {
+        const unsigned zz = (z & 15) * 0x10001u;
+        zlo = 0xE400E400u | zz;
+        zhi = 0xD400D400u | (zz << 4);
+    }
+    const unsigned v8 = v >> 8;
+    const f16x2 sixteenth = {(f16)0.0625f, (f16)0.0625f}, clo = __builtin_bit_cast(f16x2, zlo), chi = __builtin_bit_cast(f16x2, zhi);
+    const f16x2 w0 = __builtin_bit_cast(f16x2, (v & 0x000F000Fu) | magic) + clo;
+    const f16x2 w1 = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (v & 0x00F000F0u) | magic), sixteenth, chi);
+    const f16x2 w2 = __builtin_bit_cast(f16x2, (v8 & 0x000F000Fu) | magic) + clo;
+    const f16x2 w3 = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (v8 & 0x00F000F0u) | magic), sixteenth, chi);
+    return f16x8{w0[0], w0[1], w1[0], w1[1], w2[0], w2[1], w3[0], w3[1]};
+}
+
+// Eight activations as they are stored, from input k on (zeros behind cin).
+template <int X>
+struct Fc4X {
+    static constexpr int WORDS = X == X_F32 ? 2 : 1;
+    u32x4 raw[WORDS];
+    static constexpr int SIZE = X == X_F32 ? 4 : 2;
+    // From input k on, or where the row ends among them or before, its last eight (see shift).
+    __device__ void load(const void *row, int k, int cin) {
+        const u32x4_any *p = reinterpret_cast<const u32x4_any *>(static_cast<const char *>(row) + (int64_t)(k + 8 <= cin ? k : cin - 8) * SIZE);
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) raw[i] = p[i];
+    }
+    __device__ void shift(int k, int cin) { fc4_shift_down<4 * WORDS>(raw, k + 8 <= cin ? 0u : (unsigned)(k + 8 - cin) * (8 * SIZE)); }
+    __device__ float value(int i) const {
+        const unsigned word = raw[i / 4 % WORDS][i % 4];   // a bit_cast of a vector's element itself takes the first one
+        if (X == X_F32) return __builtin_bit_cast(float, word);
+        return __builtin_bit_cast(float, i % 2 ? raw[0][i / 2] & 0xffff0000u : raw[0][i / 2] << 16);   // bf16
+    }
+    // The largest magnitude, as the bits of its exponent and below (of a NaN: larger than any number's).
+    __device__ unsigned most() const {
+        if (X == X_F32) {
+            unsigned m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const unsigned v = raw[i / 4 % WORDS][i % 4] & 0x7fffffffu;
+                m = m > v ? m : v;
+            }
+            return m;
+        }
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 m = __builtin_bit_cast(u16x2, raw[0][0] & 0x7fff7fffu);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, raw[0][i] & 0x7fff7fffu));
+        return (unsigned)(m[0] > m[1] ? m[0] : m[1]) << 16;
+    }
+    // In the order in which the weights come, times `by`: the rounded value and, of fp32, what the rounding left.
+    __device__ void operands(float by, f16x8 &hi, f16x8 &lo) const {
+        if (X == X_F16) {
+            const u32x4 v = raw[0];
+            const u32x4 o = {__builtin_amdgcn_perm(v[2], v[0], 0x05040100u), __builtin_amdgcn_perm(v[2], v[0], 0x07060302u),
+                             __builtin_amdgcn_perm(v[3], v[1], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u)};
+            hi = __builtin_bit_cast(f16x8, o);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float v0 = value(i) * by, v1 = value(i + 4) * by;
+            if (X == X_BF16) {   // eight bits fit: only what is below 2^-24 of the scaled range is cut off
+                const auto p = __builtin_amdgcn_cvt_pkrtz(v0, v1);
+                hi[2 * i] = (f16)p[0];
+                hi[2 * i + 1] = (f16)p[1];
+            } else {
+                hi[2 * i] = (f16)v0;
+                hi[2 * i + 1] = (f16)v1;
+                lo[2 * i] = (f16)fmaf((float)hi[2 * i], -1.f, v0);
+                lo[2 * i + 1] = (f16)fmaf((float)hi[2 * i + 1], -1.f, v1);
+            }
+        }
+    }
+};
+// 2^(14 - e) for a largest magnitude of 2^e..2^(e+1): its numbers stay below 2^15; and 2^(e - 14).  Neither leaves fp32's range.
+__device__ static inline void fc4_power(unsigned most, float &by, float &back) {
+    int e = (int)(most >> 23) - 127;
+    e = e > 127 ? 127 : e < -112 ? -112 : e;
+    by = __builtin_bit_cast(float, (unsigned)(14 - e + 127) << 23);
+    back = __builtin_bit_cast(float, (unsigned)(e - 14 + 127) << 23);
+}
+
+// The largest of 16 lanes' numbers.
+__device__ static inline unsigned fc4_max_row(unsigned v) {
+    auto join = [&](int o) { v = v > (unsigned)o ? v : (unsigned)o; };
+    join(__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, false));    // lanes 1 0 3 2
+    join(__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, false));    // lanes 2 3 0 1
+    join(__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, false));   // mirrored in 8
+    join(__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, false));   // mirrored in 16
+    return v;
+}
+
+// ---- few rows: up to 16 of x, which LDS holds -----------------------------------------------------------
+// x lies in LDS as fp16 operands, [part][block][row][128], made once a workgroup, and so do the scales of all its weight rows.  The workgroup walks tiles
+// of 16 NT NW weight rows; its KW groups of waves take the blocks of K in turn and D blocks a wave are under way all the time, also from one tile to the next.
+template <int X, int NT, int NW, int KW, int GM, int D, bool Z>
+__global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f, int tiles, int wgs, int groups, int own) {   // own: tiles of a workgroup at most
+    constexpr int THREADS = 64 * NW * KW, PARTS = X == X_F32 ? 2 : 1, MEET = NW * KW * NT * 256, ROWS = 16 * NT * NW;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const Fc4Args &a = f.a;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), nw = wave % NW, kw = wave / NW;
+    const int c = lane & 15, kq = lane >> 4;
+    const int rows = a.rows, blocks = (a.cin + kBlock - 1) / kBlock, part_bytes = blocks * rows * (kBlock * 2);
+    float *meet = reinterpret_cast<float *>(lds + PARTS * part_bytes), *xs = meet + 2 * MEET;           // xs: [block][16], what x was divided by
+    float *scales = xs + (X == X_F16 ? 0 : blocks * 16);                                                   // [tile][group][ROWS]
+    uint8_t *zeros = reinterpret_cast<uint8_t *>(scales + own * groups * ROWS);
+    const int mine = (blocks - kw + KW - 1) / KW;   // blocks of a tile: kw, kw + KW, ...
+    const int todo_tiles = (tiles - (int)blockIdx.x + wgs - 1) / wgs, todo = todo_tiles * mine;
+
+    // The next block to ask for.
+    const uint8_t *q[NT];
+    Fc4Weights<NT> w[D];
+    int at_tile = blockIdx.x, at = kw;
+    fc4_rows<NT>(q, a, (at_tile * NW + nw) * (16 * NT), c);
+    auto ask = [&](Fc4Weights<NT> &to) {
+        to.load(f, q, at, kq);
+        at += KW;
+        if (at >= blocks) {   // behind the last tile: its last block again
+            const bool more = at_tile + wgs < tiles;
+            at = more ? kw : at - KW;
+            if (more) {
+                at_tile += wgs;
+                fc4_rows<NT>(q, a, (at_tile * NW + nw) * (16 * NT), c);
+            }
+        }
+    };
+    if (todo > 0)
+#pragma unroll
+        for (int u = 0; u < D; ++u) ask(w[u]);
+
+    constexpr int U = 4;   // pieces of eight inputs a thread has under way; sixteen threads a row and block
+    const int piece = t & 15;
+    for (int base = 0; base < rows * blocks * 16; base += U * THREADS) {
+        Fc4X<X> x[U];
+        int row[U], block[U];
+        const int item = base + t;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (base + u * THREADS >= rows * blocks * 16) break;
+            const int at = (item + u * THREADS) >> 4, rb = at < rows * blocks ? at : rows * blocks - 1;
+            block[u] = rows == 1 ? rb : rb / rows;
+            row[u] = rb - block[u] * rows;
+            x[u].load(static_cast<const char *>(a.x) + row[u] * a.x_stride * (X == X_F32 ? 4 : 2), block[u] * kBlock + piece * 8, a.cin);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (item + u * THREADS >= rows * blocks * 16) break;
+            const int k = block[u] * kBlock + piece * 8;
+            if (k + 8 > a.cin) x[u].shift(k, a.cin);
+            float by = 1.f, back;
+            if (X != X_F16) {
+                fc4_power(fc4_max_row(x[u].most()), by, back);
+                if (piece == 0) xs[block[u] * 16 + row[u]] = back;
+            }
+            f16x8 hi, lo;
+            x[u].operands(by, hi, lo);
+            char *to = lds + (block[u] * rows + row[u]) * (kBlock * 2) + ((piece ^ row[u]) << 4);
+            *reinterpret_cast<f16x8 *>(to) = hi;
+            if (X == X_F32) *reinterpret_cast<f16x8 *>(to + part_bytes) = lo;
+        }
+    }
+    fc4_scales<ROWS, THREADS, Z>(f, blockIdx.x, wgs, todo_tiles, 0, groups, scales, zeros, t);
+    __syncthreads();
+
+    // A row's sixteen pieces of a block change places with the row's number: every sixteen lanes write, and read, 256 different bytes of the 256 that LDS serves at a time.
+    const int xrow = c < rows ? c : rows - 1;
+    int xat[4];
+#pragma unroll
+    for (int step = 0; step < 4; ++step) xat[step] = xrow * (kBlock * 2) + (((step * 4 + kq) ^ xrow) << 4);
+    unsigned magic = 0x64006400u;
+    asm("" : "+v"(magic));   // in a register
+    f32x4 total[NT] = {};
+    int tile = blockIdx.x, side = 0, block = kw, slot = nw * (16 * NT) + c;   // slot: this lane's first row among the scales
+    auto work = [&](Fc4Weights<NT> &v) {
+        const f32x4 back = X != X_F16 ? *reinterpret_cast<const f32x4 *>(xs + block * 16 + kq * 4) : f32x4{};
+        if ((block + 1) * kBlock > a.cin) v.shift(f, block, kq);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fc4_turn(v.w[j]);
+        f32x4 p[NT];
+        int at[4 / GM];
+#pragma unroll
+        for (int g = 0; g < 4 / GM; ++g) {
+            const int k = block * kBlock + g * GM * 32;
+            at[g] = slot + (int)fast_div(k < a.cin ? k : a.cin - 1, f.group_div) * ROWS;
+        }
+#pragma unroll
+        for (int step = 0; step < 4; ++step) {
+            f16x8 x[PARTS];
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) x[part] = *reinterpret_cast<const f16x8 *>(lds + part * part_bytes + block * rows * (kBlock * 2) + xat[step]);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const f16x8 ww = fc4_operand<Z>(v.w[j][step], Z ? zeros[at[step / GM] + j * 16] : 0u, magic);
+                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                p[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[0], ww, step % GM == 0 ? zero : p[j], 0, 0, 0);
+                if (X == X_F32) p[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[PARTS - 1], ww, p[j], 0, 0, 0);
+                if (step % GM == GM - 1) {
+                    const float scale = scales[at[step / GM] + j * 16];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) total[j][e] = X == X_F16 ? fmaf(p[j][e], scale, total[j][e]) : fmaf(p[j][e] * scale, back[e], total[j][e]);
+                }
+            }
+        }
+        block += KW;
+    };
+    // The end of a tile: the sums of the groups of waves in LDS, [kw][nw][tile][4][64], on the two sides in turn.
+    auto finish = [&]() {
+        float *part = meet + side * MEET;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                part[((wave * NT + j) * 4 + e) * 64 + lane] = total[j][e];
+                total[j][e] = 0.f;
+            }
+        __syncthreads();
+        for (int o = t; o < NW * NT * 256; o += THREADS) {   // o = (tile of 16, e, lane)
+            const int l = o & 63, m = (l >> 4) * 4 + ((o >> 6) & 3), n = tile * ROWS + (o >> 8) * 16 + (l & 15);
+            if (m >= rows || n >= a.cout) continue;
+            float v = 0.f;
+#pragma unroll
+            for (int k = 0; k < KW; ++k) v += part[k * (NW * NT * 256) + o];
+            fc4_store(a.y, m * a.y_stride + n, a.y_dtype, v + (a.bias ? a.bias[n] : 0.f));
+        }
+        tile += wgs;
+        side ^= 1;
+        block = kw;
+        slot += groups * ROWS;
+    };
+    if (todo == 0) {   // fewer blocks than groups of waves
+        while (tile < tiles) finish();
+        return;
+    }
+    int done = 0;
+    for (; done + D < todo; done += D)
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+            work(w[u]);
+            ask(w[u]);
+            if (block >= blocks) finish();
+        }
+#pragma unroll
+    for (int u = 0; u < D; ++u)
+        if (done + u < todo) {
+            work(w[u]);
+            if (block >= blocks) finish();
+        }
+}
+
+// ---- many rows --------------------------------------------------------------------------------------
+// A workgroup computes 16 MT rows by 16 NT NW weight rows; its KW groups of waves take the blocks of K in turn.  The NW waves of a group stage the group's
+// block of x in one of two LDS buffers while they multiply the other one, from registers that were loaded two blocks ahead; weights go straight to the
+// registers of the wave that multiplies them, three blocks ahead.
+template <int X, int MT, int NT, int NW, int KW>
+struct Fc4Many {
+    static constexpr int ROWS = 16 * MT, COLS = 16 * NT * NW, THREADS = 64 * NW * KW, PARTS = X == X_F32 ? 2 : 1, ITEMS = ROWS / 4 / NW;   // ITEMS of a wave: four rows of a block each
+    static constexpr int PART = 4 * ROWS * 64, BUFFER = PARTS * PART + (X == X_F16 ? 0 : ROWS * 4);   // bytes of a block
+    static constexpr int STAGED = KW * 2 * BUFFER, MEET = NW * KW * MT * NT * 1024;
+};
+
+template <int X, int MT, int NT, int NW, int KW, int GM, bool Z>
+__global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel f, int chunk, int chunk_groups) {   // chunk: phases whose scales LDS holds, in chunk_groups groups
+    typedef Fc4Many<X, MT, NT, NW, KW> S;
+    constexpr int ROWS = S::ROWS, COLS = S::COLS, PARTS = S::PARTS, ITEMS = S::ITEMS, PART = S::PART, BUFFER = S::BUFFER;
+    static_assert(ROWS / 4 % NW == 0, "rows in fours, evenly");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const Fc4Args &a = f.a;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), nw = wave % NW, kw = wave / NW;
+    const int c = lane & 15, kq = lane >> 4;
+    const int m0 = blockIdx.y * ROWS, rows = a.rows - m0 < ROWS ? a.rows - m0 : ROWS;
+    const uint8_t *q[NT];
+    fc4_rows<NT>(q, a, (blockIdx.x * NW + nw) * (16 * NT), c);
+    const int blocks = (a.cin + kBlock - 1) / kBlock, phases = (blocks + KW - 1) / KW;
+    char *const mine = lds + kw * (2 * BUFFER);
+    float *scales = reinterpret_cast<float *>(lds + S::STAGED);
+    uint8_t *zeros = reinterpret_cast<uint8_t *>(scales + chunk_groups * COLS);
+    f32x4 total[MT][NT] = {};
+    unsigned magic = 0x64006400u;
+    asm("" : "+v"(magic));   // in a register
+
+    // Staging: sixteen lanes a row, whose sixteen pieces of a block change places with the row's number (modulo 16): every sixteen lanes write, and read, 256
+    // different bytes of the 256 that LDS serves at a time.
+    Fc4X<X> x[2][ITEMS];
+    const int piece = lane & 15;
+    const char *xrow[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int row = (nw * ITEMS + i) * 4 + (lane >> 4);
+        xrow[i] = static_cast<const char *>(a.x) + (m0 + (row < rows ? row : rows - 1)) * a.x_stride * (X == X_F32 ? 4 : 2);
+    }
+    auto block_of = [&](int phase) {   // behind the last block: that one again
+        const int block = phase * KW + kw;
+        return block < blocks ? block : blocks - 1;
+    };
+    auto ask_x = [&](int phase, Fc4X<X> (&to)[ITEMS]) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) to[i].load(xrow[i], block_of(phase) * kBlock + piece * 8, a.cin);
+    };
+    auto stage = [&](int phase, Fc4X<X> (&v)[ITEMS], char *to) {
+        const int block = block_of(phase);
+        if ((block + 1) * kBlock > a.cin)
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) v[i].shift(block * kBlock + piece * 8, a.cin);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int row = (nw * ITEMS + i) * 4 + (lane >> 4);
+            float by = 1.f, back;
+            if (X != X_F16) {
+                fc4_power(fc4_max_row(v[i].most()), by, back);
+                if (piece == 0) reinterpret_cast<float *>(to + PARTS * PART)[row] = back;
+            }
+            f16x8 hi, lo;
+            v[i].operands(by, hi, lo);
+            char *at = to + row * (kBlock * 2) + (((piece ^ row) & 15) << 4);
+            *reinterpret_cast<f16x8 *>(at) = hi;
+            if (X == X_F32) *reinterpret_cast<f16x8 *>(at + PART) = lo;
+        }
+    };
+    Fc4Weights<NT> w[4];
+    const int slot = nw * (16 * NT) + c;
+    int xat[4];
+#pragma unroll
+    for (int step = 0; step < 4; ++step) xat[step] = c * (kBlock * 2) + (((step * 4 + kq) ^ c) << 4);
+    int j0 = 0;   // first group of the chunk
+    auto multiply = [&](Fc4Weights<NT> &v, int block, const char *from) {
+        if ((block + 1) * kBlock > a.cin) v.shift(f, block, kq);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fc4_turn(v.w[j]);
+        f32x4 p[MT][NT];
+        int at[4 / GM];
+#pragma unroll
+        for (int g = 0; g < 4 / GM; ++g) {
+            const int k = block * kBlock + g * GM * 32;
+            at[g] = slot + ((int)fast_div(k < a.cin ? k : a.cin - 1, f.group_div) - j0) * COLS;
+        }
+#pragma unroll
+        for (int step = 0; step < 4; ++step) {
+            f16x8 xx[PARTS][MT];
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    xx[part][i] = *reinterpret_cast<const f16x8 *>(from + part * PART + i * (16 * kBlock * 2) + xat[step]);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const f16x8 ww = fc4_operand<Z>(v.w[j][step], Z ? zeros[at[step / GM] + j * 16] : 0u, magic);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                    p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xx[0][i], ww, step % GM == 0 ? zero : p[i][j], 0, 0, 0);
+                    if (X == X_F32) p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xx[PARTS - 1][i], ww, p[i][j], 0, 0, 0);
+                }
+            }
+            if (step % GM == GM - 1) {
+                float scale[NT];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) scale[j] = scales[at[step / GM] + j * 16];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const f32x4 back = X != X_F16 ? *reinterpret_cast<const f32x4 *>(from + PARTS * PART + (i * 16 + kq * 4) * 4) : f32x4{};
+#pragma unroll
+                    for (int j = 0; j < NT; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            total[i][j][e] = X == X_F16 ? fmaf(p[i][j][e], scale[j], total[i][j][e]) : fmaf(p[i][j][e] * scale[j], back[e], total[i][j][e]);
+                }
+            }
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < 3; ++u) w[u].load(f, q, block_of(u), kq);
+    ask_x(0, x[0]);
+    ask_x(1, x[1]);
+    stage(0, x[0], mine);
+    for (int phase = 0; phase < phases; phase += 4) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (phase + u >= phases) break;
+            if ((phase + u) % chunk == 0) {   // the scales of the next phases
+                const int k0 = (phase + u) * KW * kBlock, k1 = k0 + chunk * KW * kBlock;
+                j0 = (int)fast_div(k0, f.group_div);
+                if (phase + u > 0) __syncthreads();
+                fc4_scales<COLS, S::THREADS, Z>(f, blockIdx.x, 1, 1, j0, (int)fast_div((k1 < a.cin ? k1 : a.cin) - 1, f.group_div) - j0 + 1, scales, zeros, t);
+            }
+            ask_x(phase + u + 2, x[u & 1]);
+            w[(u + 3) & 3].load(f, q, block_of(phase + u + 3), kq);
+            __syncthreads();
+            const int block = (phase + u) * KW + kw;
+            if (block < blocks) multiply(w[u], block, mine + (u & 1) * BUFFER);
+            stage(phase + u + 1, x[(u + 1) & 1], mine + ((u + 1) & 1) * BUFFER);
+        }
+    }
+    // The groups of waves meet in LDS: [kw][nw][tile][4][64]
+    __syncthreads();
+    float *part = reinterpret_cast<float *>(lds);
+    constexpr int TILES = MT * NT;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[(((wave * MT + i) * NT + j) * 4 + e) * 64 + lane] = total[i][j][e];
+    __syncthreads();
+    for (int o = t; o < NW * TILES * 256; o += 64 * NW * KW) {   // o = ((nw, i, j), e, lane)
+        const int l = o & 63, e = (o >> 6) & 3, tile = (o >> 8) % TILES, ow = (o >> 8) / TILES;
+        const int m = (tile / NT) * 16 + (l >> 4) * 4 + e, n = (blockIdx.x * NW + ow) * (16 * NT) + (tile % NT) * 16 + (l & 15);
+        if (m >= rows || n >= a.cout) continue;
+        float v = 0.f;
+#pragma unroll
+        for (int k = 0; k < KW; ++k) v += part[k * (NW * TILES * 256) + o];
+        fc4_store(a.y, (m0 + m) * a.y_stride + n, a.y_dtype, v + (a.bias ? a.bias[n] : 0.f));
+    }
+}
+
+constexpr int kLdsBytes = 160 * 1024, kFewBytes = 80 * 1024;   // kFewBytes: two workgroups of few rows share a CU
+
+static int fc4_groups(const Fc4Args &a) { return (a.cin + a.group - 1) / a.group; }
+static Fc4Kernel fc4_kernel_args(const Fc4Args &a) { return {a, make_fast_div((uint32_t)a.group), make_fast_div((uint32_t)(fc4_groups(a) + 15) / 16)}; }
+
+// LDS of fc4_few_kernel without the scales, and of the scales of a tile.
+template <int X, int NT, int NW, int KW>
+static int64_t few_bytes(const Fc4Args &a) {
+    const int64_t blocks = (a.cin + kBlock - 1) / kBlock;
+    return (X == X_F32 ? 2 : 1) * a.rows * blocks * kBlock * 2 + 2 * NW * KW * NT * 1024 + (X == X_F16 ? 0 : blocks * 64);
+}
+template <int NT, int NW, bool Z>
+static int64_t few_tile_bytes(const Fc4Args &a) { return (int64_t)fc4_groups(a) * (16 * NT * NW) * (Z ? 5 : 4); }
+
+template <int X, int NT, int NW, int KW, int GM, int D, bool Z>
+static hipError_t launch_few(const Fc4Args &a, hipStream_t s, int most_wgs = 512) {
+    const int64_t fixed = few_bytes<X, NT, NW, KW>(a), tile = few_tile_bytes<NT, NW, Z>(a);
+    if (a.rows > 16 || a.cin < kShortIn || fixed + tile > kFewBytes) return hipErrorInvalidValue;
+    const int tiles = (a.cout + 16 * NT * NW - 1) / (16 * NT * NW), fit = (int)((kFewBytes - fixed) / tile);
+    int own = (tiles + most_wgs - 1) / most_wgs;
+    own = own < fit ? own : fit;
+    const int wgs = (tiles + own - 1) / own;
+    fc4_few_kernel<X, NT, NW, KW, GM, D, Z><<<dim3(wgs), 64 * NW * KW, (size_t)(fixed + own * tile), s>>>(fc4_kernel_args(a), tiles, wgs, fc4_groups(a), own);
+    return hipGetLastError();
+}
+
+template <int X, int MT, int NT, int NW, int KW, int GM, bool Z>
+static hipError_t launch_many(const Fc4Args &a, hipStream_t s) {
+    typedef Fc4Many<X, MT, NT, NW, KW> S;
+    static_assert(S::MEET <= kLdsBytes && S::STAGED + (KW * 4 / GM + 1) * S::COLS * 5 <= kLdsBytes, "LDS");
+    if (a.cin < kShortIn) return hipErrorInvalidValue;
+    // The scales of as many phases as fit.  Inputs that begin anywhere touch a group more than they fill.
+    const int phases = (a.cin + KW * kBlock - 1) / (KW * kBlock), most = (kLdsBytes - S::STAGED) / (S::COLS * (Z ? 5 : 4));
+    int chunk = phases, groups = fc4_groups(a);
+    while (groups > most && chunk > 1) {
+        chunk = (chunk + 1) / 2;
+        groups = (int)(((int64_t)chunk * KW * kBlock + a.group - 1) / a.group) + 1;
+    }
+    if (groups > most) return hipErrorInvalidValue;
+    const int bytes = S::STAGED + groups * S::COLS * (Z ? 5 : 4);
+    for (int m = 0; m < a.rows; m += 65535 * S::ROWS) {   // rows beyond the grid's y
+        Fc4Kernel f = fc4_kernel_args(a);
+        f.a.rows = a.rows - m < 65535 * S::ROWS ? a.rows - m : 65535 * S::ROWS;
+        f.a.x = static_cast<const char *>(a.x) + m * a.x_stride * (a.x_dtype == DT_F32 ? 4 : 2);
+        f.a.y = static_cast<char *>(a.y) + m * a.y_stride * (a.y_dtype == DT_F32 ? 4 : 2);
+        fc4_many_kernel<X, MT, NT, NW, KW, GM, Z><<<dim3((a.cout + S::COLS - 1) / S::COLS, (f.a.rows + S::ROWS - 1) / S::ROWS), S::THREADS, bytes > S::MEET ? bytes : S::MEET, s>>>(f, chunk, groups);
+    }
+    return hipGetLastError();
+}
+
+// ---- the choice of a form ----------------------------------------------------------------------------
+struct Fc4Plan {
+    enum Form { SHORT, FEW, FEW_PAIRS, MANY1, MANY2_32, MANY2_64, MANY2_128, MANY4_32, MANY4_64, MANY4_128 } form;
+    int rows, cols, threads;   // of a workgroup; FEW and FEW_PAIRS: `cols` at a time
+};
+Fc4Plan fc4_plan(const Fc4Args &a);
+template <int X>
+hipError_t launch_fc4_x(const Fc4Args &a, const Fc4Plan &p, hipStream_t s);
+
+template <int X, int GM, bool Z>
+static hipError_t launch_fc4_form(const Fc4Args &a, const Fc4Plan &p, hipStream_t s) {
+    constexpr bool two = X == X_F32;   // operands in two parts: twice the LDS
+    switch (p.form) {
+        case Fc4Plan::FEW: return launch_few<X, 1, 1, 8, GM, 2, Z>(a, s);
+        case Fc4Plan::FEW_PAIRS: return launch_few<X, 1, 2, 4, GM, 4, Z>(a, s, 1024);
+        case Fc4Plan::MANY1: return launch_many<X, 1, 1, 1, 8, GM, Z>(a, s);
+        case Fc4Plan::MANY2_32: return launch_many<X, 2, 1, 2, 4, GM, Z>(a, s);
+        case Fc4Plan::MANY2_64: return launch_many<X, 2, 1, 4, two ? 2 : 4, GM, Z>(a, s);
+        case Fc4Plan::MANY2_128: return launch_many<X, 2, 1, 8, 2, GM, Z>(a, s);
+        case Fc4Plan::MANY4_32: return launch_many<X, 4, 1, 2, two ? 2 : 4, GM, Z>(a, s);
+        case Fc4Plan::MANY4_64: return launch_many<X, 4, 2, 2, two ? 2 : 4, GM, Z>(a, s);
+        case Fc4Plan::MANY4_128: return launch_many<X, 4, 1, 8, 2, GM, Z>(a, s);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+template <int X>
+hipError_t launch_fc4_x(const Fc4Args &a, const Fc4Plan &p, hipStream_t s) {
+    if (a.group % 128 == 0) return a.zeros ? launch_fc4_form<X, 4, true>(a, p, s) : launch_fc4_form<X, 4, false>(a, p, s);
+    if (a.group % 64 == 0) return a.zeros ? launch_fc4_form<X, 2, true>(a, p, s) : launch_fc4_form<X, 2, false>(a, p, s);
+    return a.zeros ? launch_fc4_form<X, 1, true>(a, p, s) : launch_fc4_form<X, 1, false>(a, p, s);
+}
+
+}  // namespace cw
