@@ -56,6 +56,14 @@ __device__ static inline Soft join(const Soft &a, const Soft &b, float c2) {
     return {m, a.s * ea + b.s * eb, (a.t + a.s * da) * ea + (b.t + b.s * db) * eb};
 }
 
+// Of all 64 lanes.
+__device__ static inline Soft meet(const Soft &v, float c2) {
+    const auto plus = [](float p, float q) { return p + q; };
+    const float m = wave_all(v.m, [](float p, float q) { return fmaxf(p, q); }), ref = m == -INFINITY ? 0.f : m;
+    const float d = fmaxf((v.m - ref) * c2, -1e30f), e = __builtin_amdgcn_exp2f(d);
+    return {m, wave_all(v.s * e, plus), wave_all((v.t + v.s * d) * e, plus)};
+}
+
 struct AnswerLds {
     uint64_t list[kList], best[kAnswerMostTop];
     unsigned order[kThreads];
@@ -90,9 +98,9 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
     const int segments = (a.classes + kSegment - 1) / kSegment;
     const int seg0 = (int)((int64_t)segments * part / parts), seg1 = (int)((int64_t)segments * (part + 1) / parts);
     const float c2 = a.scale * 1.44269504f;
-    const int g = a.given ? a.given[row] : -1;
-    const bool inside = g >= 0 && g < a.classes;
-    const float xg = inside ? (float)x[g] : INFINITY;
+    int g = -1;
+    bool inside = false;
+    float xg = INFINITY;
 
     Soft soft{-INFINITY, 0.f, 0.f};
     int before = 0;       // logits that come before the given one
@@ -114,9 +122,18 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
                 for (int e = 0; e < N; ++e) v[j * N + e] = at + e < count ? (float)x[base + at + e] : -INFINITY;
             }
         }
+        if (seg == seg0 && a.given) {   // behind the first logits' loads: these two wait for one another
+            g = a.given[row];
+            inside = g >= 0 && g < a.classes;
+            if (inside) xg = (float)x[g];
+        }
         float most = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) most = fmaxf(most, v[i]);
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (j * CHUNK >= count) break;
+#pragma unroll
+            for (int e = 0; e < N; ++e) most = fmaxf(most, v[j * N + e]);
+        }
         {
             const float m = fmaxf(soft.m, most), ref = m == -INFINITY ? 0.f : m;
             const float d0 = fmaxf((soft.m - ref) * c2, -1e30f), e0 = __builtin_amdgcn_exp2f(d0);
@@ -137,6 +154,7 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
         if (inside) {
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j) {
+                if (j * CHUNK >= count) break;
                 const int from = base + j * CHUNK + t * N;
                 if (from + N <= g) {
 #pragma unroll
@@ -155,7 +173,11 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
             // What is above the bar, if it is not too much.
             int above = 0;
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) above += v[i] > bar;
+            for (int j = 0; j < CHUNKS; ++j) {
+                if (j * CHUNK >= count) break;
+#pragma unroll
+                for (int e = 0; e < N; ++e) above += v[j * N + e] > bar;
+            }
             l.order[t] = order_of(most);
             if (t == 0) l.n = have;
             above = wave_all(above, [](int p, int q) { return p + q; });
@@ -184,12 +206,16 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
             auto put = [&](float value, int i) { l.list[atomicAdd(&l.n, 1)] = key_of(value, base + i); };
             if (most >= from) {
 #pragma unroll
-                for (int i = 0; i < kEach; ++i)
-                    if (v[i] > from) put(v[i], (i / N) * CHUNK + t * N + i % N);
+                for (int j = 0; j < CHUNKS; ++j) {
+                    if (j * CHUNK >= count) break;
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (v[j * N + e] > from) put(v[j * N + e], j * CHUNK + t * N + e);
+                }
             }
             if (equal) {
                 // At least k logits are as large as `from`: of those equal to it the first ones are needed, chunk by chunk.
-                for (int j = 0; j < CHUNKS; ++j) {
+                for (int j = 0; j * CHUNK < count; ++j) {
                     __syncthreads();
                     const int n = l.n;
                     if (n - have >= k) break;
@@ -206,17 +232,10 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
     }
 
     // The threads meet.
-    const float m = wave_all(soft.m, [](float p, float q) { return fmaxf(p, q); });
-    {
-        const float ref = m == -INFINITY ? 0.f : m, d = fmaxf((soft.m - ref) * c2, -1e30f), e = __builtin_amdgcn_exp2f(d);
-        soft.t = (soft.t + soft.s * d) * e;
-        soft.s *= e;
-    }
     const auto plus = [](auto p, auto q) { return p + q; };
-    soft.s = wave_all(soft.s, plus);
-    soft.t = wave_all(soft.t, plus);
+    soft = meet(soft, c2);
     before = wave_all(before, plus);
-    if (lane == 0) { l.m[wave] = m; l.s[wave] = soft.s; l.t[wave] = soft.t; l.rank[wave] = before; }
+    if (lane == 0) { l.m[wave] = soft.m; l.s[wave] = soft.s; l.t[wave] = soft.t; l.rank[wave] = before; }
     __syncthreads();
     Soft all = join(join({l.m[0], l.s[0], l.t[0]}, {l.m[1], l.s[1], l.t[1]}, c2), join({l.m[2], l.s[2], l.t[2]}, {l.m[3], l.s[3], l.t[3]}, c2), c2);
     before = l.rank[0] + l.rank[1] + l.rank[2] + l.rank[3];
@@ -250,12 +269,12 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
             l.n = 0;
         }
         auto get = [&](int p, int i) { return __hip_atomic_load(reinterpret_cast<int *>(records + p * kRecordBytes) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-        all = {-INFINITY, 0.f, 0.f};
-        before = 0;
-        for (int p = 0; p < parts; ++p) {
-            all = join(all, {__builtin_bit_cast(float, get(p, 0)), __builtin_bit_cast(float, get(p, 1)), __builtin_bit_cast(float, get(p, 2))}, c2);
-            before += get(p, 3);
-        }
+        // A lane a part (kParts <= 64), joined as the threads were.
+        const int p = lane < parts ? lane : 0;
+        Soft one{lane < parts ? __builtin_bit_cast(float, get(p, 0)) : -INFINITY, lane < parts ? __builtin_bit_cast(float, get(p, 1)) : 0.f,
+                 lane < parts ? __builtin_bit_cast(float, get(p, 2)) : 0.f};
+        before = wave_all(lane < parts ? get(p, 3) : 0, plus);
+        all = meet(one, c2);
         __syncthreads();
         if (k > 0) {
             for (int i = t; i < parts * k; i += kThreads) {
