@@ -16,6 +16,8 @@ constexpr int kCounterSlots = 256;                 // rows that can be shared
 // Logits above the k-th largest of the threads' maxima lie with fewer than k threads; those equal to it are taken 2048 at a time.
 constexpr int kList = kAnswerMostTop + (kAnswerMostTop - 1) * kEach + kAnswerMostTop + kThreads * 8;
 
+constexpr int kPad = 8;   // keys that first_of reads at a time
+
 template <typename T>
 struct Vec { static constexpr int N = 16 / sizeof(T); };
 
@@ -65,27 +67,57 @@ __device__ static inline Soft meet(const Soft &v, float c2) {
 }
 
 struct AnswerLds {
-    uint64_t list[kList], best[kAnswerMostTop];
-    unsigned order[kThreads];
+    __attribute__((aligned(16))) uint64_t list[kList + kPad];
+    uint64_t best[kAnswerMostTop];
+    unsigned order[2][kThreads];
     float m[4], s[4], t[4];
     int rank[4];
     int n, last;
 };
 
-// The k first of list[0..n) in order; returns how many there are.  All threads.
+// The k first of list[0..n) in order; returns how many there are.  All threads, behind a barrier behind the last write.
 __device__ static inline int first_of(AnswerLds &l, int n, int k) {
     const int t = threadIdx.x;
+    if (t < kPad) l.list[n + t] = 0;
+    __syncthreads();
     for (int at = t; at < n; at += kThreads) {
         const uint64_t mine = l.list[at];
         int rank = 0;
-        for (int o = 0; o < n; ++o) rank += l.list[o] > mine;
+        for (int o = 0; o < n; o += kPad) {
+            uint64_t other[kPad];
+#pragma unroll
+            for (int i = 0; i < kPad; ++i) other[i] = l.list[o + i];
+#pragma unroll
+            for (int i = 0; i < kPad; ++i) rank += other[i] > mine;
+        }
         if (rank < k) l.best[rank] = mine;
     }
     __syncthreads();
     const int have = n < k ? n : k;
     if (t < have) l.list[t] = l.best[t];
-    __syncthreads();
     return have;
+}
+
+// The largest number (bits from the top on, as many as needed) that at least k of order[0..256) reach; 0 if fewer reach any above `low`.  A wave by itself.
+__device__ static inline unsigned kth_of(const unsigned *order, int k, int lane, unsigned low) {
+    unsigned o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = order[i * 64 + lane];
+    auto reach = [&](unsigned q) {
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c += __popcll(__ballot(o[i] >= q));
+        return c;
+    };
+    if (reach(low + 1) < k) return 0;
+    unsigned tau = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const unsigned q = tau | 1u << bit;
+        const int c = reach(q);
+        if (c >= k) tau = q;
+        if (c == k) break;
+    }
+    return tau;
 }
 
 template <typename T>
@@ -170,41 +202,16 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
             }
         }
         if (k > 0) {
-            // What is above the bar, if it is not too much.
-            int above = 0;
-#pragma unroll
-            for (int j = 0; j < CHUNKS; ++j) {
-                if (j * CHUNK >= count) break;
-#pragma unroll
-                for (int e = 0; e < N; ++e) above += v[j * N + e] > bar;
-            }
-            l.order[t] = order_of(most);
+            // What is above the bar, and of that no more than what reaches the k-th largest of the threads' maxima.
+            unsigned *order = l.order[(seg - seg0) & 1];
+            order[t] = order_of(most);
             if (t == 0) l.n = have;
-            above = wave_all(above, [](int p, int q) { return p + q; });
-            if (lane == 0) l.rank[wave] = above;
             __syncthreads();
-            above = l.rank[0] + l.rank[1] + l.rank[2] + l.rank[3];
-            if (above == 0) { __syncthreads(); continue; }
-            float from = bar;     // candidates are above it ...
-            bool equal = false;   // ... or, with `equal`, those equal to it too, as far as they are needed
-            if (above > 256) {
-                // The k-th largest of the threads' maxima, bit by bit: at least k logits are as large.
-                unsigned o[4], tau = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = l.order[i * 64 + lane];
-                for (int bit = 31; bit >= 0; --bit) {
-                    const unsigned q = tau | 1u << bit;
-                    int c = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) c += __popcll(__ballot(o[i] >= q));
-                    if (c >= k) tau = q;
-                    if (c == k) break;
-                }
-                const float edge = of_order(tau);
-                if (edge > bar) { from = edge; equal = true; }
-            }
+            const unsigned tau = kth_of(order, k, lane, order_of(bar));
+            const bool equal = tau != 0;                       // then those equal to it too, as far as they are needed
+            const float from = equal ? of_order(tau) : bar;
             auto put = [&](float value, int i) { l.list[atomicAdd(&l.n, 1)] = key_of(value, base + i); };
-            if (most >= from) {
+            if (most > from) {
 #pragma unroll
                 for (int j = 0; j < CHUNKS; ++j) {
                     if (j * CHUNK >= count) break;
@@ -213,21 +220,22 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
                         if (v[j * N + e] > from) put(v[j * N + e], j * CHUNK + t * N + e);
                 }
             }
-            if (equal) {
-                // At least k logits are as large as `from`: of those equal to it the first ones are needed, chunk by chunk.
-                for (int j = 0; j * CHUNK < count; ++j) {
-                    __syncthreads();
-                    const int n = l.n;
-                    if (n - have >= k) break;
+            __syncthreads();
+            int n = l.n;
+            if (equal)   // at least k logits are as large as `from`: of those equal to it the first ones are needed, chunk by chunk
+                for (int j = 0; n - have < k && j * CHUNK < count; ++j) {
                     __syncthreads();
 #pragma unroll
                     for (int i = 0; i < kEach; ++i)
                         if (i / N == j && v[i] == from) put(v[i], (i / N) * CHUNK + t * N + i % N);
+                    __syncthreads();
+                    n = l.n;
                 }
+            if (n > have) {
+                have = first_of(l, n, k);
+                __syncthreads();
+                if (have == k) bar = of_order((unsigned)(l.list[k - 1] >> 32));
             }
-            __syncthreads();
-            have = first_of(l, l.n, k);
-            if (have == k) bar = of_order((unsigned)(l.list[k - 1] >> 32));
         }
     }
 
@@ -277,13 +285,28 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
         all = meet(one, c2);
         __syncthreads();
         if (k > 0) {
-            for (int i = t; i < parts * k; i += kThreads) {
-                const int p = i / k, j = i - p * k;
-                const uint64_t key = (uint64_t)(unsigned)get(p, 5 + 2 * j) << 32 | (unsigned)get(p, 4 + 2 * j);
-                if (key) l.list[atomicAdd(&l.n, 1)] = key;
+            constexpr int EACH = kParts * kAnswerMostTop / kThreads;
+            uint64_t key[EACH], most = 0;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                key[i] = 0;
+                const int at = i * kThreads + t;
+                if (at < parts * k) {
+                    const int p = at / k, j = at - p * k;
+                    key[i] = (uint64_t)(unsigned)get(p, 5 + 2 * j) << 32 | (unsigned)get(p, 4 + 2 * j);
+                    most = most > key[i] ? most : key[i];
+                }
             }
+            l.order[0][t] = (unsigned)(most >> 32);
+            __syncthreads();
+            const unsigned tau = kth_of(l.order[0], k, lane, 0);
+            if (most)
+#pragma unroll
+                for (int i = 0; i < EACH; ++i)
+                    if (key[i] && (unsigned)(key[i] >> 32) >= tau) l.list[atomicAdd(&l.n, 1)] = key[i];
             __syncthreads();
             have = first_of(l, l.n, k);
+            __syncthreads();
         }
     }
 
