@@ -16,6 +16,7 @@ constexpr int kCounterSlots = 256;                 // rows that can be shared
 // Logits above the k-th largest of the threads' maxima lie with fewer than k threads; those equal to it are taken 2048 at a time.
 constexpr int kList = kAnswerMostTop + (kAnswerMostTop - 1) * kEach + kAnswerMostTop + kThreads * 8;
 
+constexpr int kFewThreads = (kList - kAnswerMostTop) / kEach;   // whose logits the list holds, all of them
 constexpr int kPad = 8;   // keys that first_of reads at a time
 
 template <typename T>
@@ -98,8 +99,10 @@ __device__ static inline int first_of(AnswerLds &l, int n, int k) {
     return have;
 }
 
-// The largest number (bits from the top on, as many as needed) that at least k of order[0..256) reach; 0 if fewer reach any above `low`.  A wave by itself.
-__device__ static inline unsigned kth_of(const unsigned *order, int k, int lane, unsigned low) {
+// A number that at least k of the 256 orders reach, or `low` where fewer are above it; `many`: how many reach it, or are above `low`.  A wave by itself.
+// Cheapest the k-th largest of the largest of 64 groups of four, or of 16 groups of sixteen; where the threads that reach that are too many for the list, the
+// k-th largest order itself, bit by bit.
+__device__ static inline unsigned kth_of(const unsigned *order, int k, int lane, unsigned low, int &many) {
     unsigned o[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = order[i * 64 + lane];
@@ -109,12 +112,29 @@ __device__ static inline unsigned kth_of(const unsigned *order, int k, int lane,
         for (int i = 0; i < 4; ++i) c += __popcll(__ballot(o[i] >= q));
         return c;
     };
-    if (reach(low + 1) < k) return 0;
-    unsigned tau = 0;
+    auto larger = [](unsigned p, unsigned q) { return p > q ? p : q; };
+    auto smaller = [](unsigned p, unsigned q) { return p < q ? p : q; };
+    unsigned g = larger(larger(o[0], o[1]), larger(o[2], o[3]));
+    int above = 0;   // groups above this lane's
+    if (k <= 16) {
+        g = larger(g, (unsigned)__builtin_amdgcn_update_dpp(0, (int)g, 0xB1, 0xf, 0xf, false));   // of the four lanes
+        g = larger(g, (unsigned)__builtin_amdgcn_update_dpp(0, (int)g, 0x4E, 0xf, 0xf, false));
+#pragma unroll
+        for (int i = 0; i < 64; i += 4) above += (unsigned)__builtin_amdgcn_readlane((int)g, i) > g;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 64; ++i) above += (unsigned)__builtin_amdgcn_readlane((int)g, i) > g;
+    }
+    const unsigned kth = wave_all(above < k ? g : 0xffffffffu, smaller);
+    unsigned tau = kth > low ? kth : low;
+    many = reach(tau + (tau == low));
+    if (many <= kFewThreads) return tau;
+    if (reach(low + 1) < k) return low;
+    tau = 0;
     for (int bit = 31; bit >= 0; --bit) {
         const unsigned q = tau | 1u << bit;
         const int c = reach(q);
-        if (c >= k) tau = q;
+        if (c >= k) { tau = q; many = c; }
         if (c == k) break;
     }
     return tau;
@@ -202,27 +222,28 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
             }
         }
         if (k > 0) {
-            // What is above the bar, and of that no more than what reaches the k-th largest of the threads' maxima.
+            // What is above the bar, and of that not much more than the k-th largest of the threads' maxima reach.
             unsigned *order = l.order[(seg - seg0) & 1];
             order[t] = order_of(most);
             if (t == 0) l.n = have;
             __syncthreads();
-            const unsigned tau = kth_of(order, k, lane, order_of(bar));
-            const bool equal = tau != 0;                       // then those equal to it too, as far as they are needed
+            int many = 0;
+            const unsigned low = order_of(bar), tau = kth_of(order, k, lane, low, many);
+            const bool equal = tau != low, all_equal = equal && many <= kFewThreads;   // then those equal to it too, as far as they are needed
             const float from = equal ? of_order(tau) : bar;
             auto put = [&](float value, int i) { l.list[atomicAdd(&l.n, 1)] = key_of(value, base + i); };
-            if (most > from) {
+            if (most > from || (all_equal && most == from)) {
 #pragma unroll
                 for (int j = 0; j < CHUNKS; ++j) {
                     if (j * CHUNK >= count) break;
 #pragma unroll
                     for (int e = 0; e < N; ++e)
-                        if (v[j * N + e] > from) put(v[j * N + e], j * CHUNK + t * N + e);
+                        if (v[j * N + e] > from || (all_equal && v[j * N + e] == from)) put(v[j * N + e], j * CHUNK + t * N + e);
                 }
             }
             __syncthreads();
             int n = l.n;
-            if (equal)   // at least k logits are as large as `from`: of those equal to it the first ones are needed, chunk by chunk
+            if (equal && !all_equal)   // at least k logits are as large as `from`: of those equal to it the first ones are needed, chunk by chunk
                 for (int j = 0; n - have < k && j * CHUNK < count; ++j) {
                     __syncthreads();
 #pragma unroll
@@ -267,11 +288,15 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
                 put(5 + 2 * i, (int)(unsigned)(key >> 32));
             }
         }
+        // The stores and the loads behind them go past the L2s one by one: a release and an acquire of the counter would write back and drop all of an
+        // XCD's L2 for each workgroup (64 x 50001, 448 workgroups, no top classes: 11.7 us for 7.9).
         __builtin_amdgcn_s_waitcnt(0);   // this thread's stores have been made
-        __syncthreads();
-        if (t == 0) l.last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        __syncthreads();                 // ... and so have the workgroup's
+        if (t == 0) l.last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
         __syncthreads();
         if (!l.last) return;
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
         if (t == 0) {
             __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             l.n = 0;
@@ -299,7 +324,8 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
             }
             l.order[0][t] = (unsigned)(most >> 32);
             __syncthreads();
-            const unsigned tau = kth_of(l.order[0], k, lane, 0);
+            int many;
+            const unsigned tau = kth_of(l.order[0], k, lane, 0, many);
             if (most)
 #pragma unroll
                 for (int i = 0; i < EACH; ++i)
