@@ -79,10 +79,9 @@ __device__ static inline void fc4_rows(const uint8_t *(&q)[NT], const Fc4Args &a
 // Scales and zero points in LDS, as fp32 [tile][group][ROWS] and bytes [tile][group][ROWS], of groups j0 .. j0 + groups of `count` tiles of ROWS weight rows,
 // every wgs-th from `tile` on: read from memory by the lanes that need them, a scale of each of sixteen rows would bring a line of each of them from the XCD's
 // L2 to the CU for every use.
-template <int ROWS, int THREADS, bool Z>
+template <int ROWS, int THREADS, int U, bool Z>   // U: loads of a thread under way
 __device__ static inline void fc4_scales(const Fc4Kernel &f, int tile, int wgs, int count, int j0, int groups, float *scale, uint8_t *zero, int t) {
     const Fc4Args &a = f.a;
-    constexpr int U = 4;   // loads of a thread under way
     const int lots = (groups + 15) / 16, total = count * lots * (16 * ROWS);   // sixteen groups of each row
     struct Place { int tile, row, j; };
     auto place = [&](int i) {
@@ -90,14 +89,11 @@ __device__ static inline void fc4_scales(const Fc4Kernel &f, int tile, int wgs, 
         const int lot = i / (16 * ROWS), mine = count == 1 ? 0 : (int)fast_div(lot, f.lots_div);
         return Place{mine, i / 16 % ROWS, (lot - mine * lots) * 16 + i % 16};
     };
-    auto take = [&](auto *p) {
-        typedef typename std::remove_const<typename std::remove_pointer<decltype(p)>::type>::type S;
+    auto take = [&](auto *p, auto value) {
         for (int base = 0; base < total; base += U * THREADS) {
-            S v[U];
-            uint8_t z[U];
+            unsigned v[U], z[U];   // words: 16-bit values packed two to a register would be waited for one by one
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (base + u * THREADS >= total) break;
                 const Place to = place(base + u * THREADS + t);
                 const int at = (tile + to.tile * wgs) * ROWS + to.row, n = at < a.cout ? at : a.cout - 1, j = j0 + (to.j < groups ? to.j : groups - 1);
                 v[u] = p[n * a.scale_stride + j];
@@ -107,17 +103,25 @@ __device__ static inline void fc4_scales(const Fc4Kernel &f, int tile, int wgs, 
             for (int u = 0; u < U; ++u) {
                 const int i = base + u * THREADS + t;
                 const Place at = place(i);
-                if (i >= total) break;
-                if (at.j >= groups) continue;
                 const int to = (at.tile * groups + at.j) * ROWS + at.row;
-                scale[to] = (float)v[u];
-                if (Z) zero[to] = z[u];
+                if (i < total && at.j < groups) {
+                    scale[to] = value(v[u]);
+                    if (Z) zero[to] = (uint8_t)z[u];
+                }
             }
         }
     };
-    if (a.scale_dtype == DT_F32) take(static_cast<const float *>(a.scales));
-    else if (a.scale_dtype == DT_F16) take(static_cast<const f16 *>(a.scales));
-    else take(static_cast<const bf16 *>(a.scales));
+    if (a.scale_dtype == DT_F32) take(static_cast<const unsigned *>(a.scales), [](unsigned v) { return __builtin_bit_cast(float, v); });
+    else if (a.scale_dtype == DT_F16) take(static_cast<const uint16_t *>(a.scales), [](unsigned v) { return (float)__builtin_bit_cast(f16, (uint16_t)v); });
+    else take(static_cast<const uint16_t *>(a.scales), [](unsigned v) { return __builtin_bit_cast(float, v << 16); });
+    __builtin_amdgcn_s_waitcnt(0);   // said once here, or the compiler waits in every turn of a loop behind this for loads that lanes without a place may have left
+}
+
+// The bias of the same rows, [tile][ROWS]: where a tile ends, a load would wait for the weights under way.
+template <int ROWS>
+__device__ static inline float fc4_bias(const Fc4Args &a, int tile, int wgs, int count, int i) {
+    const int n = (tile + i / ROWS * wgs) * ROWS + i % ROWS;
+    return a.bias && i < count * ROWS && n < a.cout ? a.bias[n] : 0.f;
 }
 
 // A lane has 32 inputs of its row, 8 a word; a matrix step takes 8 inputs of each of the four lanes of a row.  Word j of lane group kq becomes word kq of
@@ -242,7 +246,7 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f
     const int c = lane & 15, kq = lane >> 4;
     const int rows = a.rows, blocks = (a.cin + kBlock - 1) / kBlock, part_bytes = blocks * rows * (kBlock * 2);
     float *meet = reinterpret_cast<float *>(lds + PARTS * part_bytes), *xs = meet + 2 * MEET;           // xs: [block][16], what x was divided by
-    float *scales = xs + (X == X_F16 ? 0 : blocks * 16);                                                   // [tile][group][ROWS]
+    float *bias = xs + (X == X_F16 ? 0 : blocks * 16), *scales = bias + own * ROWS;                         // [tile][ROWS], [tile][group][ROWS]
     uint8_t *zeros = reinterpret_cast<uint8_t *>(scales + own * groups * ROWS);
     const int mine = (blocks - kw + KW - 1) / KW;   // blocks of a tile: kw, kw + KW, ...
     const int todo_tiles = (tiles - (int)blockIdx.x + wgs - 1) / wgs, todo = todo_tiles * mine;
@@ -268,6 +272,7 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f
 #pragma unroll
         for (int u = 0; u < D; ++u) ask(w[u]);
 
+    const float first_bias = fc4_bias<ROWS>(a, blockIdx.x, wgs, todo_tiles, t);
     constexpr int U = 4;   // pieces of eight inputs a thread has under way; sixteen threads a row and block
     const int piece = t & 15;
     for (int base = 0; base < rows * blocks * 16; base += U * THREADS) {
@@ -299,7 +304,8 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f
             if (X == X_F32) *reinterpret_cast<f16x8 *>(to + part_bytes) = lo;
         }
     }
-    fc4_scales<ROWS, THREADS, Z>(f, blockIdx.x, wgs, todo_tiles, 0, groups, scales, zeros, t);
+    fc4_scales<ROWS, THREADS, 2, Z>(f, blockIdx.x, wgs, todo_tiles, 0, groups, scales, zeros, t);
+    for (int i = t; i < todo_tiles * ROWS; i += THREADS) bias[i] = i == t ? first_bias : fc4_bias<ROWS>(a, blockIdx.x, wgs, todo_tiles, i);
     __syncthreads();
 
     // A row's sixteen pieces of a block change places with the row's number: every sixteen lanes write, and read, 256 different bytes of the 256 that LDS serves at a time.
@@ -360,12 +366,13 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f
             float v = 0.f;
 #pragma unroll
             for (int k = 0; k < KW; ++k) v += part[k * (NW * NT * 256) + o];
-            fc4_store(a.y, m * a.y_stride + n, a.y_dtype, v + (a.bias ? a.bias[n] : 0.f));
+            fc4_store(a.y, m * a.y_stride + n, a.y_dtype, v + bias[(o >> 8) * 16 + (l & 15)]);
         }
         tile += wgs;
         side ^= 1;
         block = kw;
         slot += groups * ROWS;
+        bias += ROWS;
     };
     if (todo == 0) {   // fewer blocks than groups of waves
         while (tile < tiles) finish();
@@ -389,13 +396,13 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f
 
 // ---- many rows --------------------------------------------------------------------------------------
 // A workgroup computes 16 MT rows by 16 NT NW weight rows; its KW groups of waves take the blocks of K in turn.  The NW waves of a group stage the group's
-// block of x in one of two LDS buffers while they multiply the other one, from registers that were loaded two blocks ahead; weights go straight to the
-// registers of the wave that multiplies them, three blocks ahead.
+// block of x in one of two LDS buffers while they multiply the other one, from registers that were loaded two phases before; weights go straight to the
+// registers of the wave that multiplies them, as early.
 template <int X, int MT, int NT, int NW, int KW>
 struct Fc4Many {
     static constexpr int ROWS = 16 * MT, COLS = 16 * NT * NW, THREADS = 64 * NW * KW, PARTS = X == X_F32 ? 2 : 1, ITEMS = ROWS / 4 / NW;   // ITEMS of a wave: four rows of a block each
     static constexpr int PART = 4 * ROWS * 64, BUFFER = PARTS * PART + (X == X_F16 ? 0 : ROWS * 4);   // bytes of a block
-    static constexpr int STAGED = KW * 2 * BUFFER, MEET = NW * KW * MT * NT * 1024;
+    static constexpr int STAGED = KW * 2 * BUFFER, MEET = NW * (KW - 1) * MT * NT * 1024, FIXED = (STAGED > MEET ? STAGED : MEET) + COLS * 4;   // LDS: x, where later the groups meet; the bias; the scales
 };
 
 template <int X, int MT, int NT, int NW, int KW, int GM, bool Z>
@@ -410,9 +417,8 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
     const int m0 = blockIdx.y * ROWS, rows = a.rows - m0 < ROWS ? a.rows - m0 : ROWS;
     const uint8_t *q[NT];
     fc4_rows<NT>(q, a, (blockIdx.x * NW + nw) * (16 * NT), c);
-    const int blocks = (a.cin + kBlock - 1) / kBlock, phases = (blocks + KW - 1) / KW;
     char *const mine = lds + kw * (2 * BUFFER);
-    float *scales = reinterpret_cast<float *>(lds + S::STAGED);
+    float *bias = reinterpret_cast<float *>(lds + S::FIXED - COLS * 4), *scales = reinterpret_cast<float *>(lds + S::FIXED);
     uint8_t *zeros = reinterpret_cast<uint8_t *>(scales + chunk_groups * COLS);
     f32x4 total[MT][NT] = {};
     unsigned magic = 0x64006400u;
@@ -428,19 +434,16 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
         const int row = (nw * ITEMS + i) * 4 + (lane >> 4);
         xrow[i] = static_cast<const char *>(a.x) + (m0 + (row < rows ? row : rows - 1)) * a.x_stride * (X == X_F32 ? 4 : 2);
     }
-    auto block_of = [&](int phase) {   // behind the last block: that one again
+    const int whole = a.cin / kBlock, phases = (whole + KW - 1) / KW;
+    auto block_of = [&](int phase) {   // behind the last whole block: that one again
         const int block = phase * KW + kw;
-        return block < blocks ? block : blocks - 1;
+        return block < whole ? block : whole - 1;
     };
-    auto ask_x = [&](int phase, Fc4X<X> (&to)[ITEMS]) {
+    auto ask_x = [&](int block, Fc4X<X> (&to)[ITEMS]) {
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) to[i].load(xrow[i], block_of(phase) * kBlock + piece * 8, a.cin);
+        for (int i = 0; i < ITEMS; ++i) to[i].load(xrow[i], block * kBlock + piece * 8, a.cin);
     };
-    auto stage = [&](int phase, Fc4X<X> (&v)[ITEMS], char *to) {
-        const int block = block_of(phase);
-        if ((block + 1) * kBlock > a.cin)
-#pragma unroll
-            for (int i = 0; i < ITEMS; ++i) v[i].shift(block * kBlock + piece * 8, a.cin);
+    auto stage = [&](Fc4X<X> (&v)[ITEMS], char *to) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int row = (nw * ITEMS + i) * 4 + (lane >> 4);
@@ -456,14 +459,13 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
             if (X == X_F32) *reinterpret_cast<f16x8 *>(at + PART) = lo;
         }
     };
-    Fc4Weights<NT> w[4];
+    Fc4Weights<NT> w[2];
     const int slot = nw * (16 * NT) + c;
     int xat[4];
 #pragma unroll
     for (int step = 0; step < 4; ++step) xat[step] = c * (kBlock * 2) + (((step * 4 + kq) ^ c) << 4);
     int j0 = 0;   // first group of the chunk
     auto multiply = [&](Fc4Weights<NT> &v, int block, const char *from) {
-        if ((block + 1) * kBlock > a.cin) v.shift(f, block, kq);
 #pragma unroll
         for (int j = 0; j < NT; ++j) fc4_turn(v.w[j]);
         f32x4 p[MT][NT];
@@ -507,52 +509,93 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
             }
         }
     };
-#pragma unroll
-    for (int u = 0; u < 3; ++u) w[u].load(f, q, block_of(u), kq);
-    ask_x(0, x[0]);
-    ask_x(1, x[1]);
-    stage(0, x[0], mine);
-    for (int phase = 0; phase < phases; phase += 4) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (phase + u >= phases) break;
-            if ((phase + u) % chunk == 0) {   // the scales of the next phases
-                const int k0 = (phase + u) * KW * kBlock, k1 = k0 + chunk * KW * kBlock;
-                j0 = (int)fast_div(k0, f.group_div);
-                if (phase + u > 0) __syncthreads();
-                fc4_scales<COLS, S::THREADS, Z>(f, blockIdx.x, 1, 1, j0, (int)fast_div((k1 < a.cin ? k1 : a.cin) - 1, f.group_div) - j0 + 1, scales, zeros, t);
+    auto take_scales = [&](int phase) {   // of the next `chunk` phases
+        const int k0 = phase * KW * kBlock, k1 = k0 + chunk * KW * kBlock;
+        j0 = (int)fast_div(k0, f.group_div);
+        fc4_scales<COLS, S::THREADS, 4, Z>(f, blockIdx.x, 1, 1, j0, (int)fast_div((k1 < a.cin ? k1 : a.cin) - 1, f.group_div) - j0 + 1, scales, zeros, t);
+    };
+    const float my_bias = fc4_bias<COLS>(a, blockIdx.x, 1, 1, t);
+    if (phases > 0) {
+        w[0].load(f, q, block_of(0), kq);
+        w[1].load(f, q, block_of(1), kq);
+        ask_x(block_of(0), x[0]);
+        ask_x(block_of(1), x[1]);
+        take_scales(0);
+        stage(x[0], mine);
+        ask_x(block_of(2), x[0]);
+        for (int from = 0; from < phases; from += chunk) {   // chunks of an even number of phases, or one
+            if (from > 0) {
+                __syncthreads();
+                take_scales(from);
             }
-            ask_x(phase + u + 2, x[u & 1]);
-            w[(u + 3) & 3].load(f, q, block_of(phase + u + 3), kq);
-            __syncthreads();
-            const int block = (phase + u) * KW + kw;
-            if (block < blocks) multiply(w[u], block, mine + (u & 1) * BUFFER);
-            stage(phase + u + 1, x[(u + 1) & 1], mine + ((u + 1) & 1) * BUFFER);
+            const int to = from + chunk < phases ? from + chunk : phases;
+            for (int phase = from; phase < to; phase += 2) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    __syncthreads();
+                    const int block = (phase + u) * KW + kw;
+                    if (block < whole) multiply(w[u], block, mine + u * BUFFER);   // an odd last phase has a second one with nothing to multiply
+                    w[u].load(f, q, block_of(phase + u + 2), kq);
+                    stage(x[1 - u], mine + (1 - u) * BUFFER);
+                    ask_x(block_of(phase + u + 3), x[1 - u]);
+                }
+            }
         }
     }
-    // The groups of waves meet in LDS: [kw][nw][tile][4][64]
-    __syncthreads();
-    float *part = reinterpret_cast<float *>(lds);
-    constexpr int TILES = MT * NT;
+    if (whole * kBlock < a.cin) {   // the rest of K is one group's
+        __syncthreads();
+        if (whole % (KW * chunk) == 0) take_scales(phases);
+        if (kw == 0) {
+            ask_x(whole, x[0]);
+            w[0].load(f, q, whole, kq);
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) part[(((wave * MT + i) * NT + j) * 4 + e) * 64 + lane] = total[i][j][e];
-    __syncthreads();
-    for (int o = t; o < NW * TILES * 256; o += 64 * NW * KW) {   // o = ((nw, i, j), e, lane)
-        const int l = o & 63, e = (o >> 6) & 3, tile = (o >> 8) % TILES, ow = (o >> 8) / TILES;
-        const int m = (tile / NT) * 16 + (l >> 4) * 4 + e, n = (blockIdx.x * NW + ow) * (16 * NT) + (tile % NT) * 16 + (l & 15);
-        if (m >= rows || n >= a.cout) continue;
-        float v = 0.f;
-#pragma unroll
-        for (int k = 0; k < KW; ++k) v += part[k * (NW * TILES * 256) + o];
-        fc4_store(a.y, (m0 + m) * a.y_stride + n, a.y_dtype, v + (a.bias ? a.bias[n] : 0.f));
+            for (int i = 0; i < ITEMS; ++i) x[0][i].shift(whole * kBlock + piece * 8, a.cin);
+            w[0].shift(f, whole, kq);
+            stage(x[0], mine);
+        }
+        __syncthreads();
+        if (kw == 0) multiply(w[0], whole, mine);
     }
+    // The groups of waves meet in LDS: [kw > 0][nw][tile][4][64]; the first group adds its own and stores.
+    __syncthreads();
+    if (t < COLS) bias[t] = my_bias;
+    float *part = reinterpret_cast<float *>(lds) + nw * (MT * NT * 256) + lane;
+    constexpr int GROUP = NW * MT * NT * 256;
+    if (kw > 0)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part[(kw - 1) * GROUP + ((i * NT + j) * 4 + e) * 64] = total[i][j][e];
+    __syncthreads();
+    if (kw > 0) return;
+    auto put = [&](auto *y) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int col = (nw * NT + j) * 16 + c, n = blockIdx.x * COLS + col;
+            const float add = bias[col];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int m = i * 16 + kq * 4 + e;
+                    float v = total[i][j][e];
+#pragma unroll
+                    for (int k = 1; k < KW; ++k) v += part[(k - 1) * GROUP + ((i * NT + j) * 4 + e) * 64];
+                    if (m < rows && n < a.cout) y[(m0 + m) * a.y_stride + n] = (typename std::remove_pointer<decltype(y)>::type)(v + add);
+                }
+        }
+    };
+    if (a.y_dtype == DT_F32) put(static_cast<float *>(a.y));
+    else if (a.y_dtype == DT_F16) put(static_cast<f16 *>(a.y));
+    else put(static_cast<bf16 *>(a.y));
 }
 
-constexpr int kLdsBytes = 160 * 1024, kFewBytes = 80 * 1024;   // kFewBytes: two workgroups of few rows share a CU
+constexpr int kLdsBytes = 160 * 1024;
+// LDS of a workgroup of few rows: two share a CU.  fp32 activations may have all of it where there is a workgroup for each CU at most: 16 x 2048 to
+// 1000 7.7 us, in the form for many rows, which converts them as often, 8.4; but fp16 16 x 4096 to 4096 8.6 us, and 7.0 in that form.
+constexpr int few_lds(bool fp32, int64_t tiles) { return fp32 && tiles <= 256 ? kLdsBytes : kLdsBytes / 2; }
 
 static int fc4_groups(const Fc4Args &a) { return (a.cin + a.group - 1) / a.group; }
 static Fc4Kernel fc4_kernel_args(const Fc4Args &a) { return {a, make_fast_div((uint32_t)a.group), make_fast_div((uint32_t)(fc4_groups(a) + 15) / 16)}; }
@@ -564,13 +607,14 @@ static int64_t few_bytes(const Fc4Args &a) {
     return (X == X_F32 ? 2 : 1) * a.rows * blocks * kBlock * 2 + 2 * NW * KW * NT * 1024 + (X == X_F16 ? 0 : blocks * 64);
 }
 template <int NT, int NW, bool Z>
-static int64_t few_tile_bytes(const Fc4Args &a) { return (int64_t)fc4_groups(a) * (16 * NT * NW) * (Z ? 5 : 4); }
+static int64_t few_tile_bytes(const Fc4Args &a) { return ((int64_t)fc4_groups(a) * (Z ? 5 : 4) + 4) * (16 * NT * NW); }
 
 template <int X, int NT, int NW, int KW, int GM, int D, bool Z>
-static hipError_t launch_few(const Fc4Args &a, hipStream_t s, int most_wgs = 512) {
+static hipError_t launch_few(const Fc4Args &a, int most_wgs, hipStream_t s) {
+    const int tiles = (a.cout + 16 * NT * NW - 1) / (16 * NT * NW), lds = few_lds(X == X_F32, tiles);
     const int64_t fixed = few_bytes<X, NT, NW, KW>(a), tile = few_tile_bytes<NT, NW, Z>(a);
-    if (a.rows > 16 || a.cin < kShortIn || fixed + tile > kFewBytes) return hipErrorInvalidValue;
-    const int tiles = (a.cout + 16 * NT * NW - 1) / (16 * NT * NW), fit = (int)((kFewBytes - fixed) / tile);
+    if (a.rows > 16 || a.cin < kShortIn || fixed + tile > lds) return hipErrorInvalidValue;
+    const int fit = (int)((lds - fixed) / tile);
     int own = (tiles + most_wgs - 1) / most_wgs;
     own = own < fit ? own : fit;
     const int wgs = (tiles + own - 1) / own;
@@ -581,31 +625,32 @@ static hipError_t launch_few(const Fc4Args &a, hipStream_t s, int most_wgs = 512
 template <int X, int MT, int NT, int NW, int KW, int GM, bool Z>
 static hipError_t launch_many(const Fc4Args &a, hipStream_t s) {
     typedef Fc4Many<X, MT, NT, NW, KW> S;
-    static_assert(S::MEET <= kLdsBytes && S::STAGED + (KW * 4 / GM + 1) * S::COLS * 5 <= kLdsBytes, "LDS");
+    static_assert(S::FIXED + (2 * KW * 4 / GM + 1) * S::COLS * 5 <= kLdsBytes, "LDS");
     if (a.cin < kShortIn) return hipErrorInvalidValue;
     // The scales of as many phases as fit.  Inputs that begin anywhere touch a group more than they fill.
-    const int phases = (a.cin + KW * kBlock - 1) / (KW * kBlock), most = (kLdsBytes - S::STAGED) / (S::COLS * (Z ? 5 : 4));
+    const int phases = (a.cin + KW * kBlock - 1) / (KW * kBlock), most = (kLdsBytes - S::FIXED) / (S::COLS * (Z ? 5 : 4));
     int chunk = phases, groups = fc4_groups(a);
-    while (groups > most && chunk > 1) {
-        chunk = (chunk + 1) / 2;
+    while (groups > most && chunk > 2) {   // an even number of them
+        chunk = (chunk + 3) / 4 * 2;
         groups = (int)(((int64_t)chunk * KW * kBlock + a.group - 1) / a.group) + 1;
     }
     if (groups > most) return hipErrorInvalidValue;
-    const int bytes = S::STAGED + groups * S::COLS * (Z ? 5 : 4);
+    const int bytes = S::FIXED + groups * S::COLS * (Z ? 5 : 4);
     for (int m = 0; m < a.rows; m += 65535 * S::ROWS) {   // rows beyond the grid's y
         Fc4Kernel f = fc4_kernel_args(a);
         f.a.rows = a.rows - m < 65535 * S::ROWS ? a.rows - m : 65535 * S::ROWS;
         f.a.x = static_cast<const char *>(a.x) + m * a.x_stride * (a.x_dtype == DT_F32 ? 4 : 2);
         f.a.y = static_cast<char *>(a.y) + m * a.y_stride * (a.y_dtype == DT_F32 ? 4 : 2);
-        fc4_many_kernel<X, MT, NT, NW, KW, GM, Z><<<dim3((a.cout + S::COLS - 1) / S::COLS, (f.a.rows + S::ROWS - 1) / S::ROWS), S::THREADS, bytes > S::MEET ? bytes : S::MEET, s>>>(f, chunk, groups);
+        fc4_many_kernel<X, MT, NT, NW, KW, GM, Z><<<dim3((a.cout + S::COLS - 1) / S::COLS, (f.a.rows + S::ROWS - 1) / S::ROWS), S::THREADS, bytes, s>>>(f, chunk, groups);
     }
     return hipGetLastError();
 }
 
 // ---- the choice of a form ----------------------------------------------------------------------------
 struct Fc4Plan {
-    enum Form { SHORT, FEW, FEW_PAIRS, MANY1, MANY2_32, MANY2_64, MANY2_128, MANY4_32, MANY4_64, MANY4_128 } form;
+    enum Form { SHORT, FEW, FEW_PAIRS, MANY1_16, MANY1_64, MANY2_16, MANY2_64, MANY4_64, MANY4_128 } form;
     int rows, cols, threads;   // of a workgroup; FEW and FEW_PAIRS: `cols` at a time
+    int most;                  // workgroups of those
 };
 Fc4Plan fc4_plan(const Fc4Args &a);
 template <int X>
@@ -615,15 +660,14 @@ template <int X, int GM, bool Z>
 static hipError_t launch_fc4_form(const Fc4Args &a, const Fc4Plan &p, hipStream_t s) {
     constexpr bool two = X == X_F32;   // operands in two parts: twice the LDS
     switch (p.form) {
-        case Fc4Plan::FEW: return launch_few<X, 1, 1, 8, GM, 2, Z>(a, s);
-        case Fc4Plan::FEW_PAIRS: return launch_few<X, 1, 2, 4, GM, 4, Z>(a, s, 1024);
-        case Fc4Plan::MANY1: return launch_many<X, 1, 1, 1, 8, GM, Z>(a, s);
-        case Fc4Plan::MANY2_32: return launch_many<X, 2, 1, 2, 4, GM, Z>(a, s);
+        case Fc4Plan::FEW: return launch_few<X, 1, 1, 8, GM, 2, Z>(a, p.most, s);
+        case Fc4Plan::FEW_PAIRS: return launch_few<X, 1, 2, 4, GM, 4, Z>(a, p.most, s);
+        case Fc4Plan::MANY1_16: return launch_many<X, 1, 1, 1, 8, GM, Z>(a, s);
+        case Fc4Plan::MANY1_64: return launch_many<X, 1, 1, 4, 4, GM, Z>(a, s);
+        case Fc4Plan::MANY2_16: return launch_many<X, 2, 1, 1, two ? 4 : 8, GM, Z>(a, s);
         case Fc4Plan::MANY2_64: return launch_many<X, 2, 1, 4, two ? 2 : 4, GM, Z>(a, s);
-        case Fc4Plan::MANY2_128: return launch_many<X, 2, 1, 8, 2, GM, Z>(a, s);
-        case Fc4Plan::MANY4_32: return launch_many<X, 4, 1, 2, two ? 2 : 4, GM, Z>(a, s);
-        case Fc4Plan::MANY4_64: return launch_many<X, 4, 2, 2, two ? 2 : 4, GM, Z>(a, s);
-        case Fc4Plan::MANY4_128: return launch_many<X, 4, 1, 8, 2, GM, Z>(a, s);
+        case Fc4Plan::MANY4_64: return launch_many<X, 4, 1, 4, two ? 2 : 4, GM, Z>(a, s);
+        case Fc4Plan::MANY4_128: return launch_many<X, 4, 2, 4, 2, GM, Z>(a, s);
         default: return hipErrorInvalidValue;
     }
 }

@@ -38,32 +38,40 @@ static hipError_t launch_short(const Fc4Args &a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Measured in graphs of calls over several sets of weights, us a call (K = 4096, fp16, groups of 128, unless said otherwise):
+//   up to 16 rows  x in LDS once a workgroup, which walks tiles of 16 weight rows; pairs of tiles where there are more than two for each CU
+//                  (1 x 8192 bf16 to 32001: 31.0 in pairs, 32.3-37.7 one by one), but one by one up to that (4 x 4096 to 16384: 10.3 and 11.0)
+//   more of x than LDS holds, or more rows: x in blocks.  64 or 128 weight rows a workgroup share a block of x, 16 make more workgroups:
+//                  16 rows to 16384 11.5 us with 64, 19.6 with 16; 32 rows to 16384 16.6 and 16.9 (32), to 4096 14.5 and 10.0;
+//                  64 rows to 16384 (groups of 64, zero points) 21-24 us with 64, 38 with 128; 512 rows to 4096 42.9 and 29.
+//   32 or 64 rows  128 rows to 1000: 10.6 us with 32 rows and 16 weight rows a workgroup, 15.6 with 64 and 32.
 Fc4Plan fc4_plan(const Fc4Args &a) {
     const bool two = a.x_dtype == DT_F32;
     auto wgs = [&](int rows, int cols) { return (int64_t)((a.rows + rows - 1) / rows) * ((a.cout + cols - 1) / cols); };
-    if (a.cin < kShortIn) return {Fc4Plan::SHORT, kShortRows, 4, 256};
+    if (a.cin < kShortIn) return {Fc4Plan::SHORT, kShortRows, 4, 256, 0};
+    constexpr int enough = 200;   // workgroups that keep 256 CUs busy
     if (a.rows <= 16) {
-        const int64_t blocks = (a.cin + kBlock - 1) / kBlock, fixed = (two ? 2 : 1) * a.rows * blocks * kBlock * 2 + 16 * 1024 + blocks * 64, scales = (int64_t)fc4_groups(a) * 16 * 5;
-        if (wgs(16, 16) > 512 && fixed + 2 * scales <= kFewBytes) return {Fc4Plan::FEW_PAIRS, 16, 32, 512};
-        if (fixed + scales <= kFewBytes) return {Fc4Plan::FEW, 16, 16, 512};
-        return {Fc4Plan::MANY1, 16, 16, 512};
+        const int64_t blocks = (a.cin + kBlock - 1) / kBlock, fixed = (two ? 2 : 1) * a.rows * blocks * kBlock * 2 + 16 * 1024 + blocks * 64, scales = ((int64_t)fc4_groups(a) * 5 + 4) * 16;
+        if (wgs(16, 16) > 1024 && fixed + 2 * scales <= few_lds(two, wgs(16, 32))) return {Fc4Plan::FEW_PAIRS, 16, 32, 512, 1024};
+        if (fixed + scales <= few_lds(two, wgs(16, 16))) return {Fc4Plan::FEW, 16, 16, 512, 512};
+        if (wgs(16, 64) >= enough) return {Fc4Plan::MANY1_64, 16, 64, 1024, 0};
+        return {Fc4Plan::MANY1_16, 16, 16, 512, 0};
     }
-    constexpr int enough = 200;
-    if (a.rows <= 32) {
-        if (wgs(32, 128) >= enough) return {Fc4Plan::MANY2_128, 32, 128, 1024};
-        if (wgs(32, 64) >= enough) return {Fc4Plan::MANY2_64, 32, 64, two ? 512 : 1024};
-        return {Fc4Plan::MANY2_32, 32, 32, 512};
+    if (a.rows > 32) {
+        if (wgs(64, 128) >= enough) return {Fc4Plan::MANY4_128, 64, 128, 512, 0};
+        if (wgs(64, 64) >= enough) return {Fc4Plan::MANY4_64, 64, 64, two ? 512 : 1024, 0};
     }
-    if (wgs(64, 128) >= enough) return {Fc4Plan::MANY4_128, 64, 128, 1024};
-    if (wgs(64, 64) >= enough) return {Fc4Plan::MANY4_64, 64, 64, two ? 256 : 512};
-    return {Fc4Plan::MANY4_32, 64, 32, two ? 256 : 512};
+    if (wgs(32, 64) >= enough) return {Fc4Plan::MANY2_64, 32, 64, two ? 512 : 1024, 0};
+    return {Fc4Plan::MANY2_16, 32, 16, two ? 256 : 512, 0};
 }
 
 void fc4_grid(const Fc4Args &a, dim3 *grid, int *block) {
     const Fc4Plan p = fc4_plan(a);
     *grid = dim3((a.cout + p.cols - 1) / p.cols, (a.rows + p.rows - 1) / p.rows);
-    if (p.form == Fc4Plan::FEW && grid->x > 512) grid->x = 512;
-    if (p.form == Fc4Plan::FEW_PAIRS && grid->x > 1024) grid->x = 1024;
+    if (p.most > 0 && (int)grid->x > p.most) {   // fewer workgroups walk all tiles, an even share of them each
+        const unsigned own = (grid->x + p.most - 1) / p.most;
+        grid->x = (grid->x + own - 1) / own;
+    }
     *block = p.threads;
 }
 
