@@ -46,6 +46,19 @@ def test_sizes(ctx, size, types):
     check(ctx, *size, x=x, scale=scale, y=y, zeros=zeros, seed=sum(size))
 
 
+# Wide enough for the forms that share activations between many weight rows or walk over tiles, with rows that end inside a block, and long enough that
+# the scales come in several lots.
+WIDE = [(1, 160, 16500, 32), (5, 200, 16433, 96), (16, 2200, 12900, 64), (16, 4000, 500, 32), (13, 10016, 40, 32), (24, 200, 12900, 64), (500, 300, 850, 128), (500, 168, 1700, 32),
+        (500, 264, 3300, 64), (450, 5000, 3300, 32), (30, 12000, 50, 32), (40, 3840, 33, 480)]
+
+
+@pytest.mark.parametrize("size", WIDE, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("types", [(F16, F16, F32, True), (BF16, BF16, F32, False), (BF16, F16, BF16, True), (F32, F32, F32, True)], ids=["fp16", "bf16", "bf16 plain", "fp32"])
+def test_wide_and_long(ctx, size, types):
+    x, scale, y, zeros = types
+    check(ctx, *size, x=x, scale=scale, y=y, zeros=zeros, seed=sum(size))
+
+
 @pytest.mark.parametrize("x", [F16, BF16, F32])
 @pytest.mark.parametrize("scale", [F16, BF16, F32])
 @pytest.mark.parametrize("y", [F16, BF16, F32])
