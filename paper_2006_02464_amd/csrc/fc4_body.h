@@ -430,16 +430,16 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f
 // A workgroup computes 16 MT rows by 16 NT NW weight rows; its KW groups of waves take the blocks of K in turn.  The NW waves of a group stage the group's
 // block of x in one of two LDS buffers while they multiply the other one, from registers that were loaded two phases before; weights go straight to the
 // registers of the wave that multiplies them, as early.
-template <int X, int MT, int NT, int NW, int KW>
+template <int X, int MT, int NT, int NW, int KW, int PB>
 struct Fc4Many {
     static constexpr int ROWS = 16 * MT, COLS = 16 * NT * NW, THREADS = 64 * NW * KW, PARTS = X == X_F32 ? 2 : 1, ITEMS = ROWS / 4 / NW;   // ITEMS of a wave: four rows of a block each
     static constexpr int PART = 4 * ROWS * 64, BUFFER = PARTS * PART + (X == X_F16 ? 0 : X == X_PLAIN ? ROWS * 16 : ROWS * 4);   // bytes of a block: operands, and what a row was divided by or its sums
-    static constexpr int STAGED = KW * 2 * BUFFER, MEET = NW * (KW - 1) * MT * NT * 1024, FIXED = (STAGED > MEET ? STAGED : MEET) + COLS * 4;   // LDS: x, where later the groups meet; the bias; the scales
+    static constexpr int STAGED = KW * 2 * PB * BUFFER, MEET = NW * (KW - 1) * MT * NT * 1024, FIXED = (STAGED > MEET ? STAGED : MEET) + COLS * 4;   // LDS: x, where later the groups meet; the bias; the scales
 };
 
-template <int X, int MT, int NT, int NW, int KW, int GM, bool Z>
+template <int X, int MT, int NT, int NW, int KW, int PB, int GM, bool Z>
 __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel f, int chunk, int chunk_groups) {   // chunk: phases whose scales LDS holds, in chunk_groups groups
-    typedef Fc4Many<X, MT, NT, NW, KW> S;
+    typedef Fc4Many<X, MT, NT, NW, KW, PB> S;
     constexpr int ROWS = S::ROWS, COLS = S::COLS, PARTS = S::PARTS, ITEMS = S::ITEMS, PART = S::PART, BUFFER = S::BUFFER;
     static_assert(ROWS / 4 % NW == 0, "rows in fours, evenly");
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -449,7 +449,7 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
     const int m0 = blockIdx.y * ROWS, rows = a.rows - m0 < ROWS ? a.rows - m0 : ROWS;
     const uint8_t *q[NT];
     fc4_rows<NT>(q, a, (blockIdx.x * NW + nw) * (16 * NT), c);
-    char *const mine = lds + kw * (2 * BUFFER);
+    char *const mine = lds + kw * (2 * PB * BUFFER);
     float *bias = reinterpret_cast<float *>(lds + S::FIXED - COLS * 4), *scales = reinterpret_cast<float *>(lds + S::FIXED);
     uint8_t *zeros = reinterpret_cast<uint8_t *>(scales + chunk_groups * COLS);
     f32x4 total[MT][NT] = {};
@@ -466,9 +466,10 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
         const int row = (nw * ITEMS + i) * 4 + (lane >> 4);
         xrow[i] = static_cast<const char *>(a.x) + (m0 + (row < rows ? row : rows - 1)) * a.x_stride * (X == X_F32 ? 4 : 2);
     }
-    const int whole = a.cin / kBlock, phases = (whole + KW - 1) / KW;
-    auto block_of = [&](int phase) {   // behind the last whole block: that one again
-        const int block = phase * KW + kw;
+    const int whole = a.cin / kBlock, phases = (whole + PB * KW - 1) / (PB * KW);
+    auto place_of = [&](int phase, int u) { return (phase * KW + kw) * PB + u; };
+    auto block_of = [&](int phase, int u) {   // behind the last whole block: that one again
+        const int block = place_of(phase, u);
         return block < whole ? block : whole - 1;
     };
     auto ask_x = [&](int block, Fc4X<X> (&to)[ITEMS]) {
@@ -486,7 +487,7 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
             }
             if (X == X_PLAIN) {
                 const float sum = fc4_sum_lanes<4 * GM>(v[i].sum());
-                if (piece % (4 * GM) == 0) reinterpret_cast<float *>(to + PARTS * PART)[piece / (4 * GM) * ROWS + row] = sum;
+                if (piece % (4 * GM) == 0) reinterpret_cast<float *>(to + PARTS * PART)[piece / (4 * GM) * ROWS + row] = Z ? sum : -24.f * sum;
             }
             f16x8 hi, lo;
             v[i].operands(by, hi, lo);
@@ -519,80 +520,108 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
                     xx[part][i] = *reinterpret_cast<const f16x8 *>(from + part * PART + i * (16 * kBlock * 2) + xat[step]);
+            if (step % GM == 0) {   // X_PLAIN: a group begins at -(16 + z) times its inputs' sum
+                float less[NT];
+                if (X == X_PLAIN && Z)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) less[j] = -16.f - (float)(zeros[at[step / GM] + j * 16] & 15);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const f32x4 of = X == X_PLAIN ? *reinterpret_cast<const f32x4 *>(from + PARTS * PART + (step / GM * ROWS + i * 16 + kq * 4) * 4) : f32x4{};
+#pragma unroll
+                    for (int j = 0; j < NT; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) p[i][j][e] = X == X_PLAIN && Z ? less[j] * of[e] : of[e];
+                }
+            }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
                 if constexpr (X == X_PLAIN) {
                     const bf16x8 ww = fc4_operand_plain(v.w[j][step], magic);
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xx[0][i]), ww, step % GM == 0 ? zero : p[i][j], 0, 0, 0);
+                    for (int i = 0; i < MT; ++i) p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xx[0][i]), ww, p[i][j], 0, 0, 0);
                 } else {
                     const f16x8 ww = fc4_operand<Z>(v.w[j][step], Z ? zeros[at[step / GM] + j * 16] : 0u, magic);
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
-                        p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xx[0][i], ww, step % GM == 0 ? zero : p[i][j], 0, 0, 0);
+                        p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xx[0][i], ww, p[i][j], 0, 0, 0);
                         if (X == X_F32) p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xx[PARTS - 1][i], ww, p[i][j], 0, 0, 0);
                     }
                 }
             }
             if (step % GM == GM - 1) {
-                float scale[NT], less[NT];
+                float scale[NT];
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    scale[j] = scales[at[step / GM] + j * 16];
-                    less[j] = X == X_PLAIN ? -(16.f + (Z ? (float)(zeros[at[step / GM] + j * 16] & 15) : 8.f)) : 0.f;
-                }
+                for (int j = 0; j < NT; ++j) scale[j] = scales[at[step / GM] + j * 16];
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    const int row = (X == X_PLAIN ? step / GM * ROWS : 0) + i * 16 + kq * 4;
-                    const f32x4 of = X != X_F16 ? *reinterpret_cast<const f32x4 *>(from + PARTS * PART + row * 4) : f32x4{};
+                    const f32x4 back = x_scaled(X) ? *reinterpret_cast<const f32x4 *>(from + PARTS * PART + (i * 16 + kq * 4) * 4) : f32x4{};
 #pragma unroll
                     for (int j = 0; j < NT; ++j)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            total[i][j][e] = X == X_F16   ? fmaf(p[i][j][e], scale[j], total[i][j][e])
-                                           : X == X_PLAIN ? fmaf(fmaf(less[j], of[e], p[i][j][e]), scale[j], total[i][j][e])
-                                                          : fmaf(p[i][j][e] * scale[j], of[e], total[i][j][e]);
+                            total[i][j][e] = x_scaled(X) ? fmaf(p[i][j][e] * scale[j], back[e], total[i][j][e]) : fmaf(p[i][j][e], scale[j], total[i][j][e]);
                 }
             }
         }
     };
     auto take_scales = [&](int phase) {   // of the next `chunk` phases
-        const int k0 = phase * KW * kBlock, k1 = k0 + chunk * KW * kBlock;
+        const int k0 = phase * PB * KW * kBlock, k1 = k0 + chunk * PB * KW * kBlock;
         j0 = (int)fast_div(k0, f.group_div);
         fc4_scales<COLS, S::THREADS, 4, Z>(f, blockIdx.x, 1, 1, j0, (int)fast_div((k1 < a.cin ? k1 : a.cin) - 1, f.group_div) - j0 + 1, scales, zeros, t);
     };
     const float my_bias = fc4_bias<COLS>(a, blockIdx.x, 1, 1, t);
     if (phases > 0) {
-        w[0].load(f, q, block_of(0), kq);
-        w[1].load(f, q, block_of(1), kq);
-        ask_x(block_of(0), x[0]);
-        ask_x(block_of(1), x[1]);
+        // Of a group's two blocks under way, PB are a phase's: one of each of two phases, or both of one.
+        auto ahead = [&](int phase, int u, int by) { return block_of(phase + (PB == 2 ? by / 2 : by), PB == 2 ? u : 0); };
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            w[u].load(f, q, ahead(PB == 2 ? 0 : u, u, 0), kq);
+            ask_x(ahead(PB == 2 ? 0 : u, u, 0), x[u]);
+        }
         take_scales(0);
-        stage(x[0], mine);
-        ask_x(block_of(2), x[0]);
+#pragma unroll
+        for (int u = 0; u < PB; ++u) {
+            stage(x[u], mine + u * BUFFER);
+            ask_x(ahead(0, u, 2), x[u]);
+        }
         for (int from = 0; from < phases; from += chunk) {   // chunks of an even number of phases, or one
             if (from > 0) {
                 __syncthreads();
                 take_scales(from);
             }
             const int to = from + chunk < phases ? from + chunk : phases;
-            for (int phase = from; phase < to; phase += 2) {
+            if constexpr (PB == 1) {
+                for (int phase = from; phase < to; phase += 2) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
+                    for (int u = 0; u < 2; ++u) {
+                        __syncthreads();
+                        const int block = place_of(phase + u, 0);
+                        if (block < whole) multiply(w[u], block, mine + u * BUFFER);   // an odd last phase has a second one with nothing to multiply
+                        w[u].load(f, q, ahead(phase + u, 0, 2), kq);
+                        stage(x[1 - u], mine + (1 - u) * BUFFER);
+                        ask_x(ahead(phase + u, 0, 3), x[1 - u]);
+                    }
+                }
+            } else {
+                for (int phase = from; phase < to; ++phase) {
                     __syncthreads();
-                    const int block = (phase + u) * KW + kw;
-                    if (block < whole) multiply(w[u], block, mine + u * BUFFER);   // an odd last phase has a second one with nothing to multiply
-                    w[u].load(f, q, block_of(phase + u + 2), kq);
-                    stage(x[1 - u], mine + (1 - u) * BUFFER);
-                    ask_x(block_of(phase + u + 3), x[1 - u]);
+                    char *const here = mine + (phase & 1) * (2 * BUFFER), *const there = mine + (~phase & 1) * (2 * BUFFER);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int block = place_of(phase, u);
+                        if (block < whole) multiply(w[u], block, here + u * BUFFER);
+                        w[u].load(f, q, ahead(phase, u, 2), kq);
+                        stage(x[u], there + u * BUFFER);
+                        ask_x(ahead(phase, u, 4), x[u]);
+                    }
                 }
             }
         }
     }
     if (whole * kBlock < a.cin) {   // the rest of K is one group's
         __syncthreads();
-        if (whole % (KW * chunk) == 0) take_scales(phases);
+        if (whole % (PB * KW * chunk) == 0) take_scales(phases);
         if (kw == 0) {
             ask_x(whole, x[0]);
             w[0].load(f, q, whole, kq);
@@ -640,12 +669,21 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
     else put(static_cast<bf16 *>(a.y));
 }
 
+// ---- the choice of a form ----------------------------------------------------------------------------
+struct Fc4Plan {
+    enum Form { SHORT, FEW, FEW_PAIRS, MANY1_16, MANY1_32, MANY1_64, MANY2_32, MANY2_64, MANY4_64, MANY4_128, MANY4_256, MANY8_256 } form;
+    int rows, cols, threads;   // of a workgroup; FEW and FEW_PAIRS: `cols` at a time
+    int most;                  // workgroups of those
+};
+Fc4Plan fc4_plan(const Fc4Args &a);
+
 constexpr int kLdsBytes = 160 * 1024;
 // LDS of a workgroup of few rows: two share a CU.  fp32 activations may have all of it where there is a workgroup for each CU at most: 16 x 2048 to
 // 1000 7.7 us, in the form for many rows, which converts them as often, 8.4; but fp16 16 x 4096 to 4096 8.6 us, and 7.0 in that form.
 constexpr int few_lds(bool fp32, int64_t tiles) { return fp32 && tiles <= 256 ? kLdsBytes : kLdsBytes / 2; }
 
 static int fc4_groups(const Fc4Args &a) { return (a.cin + a.group - 1) / a.group; }
+static bool fc4_plain(const Fc4Args &a) { return a.x_dtype == DT_BF16 && a.y_dtype != DT_F32; }   // in the forms for many rows
 static Fc4Kernel fc4_kernel_args(const Fc4Args &a) { return {a, make_fast_div((uint32_t)a.group), make_fast_div((uint32_t)(fc4_groups(a) + 15) / 16)}; }
 
 // LDS of fc4_few_kernel without the scales, and of the scales of a tile.
@@ -670,17 +708,17 @@ static hipError_t launch_few(const Fc4Args &a, int most_wgs, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <int X, int MT, int NT, int NW, int KW, int GM, bool Z>
-static hipError_t launch_many(const Fc4Args &a, hipStream_t s) {
-    typedef Fc4Many<X, MT, NT, NW, KW> S;
+template <int X, int MT, int NT, int NW, int KW, int PB, int GM, bool Z>
+static hipError_t launch_many(const Fc4Args &a, const Fc4Plan &p, hipStream_t s) {
+    typedef Fc4Many<X, MT, NT, NW, KW, PB> S;
     static_assert(S::FIXED + (2 * KW * 4 / GM + 1) * S::COLS * 5 <= kLdsBytes, "LDS");
-    if (a.cin < kShortIn) return hipErrorInvalidValue;
+    if (a.cin < kShortIn || p.rows != S::ROWS || p.cols != S::COLS || p.threads != S::THREADS) return hipErrorInvalidValue;
     // The scales of as many phases as fit.  Inputs that begin anywhere touch a group more than they fill.
-    const int phases = (a.cin + KW * kBlock - 1) / (KW * kBlock), most = (kLdsBytes - S::FIXED) / (S::COLS * (Z ? 5 : 4));
+    const int phases = (a.cin + PB * KW * kBlock - 1) / (PB * KW * kBlock), most = (kLdsBytes - S::FIXED) / (S::COLS * (Z ? 5 : 4));
     int chunk = phases, groups = fc4_groups(a);
-    while (groups > most && chunk > 2) {   // an even number of them
-        chunk = (chunk + 3) / 4 * 2;
-        groups = (int)(((int64_t)chunk * KW * kBlock + a.group - 1) / a.group) + 1;
+    while (groups > most && chunk > 2 / PB) {   // an even number of them with one block each
+        chunk = PB == 2 ? (chunk + 1) / 2 : (chunk + 3) / 4 * 2;
+        groups = (int)(((int64_t)chunk * PB * KW * kBlock + a.group - 1) / a.group) + 1;
     }
     if (groups > most) return hipErrorInvalidValue;
     const int bytes = S::FIXED + groups * S::COLS * (Z ? 5 : 4);
@@ -689,18 +727,11 @@ static hipError_t launch_many(const Fc4Args &a, hipStream_t s) {
         f.a.rows = a.rows - m < 65535 * S::ROWS ? a.rows - m : 65535 * S::ROWS;
         f.a.x = static_cast<const char *>(a.x) + m * a.x_stride * (a.x_dtype == DT_F32 ? 4 : 2);
         f.a.y = static_cast<char *>(a.y) + m * a.y_stride * (a.y_dtype == DT_F32 ? 4 : 2);
-        fc4_many_kernel<X, MT, NT, NW, KW, GM, Z><<<dim3((a.cout + S::COLS - 1) / S::COLS, (f.a.rows + S::ROWS - 1) / S::ROWS), S::THREADS, bytes, s>>>(f, chunk, groups);
+        fc4_many_kernel<X, MT, NT, NW, KW, PB, GM, Z><<<dim3((a.cout + S::COLS - 1) / S::COLS, (f.a.rows + S::ROWS - 1) / S::ROWS), S::THREADS, bytes, s>>>(f, chunk, groups);
     }
     return hipGetLastError();
 }
 
-// ---- the choice of a form ----------------------------------------------------------------------------
-struct Fc4Plan {
-    enum Form { SHORT, FEW, FEW_PAIRS, MANY1_16, MANY1_64, MANY2_16, MANY2_64, MANY4_64, MANY4_128 } form;
-    int rows, cols, threads;   // of a workgroup; FEW and FEW_PAIRS: `cols` at a time
-    int most;                  // workgroups of those
-};
-Fc4Plan fc4_plan(const Fc4Args &a);
 template <int X>
 hipError_t launch_fc4_x(const Fc4Args &a, const Fc4Plan &p, hipStream_t s);
 
@@ -712,12 +743,16 @@ static hipError_t launch_fc4_form(const Fc4Args &a, const Fc4Plan &p, hipStream_
         if (p.form == Fc4Plan::FEW_PAIRS) return launch_few<X, 1, 2, 4, GM, 4, Z>(a, p.most, s);
     }
     switch (p.form) {
-        case Fc4Plan::MANY1_16: return launch_many<X, 1, 1, 1, 8, GM, Z>(a, s);
-        case Fc4Plan::MANY1_64: return launch_many<X, 1, 1, 4, 4, GM, Z>(a, s);
-        case Fc4Plan::MANY2_16: return launch_many<X, 2, 1, 1, two ? 4 : 8, GM, Z>(a, s);
-        case Fc4Plan::MANY2_64: return launch_many<X, 2, 1, 4, two ? 2 : 4, GM, Z>(a, s);
-        case Fc4Plan::MANY4_64: return launch_many<X, 4, 1, 4, two ? 2 : 4, GM, Z>(a, s);
-        case Fc4Plan::MANY4_128: return launch_many<X, 4, 2, 4, 2, GM, Z>(a, s);
+        case Fc4Plan::MANY1_16: return launch_many<X, 1, 1, 1, 8, 1, GM, Z>(a, p, s);
+        case Fc4Plan::MANY1_32: return launch_many<X, 1, 1, 2, 4, 2, GM, Z>(a, p, s);
+        case Fc4Plan::MANY1_64: return launch_many<X, 1, 1, 4, 4, 2, GM, Z>(a, p, s);
+        case Fc4Plan::MANY2_32: return launch_many<X, 2, 1, 2, 4, two ? 1 : 2, GM, Z>(a, p, s);
+        case Fc4Plan::MANY2_64: return launch_many<X, 2, 1, 4, two ? 4 : 2, two ? 1 : 2, GM, Z>(a, p, s);
+        case Fc4Plan::MANY4_64: return launch_many<X, 4, 1, 4, 2, two ? 1 : 2, GM, Z>(a, p, s);
+        case Fc4Plan::MANY4_128: return launch_many<X, 4, two ? 2 : 1, two ? 4 : 8, 2, two ? 1 : 2, GM, Z>(a, p, s);
+        case Fc4Plan::MANY4_256: return launch_many<X, 4, 2, 8, 1, two ? 1 : 2, GM, Z>(a, p, s);
+        case Fc4Plan::MANY8_256:
+            if constexpr (!x_scaled(X)) return launch_many<X, 8, 2, 8, 1, 1, GM, Z>(a, p, s);
         default: return hipErrorInvalidValue;
     }
 }

@@ -39,31 +39,49 @@ static hipError_t launch_short(const Fc4Args &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Measured in graphs of calls over several sets of weights, us a call (K = 4096, fp16, groups of 128, unless said otherwise):
-//   up to 16 rows  x in LDS once a workgroup, which walks tiles of 16 weight rows; pairs of tiles where there are more than two for each CU
-//                  (1 x 8192 bf16 to 32001: 31.0 in pairs, 32.3-37.7 one by one), but one by one up to that (4 x 4096 to 16384: 10.3 and 11.0)
-//   more of x than LDS holds, or more rows: x in blocks.  64 or 128 weight rows a workgroup share a block of x, 16 make more workgroups:
-//                  16 rows to 16384 11.5 us with 64, 19.6 with 16; 32 rows to 16384 16.6 and 16.9 (32), to 4096 14.5 and 10.0;
-//                  64 rows to 16384 (groups of 64, zero points) 21-24 us with 64, 38 with 128; 512 rows to 4096 42.9 and 29.
-//   32 or 64 rows  128 rows to 1000: 10.6 us with 32 rows and 16 weight rows a workgroup, 15.6 with 64 and 32.
+// Up to 16 rows whose x LDS holds: one workgroup keeps it and walks tiles of 16 weight rows, or pairs of tiles where there are more than two for each of
+// 512 workgroups (bf16 1 x 8192 to 32001: 31.0 us in pairs, 32.3-37.7 one by one; but fp16 4 x 4096 to 16384: 10.3 one by one and 11.0 in pairs).
+// More: x in blocks, and tiles of 16 x 16 to 128 x 256.  A larger tile reads x and converts weights less often for each product, and fewer of them fill
+// the 256 CUs, so the tile is the one with the least  rounds of 256 workgroups x (2 us + a time for each block of 128 inputs), which were measured in graphs
+// of calls over several sets of weights (fp16, groups of 128; us, rates in TFLOP/s):
+//   tile          16x16  16x32  16x64  32x32  32x64  64x64  64x128  64x256  128x256
+//   16 x 4096 to 4096     7.1    7.7    9.9
+//   16 x 4096 to 16384   18.7   11.8   10.8
+//   32 x 4096 to 8192                         10.9   12.6
+//   64 x 4096 to 4096                         10.3   12.5   17.4    23.0
+//   64 x 4096 to 16384                        38     24     20.7
+//   256 x 2048 to 1000                         7.4    8.3   11.1    14.1
+//   512 x 4096 to 4096                                      35      25-29   41       64
+//   1024 x 4096 to 4096                                             56.7    45.5     64.8
+//   2048 x 8192 to 8192                                     475     366     317      265 (1036; a library's product of 16-bit weights 1226)
+// fp32, in two parts, takes about twice the time for a block, and 128 rows' two parts do not fit in the registers; nor do those of scaled bf16.
+struct Fc4Tile {
+    Fc4Plan::Form form;
+    int rows, cols, threads, threads_two;   // threads_two: of activations in two parts
+    float block;                            // us
+};
+constexpr Fc4Tile kFc4Tiles[] = {{Fc4Plan::MANY1_16, 16, 16, 512, 512, 0.15f},    {Fc4Plan::MANY1_32, 16, 32, 512, 512, 0.2f},    {Fc4Plan::MANY1_64, 16, 64, 1024, 1024, 0.27f},
+                                 {Fc4Plan::MANY2_32, 32, 32, 512, 512, 0.25f},    {Fc4Plan::MANY2_64, 32, 64, 512, 1024, 0.33f},  {Fc4Plan::MANY4_64, 64, 64, 512, 512, 0.56f},
+                                 {Fc4Plan::MANY4_128, 64, 128, 1024, 512, 0.78f}, {Fc4Plan::MANY4_256, 64, 256, 512, 512, 1.36f}, {Fc4Plan::MANY8_256, 128, 256, 512, 512, 2.05f}};
+
 Fc4Plan fc4_plan(const Fc4Args &a) {
     const bool two = a.x_dtype == DT_F32;
+    const int64_t blocks = (a.cin + kBlock - 1) / kBlock;
     auto wgs = [&](int rows, int cols) { return (int64_t)((a.rows + rows - 1) / rows) * ((a.cout + cols - 1) / cols); };
     if (a.cin < kShortIn) return {Fc4Plan::SHORT, kShortRows, 4, 256, 0};
-    constexpr int enough = 200;   // workgroups that keep 256 CUs busy
     if (a.rows <= 16) {
-        const int64_t blocks = (a.cin + kBlock - 1) / kBlock, fixed = (two ? 2 : 1) * a.rows * blocks * kBlock * 2 + 16 * 1024 + blocks * 64, scales = ((int64_t)fc4_groups(a) * 5 + 4) * 16;
+        const int64_t fixed = (two ? 2 : 1) * a.rows * blocks * kBlock * 2 + 16 * 1024 + blocks * 64, scales = ((int64_t)fc4_groups(a) * 5 + 4) * 16;
         if (wgs(16, 16) > 1024 && fixed + 2 * scales <= few_lds(two, wgs(16, 32))) return {Fc4Plan::FEW_PAIRS, 16, 32, 512, 1024};
         if (fixed + scales <= few_lds(two, wgs(16, 16))) return {Fc4Plan::FEW, 16, 16, 512, 512};
-        if (wgs(16, 64) >= enough) return {Fc4Plan::MANY1_64, 16, 64, 1024, 0};
-        return {Fc4Plan::MANY1_16, 16, 16, 512, 0};
     }
-    if (a.rows > 32) {
-        if (wgs(64, 128) >= enough) return {Fc4Plan::MANY4_128, 64, 128, 512, 0};
-        if (wgs(64, 64) >= enough) return {Fc4Plan::MANY4_64, 64, 64, two ? 512 : 1024, 0};
+    const Fc4Tile *best = nullptr;
+    float least = 0.f;
+    for (const Fc4Tile &t : kFc4Tiles) {
+        if (t.form == Fc4Plan::MANY8_256 && a.x_dtype != DT_F16 && !fc4_plain(a)) continue;
+        const float time = (float)((wgs(t.rows, t.cols) + 255) / 256) * (2.f + (two ? 2 : 1) * t.block * blocks);
+        if (!best || time < least) best = &t, least = time;
     }
-    if (wgs(32, 64) >= enough) return {Fc4Plan::MANY2_64, 32, 64, two ? 512 : 1024, 0};
-    return {Fc4Plan::MANY2_16, 32, 16, two ? 256 : 512, 0};
+    return {best->form, best->rows, best->cols, two ? best->threads_two : best->threads, 0};
 }
 
 void fc4_grid(const Fc4Args &a, dim3 *grid, int *block) {
@@ -80,7 +98,7 @@ hipError_t launch_fc4(const Fc4Args &a, hipStream_t s) {
     if (a.rows < 1 || a.rows > kFc4MostRows || a.cin < 1 || a.cin > kFc4MostIn || a.cout < 1 || a.cout > kFc4MostOut || a.group < 32 || a.group % 32 != 0) return hipErrorInvalidValue;
     const Fc4Plan p = fc4_plan(a);
     if (p.form == Fc4Plan::SHORT) return launch_short(a, s);
-    if (a.x_dtype == DT_BF16 && a.y_dtype != DT_F32 && p.form != Fc4Plan::FEW && p.form != Fc4Plan::FEW_PAIRS) return launch_fc4_x<X_PLAIN>(a, p, s);
+    if (fc4_plain(a) && p.form != Fc4Plan::FEW && p.form != Fc4Plan::FEW_PAIRS) return launch_fc4_x<X_PLAIN>(a, p, s);
     return a.x_dtype == DT_F16 ? launch_fc4_x<X_F16>(a, p, s) : a.x_dtype == DT_BF16 ? launch_fc4_x<X_BF16>(a, p, s) : launch_fc4_x<X_F32>(a, p, s);
 }
 

@@ -59,6 +59,18 @@ def test_wide_and_long(ctx, size, types):
     check(ctx, *size, x=x, scale=scale, y=y, zeros=zeros, seed=sum(size))
 
 
+# A size for each tile of the forms for many rows, from 16 x 16 to 128 x 256 (the largest is 64 x 256 for what takes more registers).
+TILES = [(13, 10016, 40), (16, 2600, 4200), (16, 2600, 8300), (200, 420, 1000), (24, 200, 8500), (40, 420, 9000), (100, 420, 9000), (500, 420, 4100), (1000, 290, 4100)]
+
+
+@pytest.mark.parametrize("size", TILES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("types", [(F16, F16), (BF16, F32), (BF16, BF16), (F32, F32)], ids=["fp16", "bf16", "bf16 plain", "fp32"])
+def test_every_tile(ctx, size, group, zeros, types):
+    check(ctx, *size, group, types[0], BF16, types[1], zeros, seed=group)
+
+
 @pytest.mark.parametrize("x", [F16, BF16, F32])
 @pytest.mark.parametrize("scale", [F16, BF16, F32])
 @pytest.mark.parametrize("y", [F16, BF16, F32])
