@@ -284,8 +284,11 @@ int32_t cw_profile_get(cw_ctx *ctx, int32_t model_id, int32_t batch, cw_profile 
 
 /* Fully connected layer over 4-bit weights with group scales:
  *   y[m][n] = bias[n] + sum over k < cin of x[m][k] * (q[n][k] - zero[n][k / group]) * scale[n][k / group]
- * Products and sums are exact to fp32; the result is rounded once, to y's type.  Activations of 16 bits are taken as they are;
- * fp32 ones keep 22 bits of mantissa or more of a row's largest ones (what is below 2^-36 of the row's largest is lost). */
+ * Products are exact, sums are fp32 and the result is rounded once, to y's type.  fp16 activations are taken as they are; bf16 and
+ * fp32 ones as fp16 numbers scaled by a power of two for every 128 inputs of a row, fp32 in two parts: what is below 2^-38 of the
+ * largest of these 128 is lost, and fp32 keeps 22 bits of the others.  Where y has 16 bits and the rows are more than a few, bf16 ones
+ * are taken as they are, times 16 + q, and (16 + zero) times their sum is taken off: a group's sum then loses up to four of fp32's 24
+ * bits, and activations beyond 2^115 may overflow.  A NaN or an infinity of x stays in its row, one of scale or bias in its column. */
 typedef struct {
     const void *x;          /* [rows][cin], x_dtype */
     const uint8_t *q;       /* [cout][ceil(cin / 2)]: k even in the low, k odd in the high four bits */
@@ -309,7 +312,8 @@ int32_t cw_fc4(cw_ctx *ctx, const cw_fc4_args *args, void *stream);
  *   top_id, top_logp  the `top` likeliest classes, equal ones by index, and d - ln S; behind the last class that is not masked -1
  *            and -inf
  * A row with nothing but -inf: logp -inf, entropy 0, no top classes.  A row with a NaN or +inf: logp, entropy and
- * top_logp NaN, rank and top_id -1 (a negative `given` has logp 0 all the same).  The order is that of the logits as they are stored; sums are fp32.
+ * top_logp NaN, rank and top_id -1 (a negative `given` has logp 0 all the same).  The order is that of the logits as they are stored; sums are
+ * fp32, and of two logits whose difference leaves fp32's range the smaller has no probability.
  * With few rows a row is shared by several workgroups, which meet in `workspace`: its first CW_ANSWER_COUNTERS bytes must be
  * zero before the first call and are zero behind every call.  Calls that may overlap in time need a workspace each.
  * Without one (NULL, or smaller than cw_answer_workspace_bytes) a workgroup takes a row; the answers are the same but for

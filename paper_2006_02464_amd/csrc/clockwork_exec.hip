@@ -1445,7 +1445,7 @@ int32_t cw_answer(cw_ctx *c, const cw_answer_args *r, void *stream) {
     if (!r) return set_err(c, CW_ERR_INVALID, "null arguments");
     if (!element_type(r->dtype)) return set_err(c, CW_ERR_INVALID, "bad dtype");
     if (r->rows < 0 || r->classes < 1) return set_err(c, CW_ERR_INVALID, "bad size");
-    if (r->classes > kAnswerMostClasses) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
+    if (r->classes > kAnswerMostClasses || r->rows > kAnswerMostRows) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
     const int32_t rc = answer_checks(c, r->top, r->scale);
     if (rc != CW_OK) return rc;
     if (r->stride < 0) return set_err(c, CW_ERR_INVALID, "bad stride");

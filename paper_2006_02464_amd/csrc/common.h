@@ -346,7 +346,7 @@ struct AnswerArgs {
     DType dtype;
     float scale;
 };
-constexpr int kAnswerMostTop = 64, kAnswerMostClasses = 1 << 24;
+constexpr int kAnswerMostTop = 64, kAnswerMostClasses = 1 << 24, kAnswerMostRows = 1 << 23;
 
 // Tile shapes the conv kernel is instantiated for (fixed at plan time per layer).
 // (pixels x channels per workgroup; "wN" = N waves when not 4, each wave then owning 64x64;

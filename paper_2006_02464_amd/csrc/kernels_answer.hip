@@ -1,4 +1,5 @@
 // The answer of a row of logits: log probability and rank of a given class, entropy, the likeliest classes (cw_answer has the definitions).
+#include <cfloat>
 #include <cmath>
 
 #include "conv_common.h"
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
     const T *x = static_cast<const T *>(a.x) + row * a.stride;
     const int segments = (a.classes + kSegment - 1) / kSegment;
     const int seg0 = (int)((int64_t)segments * part / parts), seg1 = (int)((int64_t)segments * (part + 1) / parts);
-    const float c2 = a.scale * 1.44269504f;
+    const float c2 = fminf(a.scale * 1.44269504f, FLT_MAX);   // 0 times infinity would be no number
     int g = -1;
     bool inside = false;
     float xg = INFINITY;
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
 size_t answer_workspace_bytes() { return kCounterSlots * 4 + (size_t)kRecords * kRecordBytes; }
 
 hipError_t launch_answer(const AnswerArgs &a, hipStream_t s) {
-    if (a.rows < 1 || a.classes < 1 || a.classes > kAnswerMostClasses || a.top < 0 || a.top > kAnswerMostTop || (a.top > 0 && (!a.top_id || !a.top_logp))) return hipErrorInvalidValue;
+    if (a.rows < 1 || a.rows > kAnswerMostRows || a.classes < 1 || a.classes > kAnswerMostClasses || a.top < 0 || a.top > kAnswerMostTop || (a.top > 0 && (!a.top_id || !a.top_logp))) return hipErrorInvalidValue;
     const int segments = (a.classes + kSegment - 1) / kSegment;
     int parts = 1;
     if (a.workspace && a.rows <= kCounterSlots) {

@@ -199,6 +199,14 @@ def test_same_bits_every_time_on_two_streams_at_once_and_replayed(ctx, rows, cla
         assert all(torch.equal(out[k], want[k]) for k in want)
 
 
+@pytest.mark.parametrize("rows, classes", [(2, 300), (3, 20011)])
+@pytest.mark.parametrize("scale", [1e-38, 3.4e38])
+def test_scales_near_the_ends_of_the_range(ctx, rows, classes, scale):
+    x = torch.full((rows, classes), -2.0)
+    x[:, 7:classes:40] = 1.5
+    check(ctx, x, torch.full((rows,), 47, dtype=torch.int32), 5, scale)
+
+
 @pytest.mark.parametrize("rows, cin, classes, x, z", [(1, 512, 1000, F32, F32), (5, 1024, 20011, F16, F16), (64, 640, 3001, BF16, F32)])
 def test_from_features_to_the_answer(ctx, rows, cin, classes, x, z):
     """The end of a network as it is used: 4-bit layer, then the answer over its logits, on one stream and as one graph."""

@@ -86,6 +86,17 @@ def test_activations_of_many_magnitudes(ctx, x, size):
     check(ctx, *size, x=x, scale=F32, y=F32, seed=11, spread=True)
 
 
+@pytest.mark.parametrize("x, y, power", [(BF16, BF16, 112), (BF16, F32, 120), (F32, F32, 120), (BF16, BF16, -110), (F32, F32, -110)])
+@pytest.mark.parametrize("rows", [3, 70])
+def test_activations_near_the_ends_of_the_range(ctx, x, y, power, rows):
+    d = fc4_data(rows, 392, 40, 64, x, F32, True, seed=12)
+    d["x"] = d["x"] * 2.0 ** power
+    d["bias"] = d["bias"] * 2.0 ** power
+    out = torch.full((rows, 40), float("nan"), dtype=y, device="cuda")
+    call(ctx, on_gpu(d), out)
+    assert_fc4(out.cpu(), *fc4_ref(d))
+
+
 @pytest.mark.parametrize("x", [F16, BF16, F32])
 @pytest.mark.parametrize("rows", [1, 5, 20, 130])
 @pytest.mark.parametrize("gap", [1, 8, 16])

@@ -60,7 +60,7 @@ def test_fc4_checks_let_through(ctx, change):
 @pytest.mark.parametrize("change, status", [
     (dict(logits=None), cw.CW_ERR_INVALID), (dict(given=None), cw.CW_ERR_INVALID), (dict(given=None, logp=None), cw.CW_ERR_INVALID), (dict(top_id=None), cw.CW_ERR_INVALID),
     (dict(top_logp=None), cw.CW_ERR_INVALID), (dict(top=0), cw.CW_ERR_INVALID), (dict(top=-1), cw.CW_ERR_UNSUPPORTED), (dict(top=65), cw.CW_ERR_UNSUPPORTED),
-    (dict(rows=-1), cw.CW_ERR_INVALID), (dict(classes=0), cw.CW_ERR_INVALID), (dict(classes=(1 << 24) + 1), cw.CW_ERR_UNSUPPORTED), (dict(dtype=3), cw.CW_ERR_INVALID),
+    (dict(rows=-1), cw.CW_ERR_INVALID), (dict(classes=0), cw.CW_ERR_INVALID), (dict(classes=(1 << 24) + 1), cw.CW_ERR_UNSUPPORTED), (dict(rows=(1 << 23) + 1), cw.CW_ERR_UNSUPPORTED), (dict(dtype=3), cw.CW_ERR_INVALID),
     (dict(scale=0.0), cw.CW_ERR_INVALID), (dict(scale=-1.0), cw.CW_ERR_INVALID), (dict(scale=float("inf")), cw.CW_ERR_INVALID), (dict(scale=float("nan")), cw.CW_ERR_INVALID),
     (dict(stride=-1), cw.CW_ERR_INVALID), (dict(logits=4098), cw.CW_ERR_INVALID), (dict(logits=4097, dtype=0), cw.CW_ERR_INVALID), (dict(given=4098), cw.CW_ERR_INVALID),
     (dict(logp=4098), cw.CW_ERR_INVALID), (dict(rank=4098), cw.CW_ERR_INVALID), (dict(entropy=4098), cw.CW_ERR_INVALID), (dict(top_id=4098), cw.CW_ERR_INVALID),
