@@ -185,16 +185,13 @@ struct Fc4X {
         if (X == X_F32) return __builtin_bit_cast(float, word);
         return __builtin_bit_cast(float, i % 2 ? raw[0][i / 2] & 0xffff0000u : raw[0][i / 2] << 16);   // bf16
     }
-    // The largest magnitude, as the bits of its exponent and below (of a NaN: larger than any number's).
+    // The largest magnitude, as the bits of its exponent and below.
     __device__ unsigned most() const {
-        if (X == X_F32) {
-            unsigned m = 0;
+        if (X == X_F32) {   // without the sign, which costs this instruction nothing; a NaN beside a number is passed over and stays one in its product
+            float m = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const unsigned v = raw[i / 4 % WORDS][i % 4] & 0x7fffffffu;
-                m = m > v ? m : v;
-            }
-            return m;
+            for (int i = 0; i < 8; i += 2) asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(m) : "v"(m), "v"(value(i)), "v"(value(i + 1)));
+            return __builtin_bit_cast(unsigned, m);
         }
         typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
         u16x2 m = __builtin_bit_cast(u16x2, raw[0][0] & 0x7fff7fffu);
@@ -229,10 +226,13 @@ struct Fc4X {
                 hi[2 * i] = (f16)p[0];
                 hi[2 * i + 1] = (f16)p[1];
             } else {
-                hi[2 * i] = (f16)v0;
-                hi[2 * i + 1] = (f16)v1;
-                lo[2 * i] = (f16)fmaf((float)hi[2 * i], -1.f, v0);
-                lo[2 * i + 1] = (f16)fmaf((float)hi[2 * i + 1], -1.f, v1);
+                typedef float f32x2 __attribute__((ext_vector_type(2)));
+                f16x2 p = __builtin_convertvector((f32x2{v0, v1}), f16x2);
+                asm("" : "+v"(p));   // products and halves are made once: again for each use they would be mixed fmas, which take longer than two instructions
+                hi[2 * i] = p[0];
+                hi[2 * i + 1] = p[1];
+                lo[2 * i] = (f16)fmaf((float)p[0], -1.f, v0);
+                lo[2 * i + 1] = (f16)fmaf((float)p[1], -1.f, v1);
             }
         }
     }
@@ -754,7 +754,7 @@ static hipError_t launch_fc4_form(const Fc4Args &a, const Fc4Plan &p, hipStream_
         case Fc4Plan::MANY2_32: return launch_many<X, 2, 1, 2, 4, two ? 1 : 2, GM, Z>(a, p, s);
         case Fc4Plan::MANY2_64: return launch_many<X, 2, 1, 4, two ? 4 : 2, two ? 1 : 2, GM, Z>(a, p, s);
         case Fc4Plan::MANY4_64: return launch_many<X, 4, 1, 4, 2, two ? 1 : 2, GM, Z>(a, p, s);
-        case Fc4Plan::MANY4_128: return launch_many<X, 4, two ? 2 : 1, two ? 4 : 8, 2, two ? 1 : 2, GM, Z>(a, p, s);
+        case Fc4Plan::MANY4_128: return launch_many<X, 4, 1, 8, 2, two ? 1 : 2, GM, Z>(a, p, s);
         case Fc4Plan::MANY4_256: return launch_many<X, 4, 2, 8, 1, two ? 1 : 2, GM, Z>(a, p, s);
         case Fc4Plan::MANY8_256:
             if constexpr (!x_scaled(X)) return launch_many<X, 8, 2, 8, 1, 1, GM, Z>(a, p, s);

@@ -62,7 +62,7 @@ struct Fc4Tile {
 };
 constexpr Fc4Tile kFc4Tiles[] = {{Fc4Plan::MANY1_16, 16, 16, 512, 512, 0.15f},    {Fc4Plan::MANY1_32, 16, 32, 512, 512, 0.2f},    {Fc4Plan::MANY1_64, 16, 64, 1024, 1024, 0.27f},
                                  {Fc4Plan::MANY2_32, 32, 32, 512, 512, 0.25f},    {Fc4Plan::MANY2_64, 32, 64, 512, 1024, 0.33f},  {Fc4Plan::MANY4_64, 64, 64, 512, 512, 0.56f},
-                                 {Fc4Plan::MANY4_128, 64, 128, 1024, 512, 0.78f}, {Fc4Plan::MANY4_256, 64, 256, 512, 512, 1.36f}, {Fc4Plan::MANY8_256, 128, 256, 512, 512, 2.05f}};
+                                 {Fc4Plan::MANY4_128, 64, 128, 1024, 1024, 0.78f}, {Fc4Plan::MANY4_256, 64, 256, 512, 512, 1.36f}, {Fc4Plan::MANY8_256, 128, 256, 512, 512, 2.05f}};
 
 Fc4Plan fc4_plan(const Fc4Args &a) {
     const bool two = a.x_dtype == DT_F32;
