@@ -6,18 +6,18 @@
 
 namespace cw {
 
-// One pass.  A workgroup takes a row, or a run of its segments, 8192 logits at a time in registers, 16 bytes a load.  Every thread keeps a
+// One pass.  A workgroup takes a row, or a run of its segments, 32 logits a thread at a time in registers, 16 bytes a load.  Every thread keeps a
 // maximum m, S = sum 2^d and T = sum d 2^d with d = (x - m) scale / ln 2 of its own (a new maximum rescales both once a segment), the
 // threads meet at the end.  For the top classes a segment gives those of its logits that can still be among them to a list in LDS.
-constexpr int kThreads = 256, kEach = 32, kSegment = kThreads * kEach;
+constexpr int kEach = 32, kThreads = 256, kFewest = 64, kRowsOfAWave = 512;
+constexpr int kSegment = kThreads * kEach;
 constexpr int kParts = 32;                         // workgroups a row at most
 constexpr int kRecords = 1024;                     // of rows that are shared
 constexpr int kRecordBytes = 16 + 8 * kAnswerMostTop;
 constexpr int kCounterSlots = 256;                 // rows that can be shared
-// Logits above the k-th largest of the threads' maxima lie with fewer than k threads; those equal to it are taken 2048 at a time.
-constexpr int kList = kAnswerMostTop + (kAnswerMostTop - 1) * kEach + kAnswerMostTop + kThreads * 8;
-
-constexpr int kFewThreads = (kList - kAnswerMostTop) / kEach;   // whose logits the list holds, all of them
+// Logits above the k-th largest of the threads' maxima lie with fewer than k threads; those equal to it are taken eight a thread at a time.
+constexpr int list_keys(int threads) { return kAnswerMostTop + (kAnswerMostTop - 1) * kEach + kAnswerMostTop + threads * 8; }
+constexpr int few_threads(int threads) { return (list_keys(threads) - kAnswerMostTop) / kEach; }   // whose logits the list holds, all of them
 constexpr int kPad = 8;   // keys that first_of reads at a time
 
 template <typename T>
@@ -68,21 +68,24 @@ __device__ static inline Soft meet(const Soft &v, float c2) {
     return {m, wave_all(v.s * e, plus), wave_all((v.t + v.s * d) * e, plus)};
 }
 
+template <int THREADS>
 struct AnswerLds {
-    __attribute__((aligned(16))) uint64_t list[kList + kPad];
+    static constexpr int WAVES = THREADS / 64, KEYS = THREADS == kFewest ? kFewest * kEach : list_keys(THREADS);   // of a wave's only segment no more can be listed
+    __attribute__((aligned(16))) uint64_t list[KEYS + kPad];
     uint64_t best[kAnswerMostTop];
-    unsigned order[2][kThreads];
-    float m[4], s[4], t[4];
-    int rank[4];
+    unsigned order[2][THREADS];
+    float m[WAVES], s[WAVES], t[WAVES];
+    int rank[WAVES];
     int n, last;
 };
 
 // The k first of list[0..n) in order; returns how many there are.  All threads, behind a barrier behind the last write.
-__device__ static inline int first_of(AnswerLds &l, int n, int k) {
+template <int THREADS>
+__device__ static inline int first_of(AnswerLds<THREADS> &l, int n, int k) {
     const int t = threadIdx.x;
     if (t < kPad) l.list[n + t] = 0;
     __syncthreads();
-    for (int at = t; at < n; at += kThreads) {
+    for (int at = t; at < n; at += THREADS) {
         const uint64_t mine = l.list[at];
         int rank = 0;
         for (int o = 0; o < n; o += kPad) {
@@ -100,22 +103,26 @@ __device__ static inline int first_of(AnswerLds &l, int n, int k) {
     return have;
 }
 
-// A number that at least k of the 256 orders reach, or `low` where fewer are above it; `many`: how many reach it, or are above `low`.  A wave by itself.
-// Cheapest the k-th largest of the largest of 64 groups of four, or of 16 groups of sixteen; where the threads that reach that are too many for the list, the
+// A number that at least k of the threads' orders reach, or `low` where fewer are above it; `many`: how many reach it, or are above `low`.  A wave by itself.
+// Cheapest the k-th largest of the largest of 64 groups, or of 16; where the threads that reach that are too many for the list, the
 // k-th largest order itself, bit by bit.
+template <int THREADS>
 __device__ static inline unsigned kth_of(const unsigned *order, int k, int lane, unsigned low, int &many) {
-    unsigned o[4];
+    constexpr int EACH = THREADS / 64;
+    unsigned o[EACH];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = order[i * 64 + lane];
+    for (int i = 0; i < EACH; ++i) o[i] = order[i * 64 + lane];
     auto reach = [&](unsigned q) {
         int c = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c += __popcll(__ballot(o[i] >= q));
+        for (int i = 0; i < EACH; ++i) c += __popcll(__ballot(o[i] >= q));
         return c;
     };
     auto larger = [](unsigned p, unsigned q) { return p > q ? p : q; };
     auto smaller = [](unsigned p, unsigned q) { return p < q ? p : q; };
-    unsigned g = larger(larger(o[0], o[1]), larger(o[2], o[3]));
+    unsigned g = o[0];
+#pragma unroll
+    for (int i = 1; i < EACH; ++i) g = larger(g, o[i]);
     int above = 0;   // groups above this lane's
     if (k <= 16) {
         g = larger(g, (unsigned)__builtin_amdgcn_update_dpp(0, (int)g, 0xB1, 0xf, 0xf, false));   // of the four lanes
@@ -129,7 +136,7 @@ __device__ static inline unsigned kth_of(const unsigned *order, int k, int lane,
     const unsigned kth = wave_all(above < k ? g : 0xffffffffu, smaller);
     unsigned tau = kth > low ? kth : low;
     many = reach(tau + (tau == low));
-    if (many <= kFewThreads) return tau;
+    if (many <= few_threads(THREADS)) return tau;
     if (reach(low + 1) < k) return low;
     tau = 0;
     for (int bit = 31; bit >= 0; --bit) {
@@ -141,14 +148,15 @@ __device__ static inline unsigned kth_of(const unsigned *order, int k, int lane,
     return tau;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, int parts) {
-    constexpr int N = Vec<T>::N, CHUNKS = kEach / N, CHUNK = kThreads * N;
-    __shared__ AnswerLds l;
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void answer_kernel(const AnswerArgs a, int parts) {
+    constexpr int N = Vec<T>::N, CHUNKS = kEach / N, CHUNK = THREADS * N, SEGMENT = THREADS * kEach;
+    typedef T TN __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    __shared__ AnswerLds<THREADS> l;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int row = blockIdx.x / parts, part = blockIdx.x - row * parts, k = a.top;
     const T *x = static_cast<const T *>(a.x) + row * a.stride;
-    const int segments = (a.classes + kSegment - 1) / kSegment;
+    const int segments = (a.classes + SEGMENT - 1) / SEGMENT;
     const int seg0 = (int)((int64_t)segments * part / parts), seg1 = (int)((int64_t)segments * (part + 1) / parts);
     const float c2 = fminf(a.scale * 1.44269504f, FLT_MAX);   // 0 times infinity would be no number
     int g = -1;
@@ -159,26 +167,62 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
     int before = 0;       // logits that come before the given one
     int have = 0;         // classes in the list, the first `have` of it in order
     float bar = -INFINITY;   // the k-th of them: later ones have to be larger
-    for (int seg = seg0; seg < seg1; ++seg) {
-        float v[kEach];
-        const int base = seg * kSegment, count = a.classes - base < kSegment ? a.classes - base : kSegment;
+    auto look_up = [&]() {   // behind the first logits' loads: these two wait for one another
+        if (!a.given) return;
+        g = a.given[row];
+        inside = g >= 0 && g < a.classes;
+        if (inside) xg = (float)x[g];
+    };
+    // Of 16 bits the next segment's logits are under way beside this one's 32 numbers (2000 x 20000, five top classes: 36.5 -> 33.9 us; 946 x 69207, none:
+    // 44 -> 40); of fp32 they take registers from the other waves (860 x 23898: 32.1 -> 34.7).
+    constexpr bool AHEAD = sizeof(T) == 2;
+    TN raw[CHUNKS];
+    auto fetch = [&](int seg) {
+        const T *from = x + (int64_t)seg * SEGMENT;
+        const int count = a.classes - seg * SEGMENT;
+        if (count >= SEGMENT) {
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j) raw[j] = *reinterpret_cast<const TN *>(from + j * CHUNK + t * N);
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < CHUNKS; ++j) {
             const int at = j * CHUNK + t * N;
             if (at + N <= count) {
-                typedef T TN __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-                const TN raw = *reinterpret_cast<const TN *>(x + base + at);
-#pragma unroll
-                for (int e = 0; e < N; ++e) v[j * N + e] = (float)raw[e];
+                raw[j] = *reinterpret_cast<const TN *>(from + at);
             } else {
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[j * N + e] = at + e < count ? (float)x[base + at + e] : -INFINITY;
+                for (int e = 0; e < N; ++e) raw[j][e] = at + e < count ? from[at + e] : (T)-INFINITY;
             }
         }
-        if (seg == seg0 && a.given) {   // behind the first logits' loads: these two wait for one another
-            g = a.given[row];
-            inside = g >= 0 && g < a.classes;
-            if (inside) xg = (float)x[g];
+    };
+    if constexpr (AHEAD) {
+        fetch(seg0);
+        look_up();
+    }
+    for (int seg = seg0; seg < seg1; ++seg) {
+        float v[kEach];
+        const int base = seg * SEGMENT, count = a.classes - base < SEGMENT ? a.classes - base : SEGMENT;
+        if constexpr (AHEAD) {
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j)
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[j * N + e] = (float)raw[j][e];
+            if (seg + 1 < seg1) fetch(seg + 1);
+        } else {
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j) {
+                const int at = j * CHUNK + t * N;
+                if (at + N <= count) {
+                    const TN now = *reinterpret_cast<const TN *>(x + base + at);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) v[j * N + e] = (float)now[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) v[j * N + e] = at + e < count ? (float)x[base + at + e] : -INFINITY;
+                }
+            }
+            if (seg == seg0) look_up();
         }
         float most = -INFINITY;
 #pragma unroll
@@ -229,8 +273,8 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
             if (t == 0) l.n = have;
             __syncthreads();
             int many = 0;
-            const unsigned low = order_of(bar), tau = kth_of(order, k, lane, low, many);
-            const bool equal = tau != low, all_equal = equal && many <= kFewThreads;   // then those equal to it too, as far as they are needed
+            const unsigned low = order_of(bar), tau = kth_of<THREADS>(order, k, lane, low, many);
+            const bool equal = tau != low, all_equal = equal && many <= few_threads(THREADS);   // then those equal to it too, as far as they are needed
             const float from = equal ? of_order(tau) : bar;
             auto put = [&](float value, int i) { l.list[atomicAdd(&l.n, 1)] = key_of(value, base + i); };
             if (most > from || (all_equal && most == from)) {
@@ -265,10 +309,13 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
     const auto plus = [](auto p, auto q) { return p + q; };
     soft = meet(soft, c2);
     before = wave_all(before, plus);
-    if (lane == 0) { l.m[wave] = soft.m; l.s[wave] = soft.s; l.t[wave] = soft.t; l.rank[wave] = before; }
-    __syncthreads();
-    Soft all = join(join({l.m[0], l.s[0], l.t[0]}, {l.m[1], l.s[1], l.t[1]}, c2), join({l.m[2], l.s[2], l.t[2]}, {l.m[3], l.s[3], l.t[3]}, c2), c2);
-    before = l.rank[0] + l.rank[1] + l.rank[2] + l.rank[3];
+    Soft all = soft;
+    if constexpr (THREADS == 256) {
+        if (lane == 0) { l.m[wave] = soft.m; l.s[wave] = soft.s; l.t[wave] = soft.t; l.rank[wave] = before; }
+        __syncthreads();
+        all = join(join({l.m[0], l.s[0], l.t[0]}, {l.m[1], l.s[1], l.t[1]}, c2), join({l.m[2], l.s[2], l.t[2]}, {l.m[3], l.s[3], l.t[3]}, c2), c2);
+        before = l.rank[0] + l.rank[1] + l.rank[2] + l.rank[3];
+    }
 
     if (parts > 1) {
         // This part's record to memory, past the XCD's own L2; the last workgroup of the row to arrive joins them, in the parts' order.
@@ -283,7 +330,7 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
                 put(2, __builtin_bit_cast(int, all.t));
                 put(3, before);
             }
-            for (int i = t; i < k; i += kThreads) {
+            for (int i = t; i < k; i += THREADS) {
                 const uint64_t key = i < have ? l.list[i] : 0;
                 put(4 + 2 * i, (int)(unsigned)key);
                 put(5 + 2 * i, (int)(unsigned)(key >> 32));
@@ -311,12 +358,12 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
         all = meet(one, c2);
         __syncthreads();
         if (k > 0) {
-            constexpr int EACH = kParts * kAnswerMostTop / kThreads;
+            constexpr int EACH = kParts * kAnswerMostTop / THREADS;
             uint64_t key[EACH], most = 0;
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
                 key[i] = 0;
-                const int at = i * kThreads + t;
+                const int at = i * THREADS + t;
                 if (at < parts * k) {
                     const int p = at / k, j = at - p * k;
                     key[i] = (uint64_t)(unsigned)get(p, 5 + 2 * j) << 32 | (unsigned)get(p, 4 + 2 * j);
@@ -326,7 +373,7 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
             l.order[0][t] = (unsigned)(most >> 32);
             __syncthreads();
             int many;
-            const unsigned tau = kth_of(l.order[0], k, lane, 0, many);
+            const unsigned tau = kth_of<THREADS>(l.order[0], k, lane, 0, many);
             if (most)
 #pragma unroll
                 for (int i = 0; i < EACH; ++i)
@@ -354,6 +401,13 @@ __global__ __launch_bounds__(kThreads) void answer_kernel(const AnswerArgs a, in
     }
 }
 
+template <int THREADS>
+static void launch_answer_threads(const AnswerArgs &a, dim3 grid, int parts, hipStream_t s) {
+    if (a.dtype == DT_F32) answer_kernel<float, THREADS><<<grid, THREADS, 0, s>>>(a, parts);
+    else if (a.dtype == DT_F16) answer_kernel<f16, THREADS><<<grid, THREADS, 0, s>>>(a, parts);
+    else answer_kernel<bf16, THREADS><<<grid, THREADS, 0, s>>>(a, parts);
+}
+
 size_t answer_workspace_bytes() { return kCounterSlots * 4 + (size_t)kRecords * kRecordBytes; }
 
 hipError_t launch_answer(const AnswerArgs &a, hipStream_t s) {
@@ -366,9 +420,9 @@ hipError_t launch_answer(const AnswerArgs &a, hipStream_t s) {
         parts = parts < segments ? parts : segments;
     }
     const dim3 grid((unsigned)a.rows * parts);
-    if (a.dtype == DT_F32) answer_kernel<float><<<grid, kThreads, 0, s>>>(a, parts);
-    else if (a.dtype == DT_F16) answer_kernel<f16><<<grid, kThreads, 0, s>>>(a, parts);
-    else answer_kernel<bf16><<<grid, kThreads, 0, s>>>(a, parts);
+    // Short rows, more than two a CU, have a wave to themselves, and no barrier: 1802 x 37 14.3 -> 7.0 us, 1962 x 1741 16.4 -> 9.6; but one row of 1000 5.2 -> 5.5.
+    if (a.rows > kRowsOfAWave && a.classes <= kFewest * kEach) launch_answer_threads<kFewest>(a, grid, 1, s);
+    else launch_answer_threads<kThreads>(a, grid, parts, s);
     return hipGetLastError();
 }
 

@@ -1,7 +1,5 @@
 """cw_answer against 64 bits: sizes from one on, types, masks that leave little or nothing, ties, orders that selection finds hard,
 strides, streams and graphs, and the chain of cw_fc4 and cw_answer."""
-import math
-
 import pytest
 import torch
 
@@ -197,6 +195,23 @@ def test_same_bits_every_time_on_two_streams_at_once_and_replayed(ctx, rows, cla
         graphs[i % 2].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(out[k], want[k]) for k in want)
+
+
+# Many short rows: of a wave each.
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("rows, classes, top", [(513, 1, 1), (600, 37, 5), (520, 64, 64), (515, 1023, 17), (514, 2047, 64), (513, 2048, 20), (530, 2049, 9)])
+def test_many_short_rows(ctx, rows, classes, top, dtype):
+    x, given = logits(rows, classes, dtype, seed=rows + classes)
+    x[5] = x[5, 0]                                     # ties everywhere
+    x[6] = (x[6].float() * 0.3).round().to(dtype)      # and many
+    x[7] = -INF
+    x[8, 1:] = -INF
+    x[9, classes // 2] = NAN
+    x[10, classes // 3] = INF
+    x[11, ::2] = torch.finfo(dtype).min
+    x[12] = x[12].sort().values
+    given[13:17] = torch.tensor([-1, classes, classes - 1, 0], dtype=torch.int32)
+    check(ctx, x, given, top, 0.9)
 
 
 @pytest.mark.parametrize("rows, classes", [(2, 300), (3, 20011)])
