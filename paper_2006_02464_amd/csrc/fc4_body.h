@@ -684,7 +684,7 @@ Fc4Plan fc4_plan(const Fc4Args &a);
 
 constexpr int kLdsBytes = 160 * 1024;
 // LDS of a workgroup of few rows: two share a CU.  fp32 activations may have all of it where there is a workgroup for each CU at most: 16 x 2048 to
-// 1000 7.7 us, in the form for many rows, which converts them as often, 8.4; but fp16 16 x 4096 to 4096 8.6 us, and 7.0 in that form.
+// 1000 7.0 us, in the form for many rows, which converts them as often, 7.4; but fp16 16 x 4096 to 4096 8.6 us, and 7.1 in that form.
 constexpr int few_lds(bool fp32, int64_t tiles) { return fp32 && tiles <= 256 ? kLdsBytes : kLdsBytes / 2; }
 
 static int fc4_groups(const Fc4Args &a) { return (a.cin + a.group - 1) / a.group; }
@@ -745,7 +745,7 @@ static hipError_t launch_fc4_form(const Fc4Args &a, const Fc4Plan &p, hipStream_
     constexpr bool two = X == X_F32;   // operands in two parts: twice the LDS
     if constexpr (X != X_PLAIN) {
         if (p.form == Fc4Plan::FEW) return launch_few<X, 1, 1, 8, GM, 2, Z>(a, p.most, s);
-        if (p.form == Fc4Plan::FEW_PAIRS) return launch_few<X, 1, 2, 4, GM, 4, Z>(a, p.most, s);
+        if (p.form == Fc4Plan::FEW_PAIRS) return launch_few<X, 2, 1, 8, GM, 2, Z>(a, p.most, s);
     }
     switch (p.form) {
         case Fc4Plan::MANY1_16: return launch_many<X, 1, 1, 1, 8, 1, GM, Z>(a, p, s);

@@ -39,8 +39,9 @@ static hipError_t launch_short(const Fc4Args &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Up to 16 rows whose x LDS holds: one workgroup keeps it and walks tiles of 16 weight rows, or pairs of tiles where there are more than two for each of
-// 512 workgroups (bf16 1 x 8192 to 32001: 31.0 us in pairs, 32.3-37.7 one by one; but fp16 4 x 4096 to 16384: 10.3 one by one and 11.0 in pairs).
+// Up to 16 rows whose x LDS holds: one workgroup keeps it and walks tiles of 16 weight rows; pairs of tiles, twice the loads under way, where there are more
+// than two for each of 512 workgroups and they are long (us one by one and in pairs, 1 x 8192 bf16 to 32001: 36.1 and 32.4, 2 x 4096 fp16 to 60000: 36.5
+// and 33.3; but 6 x 1536 fp32 to 31051: 11.7 and 14.7, 8 x 2048 bf16 to 20000: 14.2 and 15.9).
 // More: x in blocks, and tiles of 16 x 16 to 128 x 256.  A larger tile reads x and converts weights less often for each product, and fewer of them fill
 // the 256 CUs, so the tile is the one with the least  rounds of 256 workgroups x (2 us + a time for each block of 128 inputs), which were measured in graphs
 // of calls over several sets of weights (fp16, groups of 128; us, rates in TFLOP/s):
@@ -71,7 +72,7 @@ Fc4Plan fc4_plan(const Fc4Args &a) {
     if (a.cin < kShortIn) return {Fc4Plan::SHORT, kShortRows, 4, 256, 0};
     if (a.rows <= 16) {
         const int64_t fixed = (two ? 2 : 1) * a.rows * blocks * kBlock * 2 + 16 * 1024 + blocks * 64, scales = ((int64_t)fc4_groups(a) * 5 + 4) * 16;
-        if (wgs(16, 16) > 1024 && fixed + 2 * scales <= few_lds(two, wgs(16, 32))) return {Fc4Plan::FEW_PAIRS, 16, 32, 512, 1024};
+        if (wgs(16, 16) > 1024 && blocks >= 32 && fixed + 16 * 1024 + 2 * scales <= few_lds(two, wgs(16, 32))) return {Fc4Plan::FEW_PAIRS, 16, 32, 512, 1024};
         if (fixed + scales <= few_lds(two, wgs(16, 16))) return {Fc4Plan::FEW, 16, 16, 512, 512};
     }
     const Fc4Tile *best = nullptr;

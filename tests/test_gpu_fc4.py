@@ -71,6 +71,12 @@ def test_every_tile(ctx, size, group, zeros, types):
     check(ctx, *size, group, types[0], BF16, types[1], zeros, seed=group)
 
 
+@pytest.mark.parametrize("rows, group, zeros", [(1, 32, True), (2, 64, False), (2, 96, True), (1, 128, False), (3, 128, True)])
+@pytest.mark.parametrize("x", [F16, BF16, F32])
+def test_long_rows_to_a_large_vocabulary(ctx, rows, group, zeros, x):
+    check(ctx, rows, 4100, 16410, group, x, F16, x, zeros, seed=rows + group)
+
+
 @pytest.mark.parametrize("x", [F16, BF16, F32])
 @pytest.mark.parametrize("scale", [F16, BF16, F32])
 @pytest.mark.parametrize("y", [F16, BF16, F32])
