@@ -268,15 +268,15 @@ __device__ static inline float fc4_sum_lanes(float v) {
 
 // ---- few rows: up to 16 of x, which LDS holds -----------------------------------------------------------
 // x lies in LDS as fp16 operands, [part][block][row][128], made once a workgroup, and so do the scales of all its weight rows.  The workgroup walks tiles
-// of 16 NT NW weight rows; its KW groups of waves take the blocks of K in turn and D blocks a wave are under way all the time, also from one tile to the next.
+// of 16 NT weight rows; its KW waves take the blocks of K in turn and D blocks a wave are under way all the time, also from one tile to the next.
 // Bound: the weights' way from HBM.  1 x 8192 to 32001 in groups of 128: 135 MB in 30.3 us, 4.5 TB/s (a copy of 1 GiB: 5.0); 1 x 4096 to 4096 4.8 us, of
 // which an empty launch is 2.1 and the trip to HBM and the meeting of the waves the most of the others.
-template <int X, int NT, int NW, int KW, int GM, int D, bool Z>
-__global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f, int tiles, int wgs, int groups, int own) {   // own: tiles of a workgroup at most
-    constexpr int THREADS = 64 * NW * KW, PARTS = X == X_F32 ? 2 : 1, MEET = NW * KW * NT * 256, ROWS = 16 * NT * NW;
+template <int X, int NT, int KW, int GM, int D, bool Z>
+__global__ __launch_bounds__(64 * KW) void fc4_few_kernel(const Fc4Kernel f, int tiles, int wgs, int groups, int own) {   // own: tiles of a workgroup at most
+    constexpr int THREADS = 64 * KW, PARTS = X == X_F32 ? 2 : 1, MEET = KW * NT * 256, ROWS = 16 * NT;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const Fc4Args &a = f.a;
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), nw = wave % NW, kw = wave / NW;
+    const int t = threadIdx.x, lane = t & 63, kw = __builtin_amdgcn_readfirstlane(t >> 6);
     const int c = lane & 15, kq = lane >> 4;
     const int rows = a.rows, blocks = (a.cin + kBlock - 1) / kBlock, part_bytes = blocks * rows * (kBlock * 2);
     float *meet = reinterpret_cast<float *>(lds + PARTS * part_bytes), *xs = meet + 2 * MEET;           // xs: [block][16], what x was divided by
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f
     const uint8_t *q[NT];
     Fc4Weights<NT> w[D];
     int at_tile = blockIdx.x, at = kw;
-    fc4_rows<NT>(q, a, (at_tile * NW + nw) * (16 * NT), c);
+    fc4_rows<NT>(q, a, at_tile * ROWS, c);
     auto ask = [&](Fc4Weights<NT> &to) {
         to.load(f, q, at, kq);
         at += KW;
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f
             at = more ? kw : at - KW;
             if (more) {
                 at_tile += wgs;
-                fc4_rows<NT>(q, a, (at_tile * NW + nw) * (16 * NT), c);
+                fc4_rows<NT>(q, a, at_tile * ROWS, c);
             }
         }
     };
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f
     unsigned magic = 0x64006400u;
     asm("" : "+v"(magic));   // in a register
     f32x4 total[NT] = {};
-    int tile = blockIdx.x, side = 0, block = kw, slot = nw * (16 * NT) + c;   // slot: this lane's first row among the scales
+    int tile = blockIdx.x, side = 0, block = kw, slot = c;   // slot: this lane's first row among the scales
     auto work = [&](Fc4Weights<NT> &v) {
         const f32x4 back = X != X_F16 ? *reinterpret_cast<const f32x4 *>(xs + block * 16 + kq * 4) : f32x4{};
         if ((block + 1) * kBlock > a.cin) v.shift(f, block, kq);
@@ -383,23 +383,23 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f
         }
         block += KW;
     };
-    // The end of a tile: the sums of the groups of waves in LDS, [kw][nw][tile][4][64], on the two sides in turn.
+    // The end of a tile: the sums of the waves in LDS, [kw][tile][4][64], on the two sides in turn.
     auto finish = [&]() {
         float *part = meet + side * MEET;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                part[((wave * NT + j) * 4 + e) * 64 + lane] = total[j][e];
+                part[((kw * NT + j) * 4 + e) * 64 + lane] = total[j][e];
                 total[j][e] = 0.f;
             }
         __syncthreads();
-        for (int o = t; o < NW * NT * 256; o += THREADS) {   // o = (tile of 16, e, lane)
+        for (int o = t; o < NT * 256; o += THREADS) {   // o = (tile of 16, e, lane)
             const int l = o & 63, m = (l >> 4) * 4 + ((o >> 6) & 3), n = tile * ROWS + (o >> 8) * 16 + (l & 15);
             if (m >= rows || n >= a.cout) continue;
             float v = 0.f;
 #pragma unroll
-            for (int k = 0; k < KW; ++k) v += part[k * (NW * NT * 256) + o];
+            for (int k = 0; k < KW; ++k) v += part[k * (NT * 256) + o];
             fc4_store(a.y, m * a.y_stride + n, a.y_dtype, v + bias[(o >> 8) * 16 + (l & 15)]);
         }
         tile += wgs;
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_few_kernel(const Fc4Kernel f
         slot += groups * ROWS;
         bias += ROWS;
     };
-    if (todo == 0) {   // fewer blocks than groups of waves
+    if (todo == 0) {   // fewer blocks than waves
         while (tile < tiles) finish();
         return;
     }
@@ -691,25 +691,30 @@ static int fc4_groups(const Fc4Args &a) { return (a.cin + a.group - 1) / a.group
 static bool fc4_plain(const Fc4Args &a) { return a.x_dtype == DT_BF16 && a.y_dtype != DT_F32; }   // in the forms for many rows
 static Fc4Kernel fc4_kernel_args(const Fc4Args &a) { return {a, make_fast_div((uint32_t)a.group), make_fast_div((uint32_t)(fc4_groups(a) + 15) / 16)}; }
 
-// LDS of fc4_few_kernel without the scales, and of the scales of a tile.
-template <int X, int NT, int NW, int KW>
-static int64_t few_bytes(const Fc4Args &a) {
+// How fc4_few_kernel walks tiles of 16 NT weight rows with KW waves: at most `most` workgroups, an even share of the tiles each, as far as LDS has room for
+// their scales (a place for zero points is counted where there are none too).
+struct Fc4Few {
+    int tiles, own, wgs;    // wgs 0: x does not fit
+    int64_t fixed, tile;    // LDS without the scales, and of the scales of a tile
+};
+static Fc4Few fc4_few(const Fc4Args &a, int nt, int kw, int most) {
     const int64_t blocks = (a.cin + kBlock - 1) / kBlock;
-    return (X == X_F32 ? 2 : 1) * a.rows * blocks * kBlock * 2 + 2 * NW * KW * NT * 1024 + (X == X_F16 ? 0 : blocks * 64);
+    Fc4Few f;
+    f.tiles = (a.cout + 16 * nt - 1) / (16 * nt);
+    f.fixed = (a.x_dtype == DT_F32 ? 2 : 1) * a.rows * blocks * kBlock * 2 + 2 * kw * nt * 1024 + (a.x_dtype == DT_F16 ? 0 : blocks * 64);
+    f.tile = ((int64_t)fc4_groups(a) * 5 + 4) * (16 * nt);
+    const int64_t fit = (few_lds(a.x_dtype == DT_F32, f.tiles) - f.fixed) / f.tile;
+    f.own = (f.tiles + most - 1) / most;
+    f.own = f.own < fit ? f.own : (int)fit;
+    f.wgs = f.own > 0 ? (f.tiles + f.own - 1) / f.own : 0;
+    return f;
 }
-template <int NT, int NW, bool Z>
-static int64_t few_tile_bytes(const Fc4Args &a) { return ((int64_t)fc4_groups(a) * (Z ? 5 : 4) + 4) * (16 * NT * NW); }
 
-template <int X, int NT, int NW, int KW, int GM, int D, bool Z>
-static hipError_t launch_few(const Fc4Args &a, int most_wgs, hipStream_t s) {
-    const int tiles = (a.cout + 16 * NT * NW - 1) / (16 * NT * NW), lds = few_lds(X == X_F32, tiles);
-    const int64_t fixed = few_bytes<X, NT, NW, KW>(a), tile = few_tile_bytes<NT, NW, Z>(a);
-    if (a.rows > 16 || a.cin < kShortIn || fixed + tile > lds) return hipErrorInvalidValue;
-    const int fit = (int)((lds - fixed) / tile);
-    int own = (tiles + most_wgs - 1) / most_wgs;
-    own = own < fit ? own : fit;
-    const int wgs = (tiles + own - 1) / own;
-    fc4_few_kernel<X, NT, NW, KW, GM, D, Z><<<dim3(wgs), 64 * NW * KW, (size_t)(fixed + own * tile), s>>>(fc4_kernel_args(a), tiles, wgs, fc4_groups(a), own);
+template <int X, int NT, int KW, int GM, int D, bool Z>
+static hipError_t launch_few(const Fc4Args &a, const Fc4Plan &p, hipStream_t s) {
+    const Fc4Few f = fc4_few(a, NT, KW, p.most);
+    if (a.rows > 16 || a.cin < kShortIn || f.wgs < 1 || p.cols != 16 * NT || p.threads != 64 * KW) return hipErrorInvalidValue;
+    fc4_few_kernel<X, NT, KW, GM, D, Z><<<dim3(f.wgs), 64 * KW, (size_t)(f.fixed + f.own * f.tile), s>>>(fc4_kernel_args(a), f.tiles, f.wgs, fc4_groups(a), f.own);
     return hipGetLastError();
 }
 
@@ -744,8 +749,8 @@ template <int X, int GM, bool Z>
 static hipError_t launch_fc4_form(const Fc4Args &a, const Fc4Plan &p, hipStream_t s) {
     constexpr bool two = X == X_F32;   // operands in two parts: twice the LDS
     if constexpr (X != X_PLAIN) {
-        if (p.form == Fc4Plan::FEW) return launch_few<X, 1, 1, 8, GM, 2, Z>(a, p.most, s);
-        if (p.form == Fc4Plan::FEW_PAIRS) return launch_few<X, 2, 1, 8, GM, 2, Z>(a, p.most, s);
+        if (p.form == Fc4Plan::FEW) return launch_few<X, 1, 8, GM, 2, Z>(a, p, s);
+        if (p.form == Fc4Plan::FEW_PAIRS) return launch_few<X, 2, 8, GM, 2, Z>(a, p, s);
     }
     switch (p.form) {
         case Fc4Plan::MANY1_16: return launch_many<X, 1, 1, 1, 8, 1, GM, Z>(a, p, s);

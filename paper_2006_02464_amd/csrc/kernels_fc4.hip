@@ -71,9 +71,8 @@ Fc4Plan fc4_plan(const Fc4Args &a) {
     auto wgs = [&](int rows, int cols) { return (int64_t)((a.rows + rows - 1) / rows) * ((a.cout + cols - 1) / cols); };
     if (a.cin < kShortIn) return {Fc4Plan::SHORT, kShortRows, 4, 256, 0};
     if (a.rows <= 16) {
-        const int64_t fixed = (two ? 2 : 1) * a.rows * blocks * kBlock * 2 + 16 * 1024 + blocks * 64, scales = ((int64_t)fc4_groups(a) * 5 + 4) * 16;
-        if (wgs(16, 16) > 1024 && blocks >= 32 && fixed + 16 * 1024 + 2 * scales <= few_lds(two, wgs(16, 32))) return {Fc4Plan::FEW_PAIRS, 16, 32, 512, 1024};
-        if (fixed + scales <= few_lds(two, wgs(16, 16))) return {Fc4Plan::FEW, 16, 16, 512, 512};
+        if (wgs(16, 16) > 1024 && blocks >= 32 && fc4_few(a, 2, 8, 1024).wgs) return {Fc4Plan::FEW_PAIRS, 16, 32, 512, 1024};
+        if (fc4_few(a, 1, 8, 512).wgs) return {Fc4Plan::FEW, 16, 16, 512, 512};
     }
     const Fc4Tile *best = nullptr;
     float least = 0.f;
@@ -88,10 +87,7 @@ Fc4Plan fc4_plan(const Fc4Args &a) {
 void fc4_grid(const Fc4Args &a, dim3 *grid, int *block) {
     const Fc4Plan p = fc4_plan(a);
     *grid = dim3((a.cout + p.cols - 1) / p.cols, (a.rows + p.rows - 1) / p.rows);
-    if (p.most > 0 && (int)grid->x > p.most) {   // fewer workgroups walk all tiles, an even share of them each
-        const unsigned own = (grid->x + p.most - 1) / p.most;
-        grid->x = (grid->x + own - 1) / own;
-    }
+    if (p.most > 0) grid->x = fc4_few(a, p.cols / 16, p.threads / 64, p.most).wgs;
     *block = p.threads;
 }
 
