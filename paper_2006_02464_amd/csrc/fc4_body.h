@@ -687,7 +687,7 @@ constexpr int kLdsBytes = 160 * 1024;
 // 1000 7.0 us, in the form for many rows, which converts them as often, 7.4; but fp16 16 x 4096 to 4096 8.6 us, and 7.1 in that form.
 constexpr int few_lds(bool fp32, int64_t tiles) { return fp32 && tiles <= 256 ? kLdsBytes : kLdsBytes / 2; }
 
-static int fc4_groups(const Fc4Args &a) { return (a.cin + a.group - 1) / a.group; }
+static int fc4_groups(const Fc4Args &a) { return (int)fc4_layout(a.cin, a.cout, a.group).groups; }   // `group` may be anything up to 2^31 - 32
 static bool fc4_plain(const Fc4Args &a) { return a.x_dtype == DT_BF16 && a.y_dtype != DT_F32; }   // in the forms for many rows
 static Fc4Kernel fc4_kernel_args(const Fc4Args &a) { return {a, make_fast_div((uint32_t)a.group), make_fast_div((uint32_t)(fc4_groups(a) + 15) / 16)}; }
 

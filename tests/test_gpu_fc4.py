@@ -248,6 +248,14 @@ def test_same_bits_every_time_on_two_streams_at_once_and_replayed(ctx, size):
         assert torch.equal(out, want)
 
 
+@pytest.mark.parametrize("group", [1 << 20, 1 << 30, (1 << 31) - 64, (1 << 31) - 32])
+@pytest.mark.parametrize("rows, cin", [(1, 20), (3, 4096), (16, 1000), (40, 4096), (130, 1000)])
+def test_a_group_longer_than_the_rows(ctx, group, rows, cin):
+    for zeros in (False, True):
+        check(ctx, rows, cin, 50, group, F16, F16, F32, zeros, seed=16)
+        check(ctx, rows, cin, 50, group, F32, F32, F32, zeros, seed=17)
+
+
 # ---- as an operator of a model ---------------------------------------------------------------------
 def fc4_model(dtype, classes, group):
     """A small network with FC4 in the place of FC, its blob, and the same network with the weights that the 4 bits stand for."""

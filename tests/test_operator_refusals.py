@@ -152,3 +152,20 @@ def test_fc4_in_an_operator_list(ctx):
         with pytest.raises(cw.CwError) as e:
             ctx.model_define(ops, 3, 16, 16, batch_sizes=(1,))
         assert e.value.status == status
+
+
+@pytest.mark.parametrize("group", [128, 1 << 20, 1 << 30, (1 << 31) - 64, (1 << 31) - 32])
+@pytest.mark.parametrize("cout", [10, 1 << 20])
+def test_a_group_longer_than_the_rows_is_one_group(ctx, group, cout):
+    """Up to the largest one: the plan and the places of the weights are those of the shortest that holds a whole row."""
+    assert refusal(ctx, cw.lib().cw_fc4, fc4_args(group=group)) == PLANNING
+    ops = lambda g: [(T.CONV, 3, 64, 3, 3, 2, 1, 1, -1, -1, 0, 0), (T.GAVGPOOL, 64, 64, 0, 0, 1, 0, 0, -1, 0, 0, 0), (cw.CW_OP_FC4, 64, cout, 1, 1, 1, 0, 0, -1, 1, 0, g),
+                     (T.SOFTMAX, cout, cout, 0, 0, 1, 0, 0, -1, 2, 0, 0)]
+    big = cw.Context(device=-1, weight_page_bytes=64 << 20)
+    try:
+        short, long = (big.model_define(ops(g), 3, 16, 16, batch_sizes=(1, 4)) for g in (64, group))
+        assert big.model_weight_bytes(long) == big.model_weight_bytes(short) and big.model_weight_pages(long) == big.model_weight_pages(short)
+        for batch in (1, 4):
+            assert big.plan(long, batch) == big.plan(short, batch)
+    finally:
+        big.destroy()
