@@ -7,19 +7,15 @@ namespace cw {
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(1)));     // a 16-byte load from any address (global memory takes them)
 
 constexpr int kBlock = 128;   // inputs that a wave takes at a time: 16 bytes of weights a lane, four lanes a row
 
-// How x becomes operands: fp16 as it is; bf16 and fp32 as fp16, scaled by a power of two to each row's and block's largest value, fp32 in two parts;
-// X_PLAIN: bf16 as it is, for results of 16 bits.  The weights then stand as bf16 numbers 16 + q, whose seven bits of mantissa hold no sign, and what is too
-// much, (16 + z) sum x, is taken off a group's sum.  Sums of up to 31 |x| where |q - z| |x| is wanted lose three bits or more of fp32's 24, which a
-// result of 8 or 11 bits does not show; in return x needs no conversion (see Fc4X).
-enum XForm { X_F16, X_BF16, X_F32, X_PLAIN };
-constexpr bool x_scaled(int x) { return x == X_BF16 || x == X_F32; }
+// How x becomes operands: fp16 as it is; bf16 and fp32 as fp16, scaled by a power of two to each row's and block's largest value, fp32 in two parts.
+// Weights are q - z exactly, whatever the type: a sum of (16 + q) x less (16 + z) sum x, which bf16 numbers would need no conversion for (512 x 4096 to 4096:
+// 33 us for 37; 2048 x 8192 to 8192: 300 for 394), rounds with 16 to 31 times every |x|, that of an input whose weights are zero among them.
+enum XForm { X_F16, X_BF16, X_F32 };
 constexpr int kShortIn = 32;   // rows of fewer inputs have fewer bytes than a load: a kernel of their own
 
 struct Fc4Kernel {
@@ -161,12 +157,6 @@ __device__ static inline f16x8 fc4_operand(unsigned v, unsigned z, unsigned magi
     return f16x8{w0[0], w0[1], w1[0], w1[1], w2[0], w2[1], w3[0], w3[1]};
 }
 
-// The same as 16 + q in bf16: nibbles as the upper bits of the mantissa.
-__device__ static inline bf16x8 fc4_operand_plain(unsigned v, unsigned magic) {
-    const u32x4 o = {((v << 3) & 0x00780078u) | magic, ((v >> 1) & 0x00780078u) | magic, ((v >> 5) & 0x00780078u) | magic, ((v >> 9) & 0x00780078u) | magic};
-    return __builtin_bit_cast(bf16x8, o);
-}
-
 // Eight activations as they are stored, from input k on (zeros behind cin).
 template <int X>
 struct Fc4X {
@@ -199,19 +189,9 @@ struct Fc4X {
         for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, raw[0][i] & 0x7fff7fffu));
         return (unsigned)(m[0] > m[1] ? m[0] : m[1]) << 16;
     }
-    // Their sum (bf16).
-    __device__ float sum() const {
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned word = raw[0][i], ones = 0x3f803f80u;
-            s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, word), __builtin_bit_cast(bf16x2, ones), s, false);
-        }
-        return s;
-    }
     // In the order in which the weights come, times `by`: the rounded value and, of fp32, what the rounding left.
     __device__ void operands(float by, f16x8 &hi, f16x8 &lo) const {
-        if (!x_scaled(X)) {
+        if (X == X_F16) {
             const u32x4 v = raw[0];
             const u32x4 o = {__builtin_amdgcn_perm(v[2], v[0], 0x05040100u), __builtin_amdgcn_perm(v[2], v[0], 0x07060302u),
                              __builtin_amdgcn_perm(v[3], v[1], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u)};
@@ -252,17 +232,6 @@ __device__ static inline unsigned fc4_max_row(unsigned v) {
     join(__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, false));    // lanes 2 3 0 1
     join(__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, false));   // mirrored in 8
     join(__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, false));   // mirrored in 16
-    return v;
-}
-
-// The sum of 4, 8 or 16 neighbouring lanes' numbers.
-template <int LANES>
-__device__ static inline float fc4_sum_lanes(float v) {
-    auto join = [&](int o) { v += __builtin_bit_cast(float, o); };
-    join(__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0xB1, 0xf, 0xf, false));
-    join(__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x4E, 0xf, 0xf, false));
-    if (LANES > 4) join(__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x141, 0xf, 0xf, false));
-    if (LANES > 8) join(__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x140, 0xf, 0xf, false));
     return v;
 }
 
@@ -438,7 +407,7 @@ __global__ __launch_bounds__(64 * KW) void fc4_few_kernel(const Fc4Kernel f, int
 template <int X, int MT, int NT, int NW, int KW, int PB>
 struct Fc4Many {
     static constexpr int ROWS = 16 * MT, COLS = 16 * NT * NW, THREADS = 64 * NW * KW, PARTS = X == X_F32 ? 2 : 1, ITEMS = ROWS / 4 / NW;   // ITEMS of a wave: four rows of a block each
-    static constexpr int PART = 4 * ROWS * 64, BUFFER = PARTS * PART + (X == X_F16 ? 0 : X == X_PLAIN ? ROWS * 16 : ROWS * 4);   // bytes of a block: operands, and what a row was divided by or its sums
+    static constexpr int PART = 4 * ROWS * 64, BUFFER = PARTS * PART + (X == X_F16 ? 0 : ROWS * 4);   // bytes of a block: operands, and what a row was divided by
     static constexpr int STAGED = KW * 2 * PB * BUFFER, MEET = NW * (KW - 1) * MT * NT * 1024, FIXED = (STAGED > MEET ? STAGED : MEET) + COLS * 4;   // LDS: x, where later the groups meet; the bias; the scales
 };
 
@@ -458,7 +427,7 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
     float *bias = reinterpret_cast<float *>(lds + S::FIXED - COLS * 4), *scales = reinterpret_cast<float *>(lds + S::FIXED);
     uint8_t *zeros = reinterpret_cast<uint8_t *>(scales + chunk_groups * COLS);
     f32x4 total[MT][NT] = {};
-    unsigned magic = X == X_PLAIN ? 0x41804180u : 0x64006400u;
+    unsigned magic = 0x64006400u;
     asm("" : "+v"(magic));   // in a register
 
     // Staging: sixteen lanes a row, whose sixteen pieces of a block change places with the row's number (modulo 16): every sixteen lanes write, and read, 256
@@ -486,13 +455,9 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
         for (int i = 0; i < ITEMS; ++i) {
             const int row = (nw * ITEMS + i) * 4 + (lane >> 4);
             float by = 1.f, back;
-            if (x_scaled(X)) {
+            if (X != X_F16) {
                 fc4_power(fc4_max_row(v[i].most()), by, back);
                 if (piece == 0) reinterpret_cast<float *>(to + PARTS * PART)[row] = back;
-            }
-            if (X == X_PLAIN) {
-                const float sum = fc4_sum_lanes<4 * GM>(v[i].sum());
-                if (piece % (4 * GM) == 0) reinterpret_cast<float *>(to + PARTS * PART)[piece / (4 * GM) * ROWS + row] = Z ? sum : -24.f * sum;
             }
             f16x8 hi, lo;
             v[i].operands(by, hi, lo);
@@ -525,33 +490,14 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
                     xx[part][i] = *reinterpret_cast<const f16x8 *>(from + part * PART + i * (16 * kBlock * 2) + xat[step]);
-            if (step % GM == 0) {   // X_PLAIN: a group begins at -(16 + z) times its inputs' sum
-                float less[NT];
-                if (X == X_PLAIN && Z)
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) less[j] = -16.f - (float)(zeros[at[step / GM] + j * 16] & 15);
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    const f32x4 of = X == X_PLAIN ? *reinterpret_cast<const f32x4 *>(from + PARTS * PART + (step / GM * ROWS + i * 16 + kq * 4) * 4) : f32x4{};
-#pragma unroll
-                    for (int j = 0; j < NT; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) p[i][j][e] = X == X_PLAIN && Z ? less[j] * of[e] : of[e];
-                }
-            }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                if constexpr (X == X_PLAIN) {
-                    const bf16x8 ww = fc4_operand_plain(v.w[j][step], magic);
+                const f16x8 ww = fc4_operand<Z>(v.w[j][step], Z ? zeros[at[step / GM] + j * 16] : 0u, magic);
+                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xx[0][i]), ww, p[i][j], 0, 0, 0);
-                } else {
-                    const f16x8 ww = fc4_operand<Z>(v.w[j][step], Z ? zeros[at[step / GM] + j * 16] : 0u, magic);
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xx[0][i], ww, p[i][j], 0, 0, 0);
-                        if (X == X_F32) p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xx[PARTS - 1][i], ww, p[i][j], 0, 0, 0);
-                    }
+                for (int i = 0; i < MT; ++i) {
+                    p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xx[0][i], ww, step % GM == 0 ? zero : p[i][j], 0, 0, 0);
+                    if (X == X_F32) p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xx[PARTS - 1][i], ww, p[i][j], 0, 0, 0);
                 }
             }
             if (step % GM == GM - 1) {
@@ -560,12 +506,12 @@ __global__ __launch_bounds__(64 * NW * KW) void fc4_many_kernel(const Fc4Kernel 
                 for (int j = 0; j < NT; ++j) scale[j] = scales[at[step / GM] + j * 16];
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    const f32x4 back = x_scaled(X) ? *reinterpret_cast<const f32x4 *>(from + PARTS * PART + (i * 16 + kq * 4) * 4) : f32x4{};
+                    const f32x4 back = X != X_F16 ? *reinterpret_cast<const f32x4 *>(from + PARTS * PART + (i * 16 + kq * 4) * 4) : f32x4{};
 #pragma unroll
                     for (int j = 0; j < NT; ++j)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            total[i][j][e] = x_scaled(X) ? fmaf(p[i][j][e] * scale[j], back[e], total[i][j][e]) : fmaf(p[i][j][e], scale[j], total[i][j][e]);
+                            total[i][j][e] = X != X_F16 ? fmaf(p[i][j][e] * scale[j], back[e], total[i][j][e]) : fmaf(p[i][j][e], scale[j], total[i][j][e]);
                 }
             }
         }
@@ -688,7 +634,6 @@ constexpr int kLdsBytes = 160 * 1024;
 constexpr int few_lds(bool fp32, int64_t tiles) { return fp32 && tiles <= 256 ? kLdsBytes : kLdsBytes / 2; }
 
 static int fc4_groups(const Fc4Args &a) { return (int)fc4_layout(a.cin, a.cout, a.group).groups; }   // `group` may be anything up to 2^31 - 32
-static bool fc4_plain(const Fc4Args &a) { return a.x_dtype == DT_BF16 && a.y_dtype != DT_F32; }   // in the forms for many rows
 static Fc4Kernel fc4_kernel_args(const Fc4Args &a) { return {a, make_fast_div((uint32_t)a.group), make_fast_div((uint32_t)(fc4_groups(a) + 15) / 16)}; }
 
 // How fc4_few_kernel walks tiles of 16 NT weight rows with KW waves: at most `most` workgroups, an even share of the tiles each, as far as LDS has room for
@@ -748,11 +693,9 @@ hipError_t launch_fc4_x(const Fc4Args &a, const Fc4Plan &p, hipStream_t s);
 template <int X, int GM, bool Z>
 static hipError_t launch_fc4_form(const Fc4Args &a, const Fc4Plan &p, hipStream_t s) {
     constexpr bool two = X == X_F32;   // operands in two parts: twice the LDS
-    if constexpr (X != X_PLAIN) {
-        if (p.form == Fc4Plan::FEW) return launch_few<X, 1, 8, GM, 2, Z>(a, p, s);
-        if (p.form == Fc4Plan::FEW_PAIRS) return launch_few<X, 2, 8, GM, 2, Z>(a, p, s);
-    }
     switch (p.form) {
+        case Fc4Plan::FEW: return launch_few<X, 1, 8, GM, 2, Z>(a, p, s);
+        case Fc4Plan::FEW_PAIRS: return launch_few<X, 2, 8, GM, 2, Z>(a, p, s);
         case Fc4Plan::MANY1_16: return launch_many<X, 1, 1, 1, 8, 1, GM, Z>(a, p, s);
         case Fc4Plan::MANY1_32: return launch_many<X, 1, 1, 2, 4, 2, GM, Z>(a, p, s);
         case Fc4Plan::MANY1_64: return launch_many<X, 1, 1, 4, 4, 2, GM, Z>(a, p, s);
@@ -762,7 +705,7 @@ static hipError_t launch_fc4_form(const Fc4Args &a, const Fc4Plan &p, hipStream_
         case Fc4Plan::MANY4_128: return launch_many<X, 4, 1, 8, 2, two ? 1 : 2, GM, Z>(a, p, s);
         case Fc4Plan::MANY4_256: return launch_many<X, 4, 2, 8, 1, two ? 1 : 2, GM, Z>(a, p, s);
         case Fc4Plan::MANY8_256:
-            if constexpr (!x_scaled(X)) return launch_many<X, 8, 2, 8, 1, 1, GM, Z>(a, p, s);
+            if constexpr (X == X_F16) return launch_many<X, 8, 2, 8, 1, 1, GM, Z>(a, p, s);
         default: return hipErrorInvalidValue;
     }
 }

@@ -6,7 +6,6 @@ namespace cw {
 extern template hipError_t launch_fc4_x<X_F16>(const Fc4Args &, const Fc4Plan &, hipStream_t);
 extern template hipError_t launch_fc4_x<X_BF16>(const Fc4Args &, const Fc4Plan &, hipStream_t);
 extern template hipError_t launch_fc4_x<X_F32>(const Fc4Args &, const Fc4Plan &, hipStream_t);
-extern template hipError_t launch_fc4_x<X_PLAIN>(const Fc4Args &, const Fc4Plan &, hipStream_t);
 
 // Rows of fewer bytes than a load: one wave a weight row, eight rows of x.
 constexpr int kShortRows = 8;
@@ -77,7 +76,7 @@ Fc4Plan fc4_plan(const Fc4Args &a) {
     const Fc4Tile *best = nullptr;
     float least = 0.f;
     for (const Fc4Tile &t : kFc4Tiles) {
-        if (t.form == Fc4Plan::MANY8_256 && a.x_dtype != DT_F16 && !fc4_plain(a)) continue;
+        if (t.form == Fc4Plan::MANY8_256 && a.x_dtype != DT_F16) continue;
         const float time = (float)((wgs(t.rows, t.cols) + 255) / 256) * (2.f + (two ? 2 : 1) * t.block * blocks);
         if (!best || time < least) best = &t, least = time;
     }
@@ -95,7 +94,6 @@ hipError_t launch_fc4(const Fc4Args &a, hipStream_t s) {
     if (a.rows < 1 || a.rows > kFc4MostRows || a.cin < 1 || a.cin > kFc4MostIn || a.cout < 1 || a.cout > kFc4MostOut || a.group < 32 || a.group % 32 != 0) return hipErrorInvalidValue;
     const Fc4Plan p = fc4_plan(a);
     if (p.form == Fc4Plan::SHORT) return launch_short(a, s);
-    if (fc4_plain(a) && p.form != Fc4Plan::FEW && p.form != Fc4Plan::FEW_PAIRS) return launch_fc4_x<X_PLAIN>(a, p, s);
     return a.x_dtype == DT_F16 ? launch_fc4_x<X_F16>(a, p, s) : a.x_dtype == DT_BF16 ? launch_fc4_x<X_BF16>(a, p, s) : launch_fc4_x<X_F32>(a, p, s);
 }
 

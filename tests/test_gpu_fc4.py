@@ -248,6 +248,29 @@ def test_same_bits_every_time_on_two_streams_at_once_and_replayed(ctx, size):
         assert torch.equal(out, want)
 
 
+def at_the_zero_point(d, channels):
+    """The weights of these inputs become zero: nibble = zero point."""
+    d["nib"][:, channels] = d["zeros"][:, channels // d["group"]] if d["zeros"] is not None else 8
+    wide = torch.zeros(d["nib"].shape[0], d["q"].shape[1] * 2, dtype=torch.uint8)
+    wide[:, :d["nib"].shape[1]] = d["nib"]
+    d["q"] = wide[:, 0::2] | (wide[:, 1::2] << 4)
+
+
+@pytest.mark.parametrize("rows", [5, 70, 500])
+@pytest.mark.parametrize("group, zeros", [(32, True), (64, False), (128, True)])
+@pytest.mark.parametrize("x, loud", [(F16, 3000.0), (BF16, 3e4), (F32, 3e4)], ids=["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("y", [F16, BF16, F32], ids=["to fp16", "to bf16", "to fp32"])
+def test_a_loud_activation_at_the_zero_point_takes_nothing_from_the_others(ctx, rows, group, zeros, x, loud, y):
+    """One input in every 128 is thousands of times the others, and all of its weights are zero."""
+    d = fc4_data(rows, 520, 300, group, x, F16, zeros, seed=14)
+    channels = torch.arange(5, 520, 128)
+    d["x"][:, channels] *= loud
+    at_the_zero_point(d, channels)
+    out = torch.full((rows, 300), float("nan"), dtype=y, device="cuda")
+    call(ctx, on_gpu(d), out)
+    assert_fc4(out.cpu(), *fc4_ref(d))
+
+
 @pytest.mark.parametrize("group", [1 << 20, 1 << 30, (1 << 31) - 64, (1 << 31) - 32])
 @pytest.mark.parametrize("rows, cin", [(1, 20), (3, 4096), (16, 1000), (40, 4096), (130, 1000)])
 def test_a_group_longer_than_the_rows(ctx, group, rows, cin):
