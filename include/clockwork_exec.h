@@ -287,7 +287,8 @@ int32_t cw_profile_get(cw_ctx *ctx, int32_t model_id, int32_t batch, cw_profile 
  * q - zero and its products with what stands for x are exact, sums are fp32, and the result is rounded once, to y's type.  fp16 activations stand as they are;
  * bf16 and fp32 ones as fp16 numbers scaled by a power of two for every 128 inputs of a row, fp32 in two parts: an fp32 activation is off by up to 2^-23 of
  * itself and 2^-39 of the largest of these 128, a bf16 one by less than 2^-38 of the largest, and by nothing from 2^-31 of it on.  With them a scale beyond
- * 2^100 may overflow. A NaN or an infinity of x stays in its row, one of scale or bias in its column. */
+ * 2^100 may overflow. A NaN or an infinity of x stays in its row and comes out as the formula has it (an infinity times a weight of zero is a NaN),
+ * one of scale or bias stays in its column. */
 typedef struct {
     const void *x;          /* [rows][cin], x_dtype */
     const uint8_t *q;       /* [cout][ceil(cin / 2)]: k even in the low, k odd in the high four bits */

@@ -157,6 +157,8 @@ __device__ static inline f16x8 fc4_operand(unsigned v, unsigned z, unsigned magi
     return f16x8{w0[0], w0[1], w1[0], w1[1], w2[0], w2[1], w3[0], w3[1]};
 }
 
+constexpr float kFc4LeastPower = 0x1p-113f;   // fc4_power's for blocks whose largest magnitude is 2^127 or more
+
 // Eight activations as they are stored, from input k on (zeros behind cin).
 template <int X>
 struct Fc4X {
@@ -215,6 +217,8 @@ struct Fc4X {
                 lo[2 * i + 1] = (f16)fmaf((float)p[1], -1.f, v1);
             }
         }
+        // What an infinity leaves is no number.  Half a step of a number below 2^15 is 8 at most; 16 is what the infinity outweighs.
+        if (X == X_F32 && __builtin_expect(by == kFc4LeastPower, 0)) lo = __builtin_elementwise_min(lo, (f16x8)(f16)16.f);
     }
 };
 // 2^(14 - e) for a largest magnitude of 2^e..2^(e+1): its numbers stay below 2^15; and 2^(e - 14).  Neither leaves fp32's range.

@@ -271,6 +271,31 @@ def test_a_loud_activation_at_the_zero_point_takes_nothing_from_the_others(ctx, 
     assert_fc4(out.cpu(), *fc4_ref(d))
 
 
+@pytest.mark.parametrize("x", [F16, BF16, F32])
+@pytest.mark.parametrize("y", [F16, BF16, F32])
+@pytest.mark.parametrize("rows, cin", [(5, 20), (5, 300), (100, 300), (100, 411)])
+def test_infinities_come_out_as_the_definition_has_them(ctx, x, y, rows, cin):
+    """x (q - z) s of an infinite x: an infinity of the product's sign, no number where the weight is zero or infinities of both signs meet."""
+    d = fc4_data(rows, cin, 40, 32, x, F16, True, seed=15)
+    inf = float("inf")
+    d["x"][0, 7] = inf
+    d["x"][1, cin - 1] = -inf
+    d["x"][2, 3], d["x"][2, 17] = inf, -inf
+    d["x"][3, 0], d["x"][3, 11] = -inf, float("nan")
+    d["x"][rows - 1, 2:9:3] = -inf
+    d["scales"][6] = 0.0
+    out = torch.zeros(rows, 40, dtype=y, device="cuda")
+    call(ctx, on_gpu(d), out)
+    out = out.cpu()
+    special = [0, 1, 2, 3, rows - 1]
+    want = (d["x"][special].double()[:, None] * fc4_weights(d)).sum(2)
+    assert not torch.isfinite(want).any() and torch.isinf(want).any() and torch.isnan(want).any()
+    assert torch.equal(out[special].double().nan_to_num(7.0, inf, -inf), want.nan_to_num(7.0, inf, -inf))
+    d["x"][special] = 0.0
+    others = [m for m in range(rows) if m not in special]
+    assert_fc4(out[others], *(v[others] for v in fc4_ref(d)))
+
+
 @pytest.mark.parametrize("group", [1 << 20, 1 << 30, (1 << 31) - 64, (1 << 31) - 32])
 @pytest.mark.parametrize("rows, cin", [(1, 20), (3, 4096), (16, 1000), (40, 4096), (130, 1000)])
 def test_a_group_longer_than_the_rows(ctx, group, rows, cin):
