@@ -313,7 +313,7 @@ int32_t cw_fc4(cw_ctx *ctx, const cw_fc4_args *args, void *stream);
  *            and -inf
  * A row with nothing but -inf: logp -inf, entropy 0, no top classes.  A row with a NaN or +inf: logp, entropy and
  * top_logp NaN, rank and top_id -1 (a negative `given` has logp 0 all the same).  The order is that of the logits as they are stored; sums are
- * fp32, and of two logits whose difference leaves fp32's range the smaller has no probability.
+ * fp32 over 32 classes and fp64 beyond, to fp32 at their end, and of two logits whose difference leaves fp32's range the smaller has no probability.
  * With few rows a row is shared by several workgroups, which meet in `workspace`: its first CW_ANSWER_COUNTERS bytes must be
  * zero before the first call and are zero behind every call.  Calls that may overlap in time need a workspace each.
  * Without one (NULL, or smaller than cw_answer_workspace_bytes) a workgroup takes a row; the answers are the same but for

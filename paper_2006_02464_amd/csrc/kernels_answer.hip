@@ -8,7 +8,8 @@ namespace cw {
 
 // One pass.  A workgroup takes a row, or a run of its segments, 32 logits a thread at a time in registers, 16 bytes a load.  Every thread keeps a
 // maximum m, S = sum 2^d and T = sum d 2^d with d = (x - m) scale / ln 2 of its own (a new maximum rescales both once a segment), the
-// threads meet at the end.  For the top classes a segment gives those of its logits that can still be among them to a list in LDS.
+// threads meet at the end.  A segment's 32 terms are added in fp32, segment to segment in fp64: one by one in fp32 equal terms round alike (error of S, one workgroup a
+// row: 6.5e-6 of it at 2^17 classes, 8.7e-4 at 2^24).  For the top classes a segment gives those of its logits that can still be among them to a list in LDS.
 constexpr int kEach = 32, kThreads = 256, kFewest = 64, kRowsOfAWave = 512;
 constexpr int kSegment = kThreads * kEach;
 constexpr int kParts = 32;                         // workgroups a row at most
@@ -58,6 +59,13 @@ __device__ static inline Soft join(const Soft &a, const Soft &b, float c2) {
     const float da = fmaxf((a.m - base) * c2, -1e30f), db = fmaxf((b.m - base) * c2, -1e30f);   // -inf times 0 is no number
     const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
     return {m, a.s * ea + b.s * eb, (a.t + a.s * da) * ea + (b.t + b.s * db) * eb};
+}
+
+// 2^d for d <= 0, near 1 with the bits of what it is less: a row that rises slowly rescales its sums in every segment.  The series' next term is 2^-21 of its sum at -1/2.
+__device__ static inline double fall(float d) {
+    const float y = d * 0.693147181f;
+    const float less = y * fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, 1.f / 720, 1.f / 120), 1.f / 24), 1.f / 6), 0.5f), 1.f);
+    return d > -0.5f ? 1.0 + (double)less : (double)__builtin_amdgcn_exp2f(d);
 }
 
 // Of all 64 lanes.
@@ -148,8 +156,9 @@ __device__ static inline unsigned kth_of(const unsigned *order, int k, int lane,
     return tau;
 }
 
+// Four waves a SIMD, as many workgroups of four as LDS holds lists for: two registers too many cost 254 x 64741 bf16 22 -> 31 us.
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS) void answer_kernel(const AnswerArgs a, int parts) {
+__global__ __launch_bounds__(THREADS, THREADS == kThreads ? 4 : 1) void answer_kernel(const AnswerArgs a, int parts) {
     constexpr int N = Vec<T>::N, CHUNKS = kEach / N, CHUNK = THREADS * N, SEGMENT = THREADS * kEach;
     typedef T TN __attribute__((ext_vector_type(N), aligned(sizeof(T))));
     __shared__ AnswerLds<THREADS> l;
@@ -163,7 +172,8 @@ __global__ __launch_bounds__(THREADS) void answer_kernel(const AnswerArgs a, int
     bool inside = false;
     float xg = INFINITY;
 
-    Soft soft{-INFINITY, 0.f, 0.f};
+    float max_yet = -INFINITY;
+    double s_yet = 0.0, t_yet = 0.0;
     int before = 0;       // logits that come before the given one
     int have = 0;         // classes in the list, the first `have` of it in order
     float bar = -INFINITY;   // the k-th of them: later ones have to be larger
@@ -232,21 +242,23 @@ __global__ __launch_bounds__(THREADS) void answer_kernel(const AnswerArgs a, int
             for (int e = 0; e < N; ++e) most = fmaxf(most, v[j * N + e]);
         }
         {
-            const float m = fmaxf(soft.m, most), ref = m == -INFINITY ? 0.f : m;
-            const float d0 = fmaxf((soft.m - ref) * c2, -1e30f), e0 = __builtin_amdgcn_exp2f(d0);
-            soft.t = (soft.t + soft.s * d0) * e0;
-            soft.s *= e0;
-            soft.m = m;
+            const float m = fmaxf(max_yet, most), ref = m == -INFINITY ? 0.f : m;
+            const float d0 = fmaxf((max_yet - ref) * c2, -1e30f);
+            const double e0 = fall(d0);
+            max_yet = m;
+            float s1 = 0.f, t1 = 0.f;
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j) {
                 if (j * CHUNK >= count) break;
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float d = (v[j * N + e] - ref) * c2, p = __builtin_amdgcn_exp2f(d);
-                    soft.s += p;
-                    soft.t = fmaf(p, fmaxf(d, -1000.f), soft.t);   // p is 0 long before
+                    s1 += p;
+                    t1 = fmaf(p, fmaxf(d, -1000.f), t1);   // p is 0 long before
                 }
             }
+            t_yet = fma(fma(s_yet, (double)d0, t_yet), e0, (double)t1);
+            s_yet = fma(s_yet, e0, (double)s1);
         }
         if (inside) {
 #pragma unroll
@@ -307,7 +319,7 @@ __global__ __launch_bounds__(THREADS) void answer_kernel(const AnswerArgs a, int
 
     // The threads meet.
     const auto plus = [](auto p, auto q) { return p + q; };
-    soft = meet(soft, c2);
+    const Soft soft = meet({max_yet, (float)s_yet, (float)t_yet}, c2);
     before = wave_all(before, plus);
     Soft all = soft;
     if constexpr (THREADS == 256) {

@@ -1,5 +1,7 @@
 """cw_answer against 64 bits: sizes from one on, types, masks that leave little or nothing, ties, orders that selection finds hard,
 strides, streams and graphs, and the chain of cw_fc4 and cw_answer."""
+import math
+
 import pytest
 import torch
 
@@ -220,6 +222,30 @@ def test_scales_near_the_ends_of_the_range(ctx, rows, classes, scale):
     x = torch.full((rows, classes), -2.0)
     x[:, 7:classes:40] = 1.5
     check(ctx, x, torch.full((rows,), 47, dtype=torch.int32), 5, scale)
+
+
+@pytest.mark.parametrize("classes", [1 << 17, (1 << 20) + 77, 1 << 24])
+@pytest.mark.parametrize("order", ["one above the rest", "few values", "rising", "rising fast", "random"])
+def test_sums_of_many_classes_keep_their_bits(ctx, classes, order):
+    """Rows that one workgroup walks, whose terms are alike and round alike.  In units of 2^-24 (mean and square: of |d| and d^2 under the probabilities): S of 32
+    terms in a row, then in more bits, then of 64 lanes and 4 waves: 31 + 10; its exponentials 4 + 2 mean; a maximum's rise a few: less than 64 + 8 mean together.
+    sum(d e) / S: 31 + 10 + 4 and S's own, each times mean, and 2 square from its exponentials: less than 128 mean + 8 square.  The last logarithm, product and
+    difference: two steps of what they give."""
+    i = torch.arange(classes, device="cuda")
+    x = {"one above the rest": torch.where(i == classes // 3, 0.0, -0.7), "few values": (i * 7919 % 5) * -0.3, "rising": i * (1.0 / (1 << 24)),
+         "rising fast": i * (20.0 / classes), "random": torch.randn(classes, device="cuda", generator=torch.Generator("cuda").manual_seed(3)) * 2.5}[order].float()[None]
+    given = torch.tensor([classes // 3], dtype=torch.int32, device="cuda")
+    got = {k: v[0].tolist() for k, v in call(ctx, x, given, 3).items()}
+    d = x[0].double() - x[0].double().max()
+    e = d.exp()
+    s = float(e.sum())
+    ls, mean, square = math.log(s), float(-(d * e).sum()) / s, float((d * d * e).sum()) / s
+    far = 2.0 ** -24 * (64 + 8 * mean)
+    step = 2.0 ** -22
+    for have, at in [(got["logp"], classes // 3)] + list(zip(got["top_logp"], got["top_id"])):
+        assert abs(have - (float(d[at]) - ls)) <= far + step * (abs(float(d[at])) + ls)
+    assert abs(got["entropy"] - (ls + mean)) <= 2.0 ** -24 * (64 + 128 * mean + 8 * square) + step * (ls + mean)
+    assert got["rank"] == int(((x[0] > x[0, classes // 3]) | ((x[0] == x[0, classes // 3]) & (i < classes // 3))).sum())
 
 
 @pytest.mark.parametrize("rows, cin, classes, x, z", [(1, 512, 1000, F32, F32), (5, 1024, 20011, F16, F16), (64, 640, 3001, BF16, F32)])
