@@ -237,13 +237,15 @@ int32_t cw_output(cw_ctx *ctx, int32_t slot, float *host_probs, float *host_logi
 /* OUTPUT of the answer instead of the rows of probabilities (see cw_answer for what it holds): computed on
  * `stream` behind the slot's EXEC from its logits and copied to host_answer [host], cw_answer_bytes(batch, top)
  * bytes: logp fp32 [batch], rank int32 [batch], entropy fp32 [batch], top_id int32 [batch][top], top_logp fp32
- * [batch][top], back to back.  host_given [host] int32 [batch] or NULL (nothing given).  Then releases the slot as
- * cw_output does.  CW_ERR_NO_INPUT if no EXEC ran, CW_ERR_INVALID / CW_ERR_UNSUPPORTED for arguments that cw_answer
+ * [batch][top], back to back.  host_given [host] int32 [batch] or NULL (nothing given); it is copied on `stream` and, like
+ * host_answer, belongs to the call until that copy is over.  Then releases the slot as cw_output does.  CW_ERR_NO_INPUT if no EXEC ran, CW_ERR_INVALID / CW_ERR_UNSUPPORTED for arguments that cw_answer
  * refuses, CW_ERR_NO_MEMORY where the answer is larger than the slot's input and its probabilities; the slot then stays. */
 int32_t cw_output_answer(cw_ctx *ctx, int32_t slot, const int32_t *host_given, int32_t top, float scale,
                          void *host_answer, void *stream);
 /* Bytes of that answer (0 for batch < 0 or top outside 0..CW_ANSWER_MOST_TOP). */
 size_t cw_answer_bytes(int32_t batch, int32_t top);
+/* Batch size of the request that holds the slot; CW_ERR_NO_INPUT if none does. */
+int32_t cw_slot_batch(cw_ctx *ctx, int32_t slot);
 /* Section 5.2, INFER: an action that is rejected after its INPUT (its window passed, its EXEC
  * failed) must give its IO-cache entry back without an OUTPUT.  Releases the slot without
  * copying anything out; the memory is reused only after its INPUT copy and its last EXEC have

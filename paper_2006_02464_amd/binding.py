@@ -108,6 +108,7 @@ SIGNATURES = {
     "cw_output": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_void_p]),
     "cw_output_answer": (c_int32, [c_void_p, c_int32, c_void_p, c_int32, c_float, c_void_p, c_void_p]),
     "cw_answer_bytes": (c_size_t, [c_int32, c_int32]),
+    "cw_slot_batch": (c_int32, [c_void_p, c_int32]),
     "cw_fc4": (c_int32, [c_void_p, c_void_p, c_void_p]),
     "cw_answer": (c_int32, [c_void_p, c_void_p, c_void_p]),
     "cw_answer_workspace_bytes": (c_size_t, []),
@@ -240,6 +241,19 @@ def _vector(t, what, device, count, kind):
     return t.data_ptr()
 
 
+def _host(x, what):
+    """(address, bytes, element type by name) of contiguous host memory: a numpy array, a CPU tensor."""
+    if isinstance(x, np.ndarray):
+        here, whole, nbytes, kind = True, x.flags["C_CONTIGUOUS"], x.nbytes, x.dtype.name if x.dtype.isnative else x.dtype.str
+    elif hasattr(x, "data_ptr"):
+        here, whole, nbytes, kind = x.device.type == "cpu", x.is_contiguous(), x.numel() * x.itemsize, str(x.dtype)[len("torch."):]
+    else:
+        raise TypeError("%s: %s is no array" % (what, type(x).__name__))
+    if not here or not whole:
+        raise ValueError("%s must be contiguous host memory" % what)
+    return _ptr(x), nbytes, kind
+
+
 def _stream(s):
     if s is None:
         return None
@@ -360,8 +374,27 @@ class Context:
         self._check(lib().cw_output(self._h, slot, _ptr(host_probs), _ptr(host_logits), _stream(stream)))
 
     def output_answer(self, slot, host_answer, given=None, top=0, scale=1.0, stream=None):
-        """host_answer: answer_bytes(batch, top) bytes; split_answer() names their parts once `stream` has been synchronised."""
-        self._check(lib().cw_output_answer(self._h, slot, _ptr(given), top, scale, _ptr(host_answer), _stream(stream)))
+        """host_answer: answer_bytes(batch, top) bytes; split_answer() names their parts once `stream` has been synchronised.
+        given: int32, one for each sample.  Both are host memory that stays until then: arrays, CPU tensors or, unchecked, addresses."""
+        batch = lib().cw_slot_batch(self._h, slot)   # none: the call says so
+        if host_answer is None or isinstance(host_answer, int):
+            to = _ptr(host_answer)
+        else:
+            to, nbytes, _ = _host(host_answer, "host_answer")
+            if isinstance(host_answer, np.ndarray) and not host_answer.flags["WRITEABLE"]:
+                raise ValueError("host_answer cannot be written")
+            if nbytes < self.answer_bytes(batch, top):
+                raise ValueError("host_answer has %d bytes, the answer %d" % (nbytes, self.answer_bytes(batch, top)))
+        if given is None or isinstance(given, int):
+            classes = _ptr(given)
+        else:
+            classes, nbytes, kind = _host(given, "given")
+            if kind != "int32" or (batch >= 0 and nbytes != 4 * batch):
+                raise ValueError("given must be %s contiguous elements of int32" % (batch if batch >= 0 else "a sample's"))
+        self._check(lib().cw_output_answer(self._h, slot, classes, top, scale, to, _stream(stream)))
+
+    def slot_batch(self, slot):
+        return self._check(lib().cw_slot_batch(self._h, slot))
 
     @staticmethod
     def answer_bytes(batch, top):

@@ -1361,6 +1361,12 @@ size_t cw_answer_bytes(int32_t batch, int32_t top) {
     return batch < 0 || top < 0 || top > kAnswerMostTop ? 0 : (size_t)batch * (12 + 8 * (size_t)top);
 }
 
+int32_t cw_slot_batch(cw_ctx *c, int32_t slot) {
+    if (!c) return CW_ERR_INVALID;
+    if (slot < 0 || slot >= kMaxSlots || c->slots[slot].state < SLOT_INPUT) return set_err(c, CW_ERR_NO_INPUT, "slot holds no request");
+    return c->slots[slot].batch;
+}
+
 int32_t cw_output_answer(cw_ctx *c, int32_t slot, const int32_t *host_given, int32_t top, float scale, void *host_answer, void *stream) {
     if (!c) return CW_ERR_INVALID;
     if (!host_answer) return set_err(c, CW_ERR_INVALID, "null output buffer");

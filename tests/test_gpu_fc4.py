@@ -376,3 +376,33 @@ def test_fc4_in_a_model(dtype, classes, group):
         assert rel_err_per_sample(again, want).max() <= TOL
     finally:
         wk.close()
+
+
+def test_output_answer_refuses_arrays_of_other_sizes():
+    """Too few given classes, or too many, and too little room: nothing is read or written, and the slot stays."""
+    import numpy as np
+
+    from operator_refs import answer_ref, assert_answer
+    from paper_2006_02464_amd.runner import Worker, pinned_like
+    from workload import gen
+    ops, blob, _, _, _ = fc4_model("fp16", 33, 64)
+    wk = Worker(workspace_bytes=64 << 20, io_bytes=8 << 20, weight_pool_bytes=64 << 20, load_staging_bytes=8 << 20)
+    try:
+        ctx = wk.ctx
+        mid = ctx.model_define(ops, 3, 30, 30, batch_sizes=(3,), dtype="fp16")
+        wk.load(mid, blob)
+        x = gen.images(5, 0, 3, 3, 30, 30, "normal", "fp16")
+        logits = torch.from_numpy(wk.infer(mid, x, 33)[1])
+        slot = ctx.input(mid, 3, pinned_like(np.ascontiguousarray(x, dtype=np.float32)), wk.stream)
+        assert ctx.slot_batch(slot) == 3
+        ctx.exec(mid, 3, slot, wk.stream)
+        given, host = torch.tensor([5, 0, 32], dtype=torch.int32), torch.zeros(ctx.answer_bytes(3, 4), dtype=torch.uint8)
+        for change in (dict(given=given[:2]), dict(given=given.repeat(2)), dict(given=given.long()), dict(given=given.cuda()), dict(host_answer=host[:-1]), dict(host_answer=host.cuda())):
+            with pytest.raises(ValueError):
+                ctx.output_answer(**dict(dict(slot=slot, host_answer=host, given=given, top=4, stream=wk.stream), **change))
+        assert ctx.slot_batch(slot) == 3 and not bool(host.any())
+        ctx.output_answer(slot, host, given, 4, stream=wk.stream)
+        wk.stream.synchronize()
+        assert_answer({k: torch.from_numpy(v.copy()) for k, v in ctx.split_answer(host, 3, 4).items()}, answer_ref(logits, given, 4, 1.0))
+    finally:
+        wk.close()

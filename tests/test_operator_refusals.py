@@ -94,6 +94,27 @@ def test_output_answer_refuses(ctx):
     assert e.value.status == cw.CW_ERR_INVALID
 
 
+def test_output_answer_refuses_arrays_that_do_not_fit(ctx):
+    """Before the call: other types than int32, memory with gaps, memory that cannot be written."""
+    host, given = np.zeros(4096, np.uint8), np.zeros(3, np.int32)
+    locked = host.copy()
+    locked.flags.writeable = False
+    for change in (dict(given=given.astype(np.int64)), dict(given=torch.zeros(3, dtype=torch.int64)), dict(given=torch.zeros(3)), dict(given=np.zeros(6, np.int32)[::2]),
+                   dict(given=torch.zeros(6, dtype=torch.int32)[::2]), dict(given=given.astype(">i4")), dict(host_answer=host[::2]), dict(host_answer=locked)):
+        with pytest.raises(ValueError):
+            ctx.output_answer(**dict(dict(slot=0, host_answer=host, given=given), **change))
+    with pytest.raises(TypeError):
+        ctx.output_answer(0, host, [1, 2, 3])
+    for ok in (given, torch.zeros(3, dtype=torch.int32), None):
+        with pytest.raises(cw.CwError) as e:
+            ctx.output_answer(0, host, ok)
+        assert "planning-only" in str(e.value)
+    for slot in (-1, 0, 1 << 20):
+        with pytest.raises(cw.CwError) as e:
+            ctx.slot_batch(slot)
+        assert e.value.status == cw.CW_ERR_NO_INPUT
+
+
 def test_answer_sizes():
     assert cw.Context.answer_bytes(3, 5) == 3 * 52 and cw.Context.answer_bytes(0, 5) == 0 and cw.Context.answer_bytes(7, 0) == 84
     assert cw.Context.answer_bytes(-1, 5) == 0 and cw.Context.answer_bytes(1, 65) == 0 and cw.Context.answer_bytes(1, -1) == 0
