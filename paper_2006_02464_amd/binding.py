@@ -200,6 +200,16 @@ def _packed(args):
 _pack_fc4, _pack_answer = _packed(cw_fc4_args), _packed(cw_answer_args)
 
 
+def _refused(error, **numbers):
+    """The error for numbers that do not fit their fields, in the library's terms."""
+    for name, number in numbers.items():
+        if not hasattr(number, "__index__") and not (name == "scale" and hasattr(number, "__float__")):
+            return TypeError("%s: %r" % (name, number))
+    if isinstance(error, OverflowError):
+        return CwError(CW_ERR_INVALID, "scale must be finite and positive")
+    return CwError(CW_ERR_UNSUPPORTED, "too large: " + ", ".join("%s %s" % n for n in numbers.items()))
+
+
 class _Types(dict):
     """CW_DTYPE_* of a torch dtype."""
 
@@ -425,9 +435,12 @@ class Context:
         yp, ys = _matrix(y, "y", on, rows, cout)
         if q.itemsize != 1 or (zeros is not None and zeros.itemsize != 1):
             raise TypeError("q and zeros hold bytes")
-        self._check(lib().cw_fc4(self._h, _pack_fc4(
-            xp, qp, sp, zp, _vector(bias, "bias", on, cout, "torch.float32"), yp, xs, qs, ss, zs, ys,
-            rows, cin, cout, group, code[x.dtype], code[scales.dtype], code[y.dtype]), _stream(stream)))
+        try:
+            args = _pack_fc4(xp, qp, sp, zp, _vector(bias, "bias", on, cout, "torch.float32"), yp, xs, qs, ss, zs, ys,
+                             rows, cin, cout, group, code[x.dtype], code[scales.dtype], code[y.dtype])
+        except (struct.error, OverflowError) as e:
+            raise _refused(e, rows=rows, cin=cin, cout=cout, group=group) from None
+        self._check(lib().cw_fc4(self._h, args, _stream(stream)))
 
     def answer(self, logits, given=None, logp=None, rank=None, entropy=None, top_id=None, top_logp=None, scale=1.0, workspace=None,
                stream=None):
@@ -436,14 +449,20 @@ class Context:
         rows, classes = logits.shape
         on = self._device
         lp, ls = _matrix(logits, "logits", on, rows, classes)
+        if top_id is not None and top_id.dim() != 2:
+            raise ValueError("top_id is %s, not (rows, top)" % (tuple(top_id.shape),))
         top = top_id.shape[1] if top_id is not None else 0
         space = workspace.numel() if workspace is not None else 0
-        self._check(lib().cw_answer(self._h, _pack_answer(
-            lp, _vector(given, "given", on, rows, "torch.int32"), _vector(logp, "logp", on, rows, "torch.float32"),
-            _vector(rank, "rank", on, rows, "torch.int32"), _vector(entropy, "entropy", on, rows, "torch.float32"),
-            _vector(top_id, "top_id", on, rows * top, "torch.int32"), _vector(top_logp, "top_logp", on, rows * top, "torch.float32"),
-            _vector(workspace, "workspace", on, space, "torch.uint8"), space, ls,
-            rows, classes, top, _element_codes[logits.dtype], scale), _stream(stream)))
+        try:
+            args = _pack_answer(
+                lp, _vector(given, "given", on, rows, "torch.int32"), _vector(logp, "logp", on, rows, "torch.float32"),
+                _vector(rank, "rank", on, rows, "torch.int32"), _vector(entropy, "entropy", on, rows, "torch.float32"),
+                _vector(top_id, "top_id", on, rows * top, "torch.int32"), _vector(top_logp, "top_logp", on, rows * top, "torch.float32"),
+                _vector(workspace, "workspace", on, space, "torch.uint8"), space, ls,
+                rows, classes, top, _element_codes[logits.dtype], scale)
+        except (struct.error, OverflowError) as e:
+            raise _refused(e, rows=rows, classes=classes, top=top, scale=scale) from None
+        self._check(lib().cw_answer(self._h, args, _stream(stream)))
 
     @staticmethod
     def answer_workspace_bytes():

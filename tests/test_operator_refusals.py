@@ -151,6 +151,26 @@ def test_binding_refuses_tensors_that_do_not_fit(ctx):
         ctx.answer(**dict(ok, logits=z.double()))
 
 
+def test_binding_refuses_numbers_out_of_range_as_the_library_does(ctx):
+    """A group or a number of rows beyond 32 bits and a scale beyond fp32: the library's error; no numbers at all: TypeError."""
+    y, q, s = torch.zeros(3, 20), torch.zeros(20, 50, dtype=torch.uint8), torch.zeros(20, 1)
+    fc4 = dict(x=torch.zeros(3, 100), q=q, scales=s, y=y, group=128)
+    answer = dict(logits=torch.zeros(3, 50), given=torch.zeros(3, dtype=torch.int32), logp=torch.zeros(3))
+    many = dict(x=torch.zeros(1, 100).expand(1 << 31, -1), y=torch.zeros(1, 20).expand(1 << 31, -1))
+    for call, args, status in ((ctx.fc4, dict(fc4, group=1 << 31), cw.CW_ERR_UNSUPPORTED), (ctx.fc4, dict(fc4, group=1 << 70), cw.CW_ERR_UNSUPPORTED), (ctx.fc4, dict(fc4, **many), cw.CW_ERR_UNSUPPORTED),
+                               (ctx.answer, dict(logits=torch.zeros(1, 50).expand(1 << 31, -1)), cw.CW_ERR_UNSUPPORTED),
+                               (ctx.answer, dict(answer, scale=1e39), cw.CW_ERR_INVALID), (ctx.answer, dict(answer, scale=float("inf")), cw.CW_ERR_INVALID), (ctx.answer, dict(answer, scale=-1e300), cw.CW_ERR_INVALID)):
+        with pytest.raises(cw.CwError) as e:
+            call(**args)
+        assert e.value.status == status and "planning-only" not in str(e.value)
+    for call, args in ((ctx.fc4, dict(fc4, group=128.0)), (ctx.fc4, dict(fc4, group="128")), (ctx.answer, dict(answer, scale="1")), (ctx.answer, dict(answer, scale=None))):
+        with pytest.raises(TypeError):
+            call(**args)
+    for top_id in (torch.zeros(3, dtype=torch.int32), torch.zeros(3, 2, 2, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            ctx.answer(**dict(answer, top_id=top_id, top_logp=torch.zeros(3, 2)))
+
+
 def test_fc4_in_an_operator_list(ctx):
     conv, pool, soft = (T.CONV, 3, 64, 3, 3, 2, 1, 1, -1, -1, 0, 0), (T.GAVGPOOL, 64, 64, 0, 0, 1, 0, 0, -1, 0, 0, 0), (T.SOFTMAX, 10, 10, 0, 0, 1, 0, 0, -1, 2, 0, 0)
     fc4 = lambda group=32, src=1: (cw.CW_OP_FC4, 64, 10, 1, 1, 1, 0, 0, -1, src, 0, group)
