@@ -210,3 +210,24 @@ def test_a_group_longer_than_the_rows_is_one_group(ctx, group, cout):
             assert big.plan(long, batch) == big.plan(short, batch)
     finally:
         big.destroy()
+
+
+@pytest.mark.parametrize("classes, page, fc_pages", [(2000, 1 << 20, 2), (4000, 2 << 20, 2), (4000, 1 << 20, None)])
+def test_fc4_takes_fewer_bytes_and_pages_than_the_layer_in_16_bits(classes, page, fc_pages):
+    """256 features in groups of 64: 128 + 4 (2 + 1) bytes a class for 512.  The last size in 16 bits is larger than a page."""
+    convs = [(T.CONV, 3, 256, 3, 3, 2, 1, 1, -1, -1, 0, 0), (T.CONV, 256, 256, 1, 1, 1, 0, 1, -1, 0, 0, 0), (T.GAVGPOOL, 256, 256, 0, 0, 1, 0, 0, -1, 1, 0, 0)]
+    ops = lambda op, g: convs + [(op, 256, classes, 1, 1, 1, 0, 0, -1, 2, 0, g), (T.SOFTMAX, classes, classes, 0, 0, 1, 0, 0, -1, 3, 0, 0)]
+    c = cw.Context(device=-1, weight_page_bytes=page)
+    try:
+        small = c.model_define(ops(cw.CW_OP_FC4, 64), 3, 16, 16, batch_sizes=(1,))
+        assert c.model_weight_pages(small) == 1
+        if fc_pages is None:
+            with pytest.raises(cw.CwError) as e:
+                c.model_define(ops(T.FC, 0), 3, 16, 16, batch_sizes=(1,))
+            assert e.value.status == cw.CW_ERR_UNSUPPORTED
+        else:
+            large = c.model_define(ops(T.FC, 0), 3, 16, 16, batch_sizes=(1,))
+            assert c.model_weight_pages(large) == fc_pages
+            assert c.model_weight_bytes(large) - c.model_weight_bytes(small) == (512 - 140) * classes
+    finally:
+        c.destroy()
