@@ -349,7 +349,9 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 4 : 1) void answer_k
             }
         }
         // The stores and the loads behind them go past the L2s one by one: a release and an acquire of the counter would write back and drop all of an
-        // XCD's L2 for each workgroup (64 x 50001, 448 workgroups, no top classes: 11.7 us for 7.9).
+        // XCD's L2 for each workgroup (64 x 50001, 448 workgroups, no top classes: 11.7 us for 7.9).  C++ promises no order of relaxed accesses to different words; it comes
+        // from the hardware, as the memory model of gfx942 in LLVM's guide to the AMDGPU backend has it: an agent's store (sc1) counts as outstanding (vmcnt) until
+        // it is where the other XCDs' loads of that scope look.  What a release would add, writing back the L2's other lines, is about none of these words.
         __builtin_amdgcn_s_waitcnt(0);   // this thread's stores have been made
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
         __syncthreads();                 // ... and so have the workgroup's
