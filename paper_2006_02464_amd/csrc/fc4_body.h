@@ -241,12 +241,13 @@ __device__ static inline unsigned fc4_max_row(unsigned v) {
 
 // ---- few rows: up to 16 of x, which LDS holds -----------------------------------------------------------
 // x lies in LDS as fp16 operands, [part][block][row][128], made once a workgroup, and so do the scales of all its weight rows.  The workgroup walks tiles
-// of 16 NT weight rows; its KW waves take the blocks of K in turn and D blocks a wave are under way all the time, also from one tile to the next.
+// of 16 NT weight rows; its eight waves take the blocks of K in turn and two blocks a wave are under way all the time, also from one tile to the next.
 // Bound: the weights' way from HBM.  1 x 8192 to 32001 in groups of 128: 135 MB in 30.3 us, 4.5 TB/s (a copy of 1 GiB: 5.0); 1 x 4096 to 4096 4.8 us, of
 // which an empty launch is 2.1 and the trip to HBM and the meeting of the waves the most of the others.
-template <int X, int NT, int KW, int GM, int D, bool Z>
-__global__ __launch_bounds__(64 * KW) void fc4_few_kernel(const Fc4Kernel f, int tiles, int wgs, int groups, int own) {   // own: tiles of a workgroup at most
-    constexpr int THREADS = 64 * KW, PARTS = X == X_F32 ? 2 : 1, MEET = KW * NT * 256, ROWS = 16 * NT;
+constexpr int kFewWaves = 8;
+template <int X, int NT, int GM, bool Z>
+__global__ __launch_bounds__(64 * kFewWaves) void fc4_few_kernel(const Fc4Kernel f, int tiles, int wgs, int groups, int own) {   // own: tiles of a workgroup at most
+    constexpr int KW = kFewWaves, D = 2, THREADS = 64 * KW, PARTS = X == X_F32 ? 2 : 1, MEET = KW * NT * 256, ROWS = 16 * NT;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const Fc4Args &a = f.a;
     const int t = threadIdx.x, lane = t & 63, kw = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -640,17 +641,17 @@ constexpr int few_lds(bool fp32, int64_t tiles) { return fp32 && tiles <= 256 ? 
 static int fc4_groups(const Fc4Args &a) { return (int)fc4_layout(a.cin, a.cout, a.group).groups; }   // `group` may be anything up to 2^31 - 32
 static Fc4Kernel fc4_kernel_args(const Fc4Args &a) { return {a, make_fast_div((uint32_t)a.group), make_fast_div((uint32_t)(fc4_groups(a) + 15) / 16)}; }
 
-// How fc4_few_kernel walks tiles of 16 NT weight rows with KW waves: at most `most` workgroups, an even share of the tiles each, as far as LDS has room for
+// How fc4_few_kernel walks tiles of 16 NT weight rows: at most `most` workgroups, an even share of the tiles each, as far as LDS has room for
 // their scales (a place for zero points is counted where there are none too).
 struct Fc4Few {
     int tiles, own, wgs;    // wgs 0: x does not fit
     int64_t fixed, tile;    // LDS without the scales, and of the scales of a tile
 };
-static Fc4Few fc4_few(const Fc4Args &a, int nt, int kw, int most) {
+static Fc4Few fc4_few(const Fc4Args &a, int nt, int most) {
     const int64_t blocks = (a.cin + kBlock - 1) / kBlock;
     Fc4Few f;
     f.tiles = (a.cout + 16 * nt - 1) / (16 * nt);
-    f.fixed = (a.x_dtype == DT_F32 ? 2 : 1) * a.rows * blocks * kBlock * 2 + 2 * kw * nt * 1024 + (a.x_dtype == DT_F16 ? 0 : blocks * 64);
+    f.fixed = (a.x_dtype == DT_F32 ? 2 : 1) * a.rows * blocks * kBlock * 2 + 2 * kFewWaves * nt * 1024 + (a.x_dtype == DT_F16 ? 0 : blocks * 64);
     f.tile = ((int64_t)fc4_groups(a) * 5 + 4) * (16 * nt);
     const int64_t fit = (few_lds(a.x_dtype == DT_F32, f.tiles) - f.fixed) / f.tile;
     f.own = (f.tiles + most - 1) / most;
@@ -659,11 +660,11 @@ static Fc4Few fc4_few(const Fc4Args &a, int nt, int kw, int most) {
     return f;
 }
 
-template <int X, int NT, int KW, int GM, int D, bool Z>
+template <int X, int NT, int GM, bool Z>
 static hipError_t launch_few(const Fc4Args &a, const Fc4Plan &p, hipStream_t s) {
-    const Fc4Few f = fc4_few(a, NT, KW, p.most);
-    if (a.rows > 16 || a.cin < kShortIn || f.wgs < 1 || p.cols != 16 * NT || p.threads != 64 * KW) return hipErrorInvalidValue;
-    fc4_few_kernel<X, NT, KW, GM, D, Z><<<dim3(f.wgs), 64 * KW, (size_t)(f.fixed + f.own * f.tile), s>>>(fc4_kernel_args(a), f.tiles, f.wgs, fc4_groups(a), f.own);
+    const Fc4Few f = fc4_few(a, NT, p.most);
+    if (a.rows > 16 || a.cin < kShortIn || f.wgs < 1 || p.cols != 16 * NT || p.threads != 64 * kFewWaves) return hipErrorInvalidValue;
+    fc4_few_kernel<X, NT, GM, Z><<<dim3(f.wgs), 64 * kFewWaves, (size_t)(f.fixed + f.own * f.tile), s>>>(fc4_kernel_args(a), f.tiles, f.wgs, fc4_groups(a), f.own);
     return hipGetLastError();
 }
 
@@ -698,8 +699,8 @@ template <int X, int GM, bool Z>
 static hipError_t launch_fc4_form(const Fc4Args &a, const Fc4Plan &p, hipStream_t s) {
     constexpr bool two = X == X_F32;   // operands in two parts: twice the LDS
     switch (p.form) {
-        case Fc4Plan::FEW: return launch_few<X, 1, 8, GM, 2, Z>(a, p, s);
-        case Fc4Plan::FEW_PAIRS: return launch_few<X, 2, 8, GM, 2, Z>(a, p, s);
+        case Fc4Plan::FEW: return launch_few<X, 1, GM, Z>(a, p, s);
+        case Fc4Plan::FEW_PAIRS: return launch_few<X, 2, GM, Z>(a, p, s);
         case Fc4Plan::MANY1_16: return launch_many<X, 1, 1, 1, 8, 1, GM, Z>(a, p, s);
         case Fc4Plan::MANY1_32: return launch_many<X, 1, 1, 2, 4, 2, GM, Z>(a, p, s);
         case Fc4Plan::MANY1_64: return launch_many<X, 1, 1, 4, 4, 2, GM, Z>(a, p, s);

@@ -70,8 +70,8 @@ Fc4Plan fc4_plan(const Fc4Args &a) {
     auto wgs = [&](int rows, int cols) { return (int64_t)((a.rows + rows - 1) / rows) * ((a.cout + cols - 1) / cols); };
     if (a.cin < kShortIn) return {Fc4Plan::SHORT, kShortRows, 4, 256, 0};
     if (a.rows <= 16) {
-        if (wgs(16, 16) > 1024 && blocks >= 32 && fc4_few(a, 2, 8, 1024).wgs) return {Fc4Plan::FEW_PAIRS, 16, 32, 512, 1024};
-        if (fc4_few(a, 1, 8, 512).wgs) return {Fc4Plan::FEW, 16, 16, 512, 512};
+        if (wgs(16, 16) > 1024 && blocks >= 32 && fc4_few(a, 2, 1024).wgs) return {Fc4Plan::FEW_PAIRS, 16, 32, 64 * kFewWaves, 1024};
+        if (fc4_few(a, 1, 512).wgs) return {Fc4Plan::FEW, 16, 16, 64 * kFewWaves, 512};
     }
     const Fc4Tile *best = nullptr;
     float least = 0.f;
@@ -86,7 +86,7 @@ Fc4Plan fc4_plan(const Fc4Args &a) {
 void fc4_grid(const Fc4Args &a, dim3 *grid, int *block) {
     const Fc4Plan p = fc4_plan(a);
     *grid = dim3((a.cout + p.cols - 1) / p.cols, (a.rows + p.rows - 1) / p.rows);
-    if (p.most > 0) grid->x = fc4_few(a, p.cols / 16, p.threads / 64, p.most).wgs;
+    if (p.most > 0) grid->x = fc4_few(a, p.cols / 16, p.most).wgs;
     *block = p.threads;
 }
 
