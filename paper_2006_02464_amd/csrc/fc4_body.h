@@ -242,7 +242,7 @@ __device__ static inline unsigned fc4_max_row(unsigned v) {
 // ---- few rows: up to 16 of x, which LDS holds -----------------------------------------------------------
 // x lies in LDS as fp16 operands, [part][block][row][128], made once a workgroup, and so do the scales of all its weight rows.  The workgroup walks tiles
 // of 16 NT weight rows; its eight waves take the blocks of K in turn and two blocks a wave are under way all the time, also from one tile to the next.
-// Bound: the weights' way from HBM.  1 x 8192 to 32001 in groups of 128: 135 MB in 30.3 us, 4.5 TB/s (a copy of 1 GiB: 5.0); 1 x 4096 to 4096 4.8 us, of
+// Bound: the weights' way from HBM.  1 x 8192 to 32001 in groups of 128: 135 MB in 32-33 us, 4.1 TB/s (a copy of 1 GiB: 5.0); 1 x 4096 to 4096 4.8 us, of
 // which an empty launch is 2.1 and the trip to HBM and the meeting of the waves the most of the others.
 constexpr int kFewWaves = 8;
 template <int X, int NT, int GM, bool Z>
@@ -407,7 +407,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void fc4_few_kernel(const Fc4Kernel
 // phase, PB blocks of x, in one of two LDS buffers while they multiply the other one, from registers that were loaded two blocks before; weights go straight
 // to the registers of the wave that multiplies them, as early.
 // Bound: vector instructions, next to which the matrix cores run: of a block's 16 weight rows and 64 rows of x about 90 to make operands and scale sums and
-// 16 on the matrix cores, which twice the rows share (64 x 4096 to 16384: vector units 53% of the time, matrix cores 18%; 2048 x 8192 to 8192: 52% and 45%).
+// 16 on the matrix cores, which twice the rows share (fp16, 64 x 4096 to 16384: vector units 52% of the time, matrix cores 18%; 2048 x 8192 to 8192: 52% and 46%; bf16, 512 x 4096 to 4096: 80% and 23%).
 // Two blocks between barriers: 512 x 4096 to 4096 fp16 26.1 -> 25.2 us; 32 x 4096 to 16384 14.3 -> 13.2.
 template <int X, int MT, int NT, int NW, int KW, int PB>
 struct Fc4Many {

@@ -184,7 +184,7 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 4 : 1) void answer_k
         if (inside) xg = (float)x[g];
     };
     // Of 16 bits the next segment's logits are under way beside this one's 32 numbers (2000 x 20000, five top classes: 36.5 -> 33.9 us; 946 x 69207, none:
-    // 44 -> 40); of fp32 they take registers from the other waves (860 x 23898: 32.1 -> 34.7).
+    // 44 -> 40; but rows in four parts of two segments, 254 x 64741: 20.2 -> 21.4); of fp32 they take registers from the other waves (860 x 23898: 32.1 -> 34.7).
     constexpr bool AHEAD = sizeof(T) == 2;
     TN raw[CHUNKS];
     auto fetch = [&](int seg) {
@@ -426,6 +426,8 @@ size_t answer_workspace_bytes() { return kCounterSlots * 4 + (size_t)kRecords * 
 
 hipError_t launch_answer(const AnswerArgs &a, hipStream_t s) {
     if (a.rows < 1 || a.rows > kAnswerMostRows || a.classes < 1 || a.classes > kAnswerMostClasses || a.top < 0 || a.top > kAnswerMostTop || (a.top > 0 && (!a.top_id || !a.top_logp))) return hipErrorInvalidValue;
+    // Shared are as many rows as there are counters, each by as many workgroups as records and segments allow: 256 x 64741 bf16 21.8 us in four parts a row, 257 rows in
+    // one 34.1; 64 x 50001 11.9 in seven.
     const int segments = (a.classes + kSegment - 1) / kSegment;
     int parts = 1;
     if (a.workspace && a.rows <= kCounterSlots) {

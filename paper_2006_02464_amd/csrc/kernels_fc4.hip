@@ -40,7 +40,7 @@ static hipError_t launch_short(const Fc4Args &a, hipStream_t s) {
 
 // Up to 16 rows whose x LDS holds: one workgroup keeps it and walks tiles of 16 weight rows; pairs of tiles, twice the loads under way, where there are more
 // than two for each of 512 workgroups and they are long (us one by one and in pairs, 1 x 8192 bf16 to 32001: 36.1 and 32.4, 2 x 4096 fp16 to 60000: 36.5
-// and 33.3; but 6 x 1536 fp32 to 31051: 11.7 and 14.7, 8 x 2048 bf16 to 20000: 14.2 and 15.9).
+// and 33.3; but 6 x 1536 fp32 to 31051: 11.7 and 14.7, 8 x 2048 bf16 to 20000, groups of 32: 14.2 and 15.9).
 // More: x in blocks, and tiles of 16 x 16 to 128 x 256.  A larger tile reads x and converts weights less often for each product, and fewer of them fill
 // the 256 CUs, so the tile is the one with the least  rounds of 256 workgroups x (2 us + a time for each block of 128 inputs), which were measured in graphs
 // of calls over several sets of weights (fp16, groups of 128; us, rates in TFLOP/s):
@@ -54,7 +54,7 @@ static hipError_t launch_short(const Fc4Args &a, hipStream_t s) {
 //   512 x 4096 to 4096                                      35      25-29   41       64
 //   1024 x 4096 to 4096                                             56.7    45.5     64.8
 //   2048 x 8192 to 8192                                     475     366     317      265 (1036; a library's product of 16-bit weights 1226)
-// fp32, in two parts, takes about twice the time for a block, and 128 rows' two parts do not fit in the registers; nor do those of scaled bf16.
+// fp32, in two parts, takes about twice the time for a block, and 128 rows' two parts do not fit in the registers; nor do 128 rows of bf16 beside their conversion.
 struct Fc4Tile {
     Fc4Plan::Form form;
     int rows, cols, threads, threads_two;   // threads_two: of activations in two parts
