@@ -296,6 +296,33 @@ def test_infinities_come_out_as_the_definition_has_them(ctx, x, y, rows, cin):
     assert_fc4(out[others], *(v[others] for v in fc4_ref(d)))
 
 
+@pytest.mark.parametrize("rows", [16, 100])
+@pytest.mark.parametrize("x, most", [(F16, 1.0), (F16, 1.9921875)] + [(x, most) for x in (BF16, F32) for most in (1.0, 1.9921875, 2.0 ** 100, 1.5 * 2.0 ** -100)])
+def test_what_is_kept_of_an_activation_beside_a_larger_one(ctx, rows, x, most):
+    """Each row has one input of weight 0, the largest, and one of weight 1, smaller by more from row to row: the result is what stands for it, no sum and no
+    rounding of its own.  The bounds are the header's."""
+    g = torch.Generator().manual_seed(18)
+    d = fc4_data(rows, 130, 16, 128, x, F32, False, seed=18)
+    d["x"].zero_()
+    d["x"][:, 40] = most
+    small = ((1.0 + torch.rand(rows, generator=g)) * 0.5 * most * 2.0 ** -(torch.arange(rows) % 48).double()).to(x)
+    d["x"][:, 77] = small * (1 - 2 * (torch.arange(rows) % 2)).to(x)
+    d["nib"][:, 77] = 9
+    at_the_zero_point(d, torch.tensor([40]))
+    d["scales"].fill_(1.0)
+    d["bias"].zero_()
+    out = torch.full((rows, 16), float("nan"), device="cuda")
+    call(ctx, on_gpu(d), out)
+    have, want = out.cpu().double(), d["x"][:, 77:78].double()
+    off = (have - want).abs()
+    if x == F16:
+        assert bool((off == 0).all())
+    elif x == BF16:
+        assert bool((off < 2.0 ** -38 * most).all()) and bool((off[want[:, 0].abs() >= 2.0 ** -31 * most] == 0).all())
+    else:
+        assert bool((off <= 2.0 ** -23 * want.abs() + 2.0 ** -39 * most).all())
+
+
 @pytest.mark.parametrize("group", [1 << 20, 1 << 30, (1 << 31) - 64, (1 << 31) - 32])
 @pytest.mark.parametrize("rows, cin", [(1, 20), (3, 4096), (16, 1000), (40, 4096), (130, 1000)])
 def test_a_group_longer_than_the_rows(ctx, group, rows, cin):
