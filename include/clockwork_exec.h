@@ -65,7 +65,7 @@ enum {
 
 enum { CW_OP_CONV = 0, CW_OP_MAXPOOL = 1, CW_OP_GAVGPOOL = 2, CW_OP_FC = 3, CW_OP_SOFTMAX = 4, CW_OP_CONCAT = 5, CW_OP_FC4 = 6 };
 enum { CW_ACT_NONE = 0, CW_ACT_RELU = 1, CW_ACT_HSWISH = 2 };   /* values of cw_op.relu */
-enum { CW_DTYPE_FP16 = 0, CW_DTYPE_BF16 = 1, CW_DTYPE_FP32 = 2 };   /* a model's storage type is one of the first two */
+enum { CW_DTYPE_FP16 = 0, CW_DTYPE_BF16 = 1, CW_DTYPE_FP32 = 2, CW_DTYPE_E4M3 = 3 };   /* a model's storage type is one of the first two; the last is for a cache's pages */
 
 /* One operator of a model.  Ops form a DAG over earlier ops' outputs.
  * CONV:     cross-correlation, kh x kw, `stride`, zero padding, + bias[cout], then (if
@@ -341,6 +341,96 @@ typedef struct {
 int32_t cw_answer(cw_ctx *ctx, const cw_answer_args *args, void *stream);
 /* Workspace that serves every call (less than 1 MiB). */
 size_t cw_answer_workspace_bytes(void);
+
+/* Keys and values of sequences of tokens, in pages of `page` tokens that a program gives out as it likes: row s of a `table` names the pages of sequence s in
+ * order, its token t lies at place t % page of page table[s][t / page].  A page number outside 0..pages - 1 stands for a page that is not there: nothing is
+ * written to it, what is read of it is 0, attention leaves its tokens out.  The same goes for tokens beyond the table's row.
+ * With CW_DTYPE_E4M3 a number is code * 2^(exponent - 127): codes have 8 bits (sign, 4, 3; the largest 448), the exponent is a byte for every token and head, of keys
+ * and of values.  Strides are in elements (bytes for codes and exponents), 16 bytes divide the addresses of all keys' and values' rows and head_dim is a multiple
+ * of 16. */
+typedef struct {
+    void *k, *v;                /* [pages][kv_heads][page][head_dim], dtype */
+    uint8_t *k_exp, *v_exp;     /* [pages][kv_heads][page] with CW_DTYPE_E4M3, else NULL */
+    int64_t page_stride, head_stride, token_stride;               /* of k and of v */
+    int64_t exp_page_stride, exp_head_stride, exp_token_stride;   /* of k_exp and of v_exp */
+    int32_t pages, kv_heads;
+    int32_t page;               /* a power of two, up to CW_CACHE_MOST_PAGE */
+    int32_t head_dim;           /* a multiple of 16, up to CW_ATTEND_MOST_DIM */
+    int32_t dtype;              /* CW_DTYPE_FP16, BF16 or E4M3 */
+} cw_cache;
+#define CW_CACHE_MOST_PAGE 4096
+#define CW_ATTEND_MOST_DIM 256
+
+/* Writes the newest tokens of sequences to their pages, reads them back.  Sequence s has lengths[s] tokens, these included, and rows first[s]..first[s + 1] - 1 of k and v
+ * are its last ones; rows outside first[0]..first[sequences] - 1 are not touched, nor read.  Tokens before a sequence's beginning (more rows than lengths[s]) are not written
+ * and read as 0.  A place that is in the table twice must not be written twice in one call.
+ * Writing: numbers are rounded to the pages' type; with CW_DTYPE_E4M3 the exponent is the least (from -127 on) with which the largest finite magnitude of a token's head is
+ * at most 448 * 2^exponent, codes are the nearest (ties to even) of x / 2^exponent, a NaN or an infinity becomes a NaN.  Reading: code * 2^exponent, rounded once to
+ * the rows' type. */
+typedef struct {
+    const cw_cache *cache;      /* [host] */
+    void *k, *v;                /* [tokens][kv_heads][head_dim], dtype: read by cw_cache_write, written by cw_cache_read */
+    const int32_t *first;       /* [sequences + 1], not falling; NULL: one row a sequence (tokens == sequences) */
+    const int32_t *lengths;     /* [sequences] */
+    const int32_t *table;       /* [sequences][table_pages] */
+    int64_t k_stride, k_head_stride, v_stride, v_head_stride, table_stride;
+    int32_t tokens, sequences, table_pages;
+    int32_t dtype;              /* CW_DTYPE_FP16, BF16 or FP32 */
+} cw_cache_args;
+int32_t cw_cache_write(cw_ctx *ctx, const cw_cache_args *args, void *stream);
+int32_t cw_cache_read(cw_ctx *ctx, const cw_cache_args *args, void *stream);
+
+/* Attention of one new token of each sequence over the tokens in its pages (its own among them, written before):
+ *   y[s][h] = sum over t of p[t] * v[t][h'],  p = softmax over t of scale * q[s][h] . k[t][h'],  h' = h / (heads / kv_heads)
+ * over the tokens t < lengths[s], with `window` > 0 the last `window` of them.  lse is the logarithm of the softmax's denominator, with which results over parts of a
+ * sequence can be joined.  A row that sees no token has y 0 and lse -inf.  Products with the numbers as they are stored are exact, sums and the softmax fp32; of
+ * fp16, and of E4M3, p goes into the second product in 11 bits, of bf16 in 16; the result is rounded once.  Scores of +inf or NaN make their row NaN; numbers of tokens that
+ * are not seen have no effect whatever they are.
+ * Sequences are shared by several workgroups, which meet in `workspace`: its first CW_ATTEND_COUNTERS bytes must be zero before the first call and are zero behind every call.  Calls
+ * that may overlap in time need a workspace each.  Without one (NULL), or with less than cw_attend_one_workspace_bytes(), a sequence's heads are shared less or not at all; the results
+ * are the same but for the order of the sums. */
+#define CW_ATTEND_COUNTERS 65536
+typedef struct {
+    const cw_cache *cache;      /* [host] */
+    const void *q;              /* [sequences][heads][head_dim], dtype */
+    void *y;                    /* the same */
+    float *lse;                 /* [sequences][heads] or NULL */
+    const int32_t *lengths;     /* [sequences] */
+    const int32_t *table;       /* [sequences][table_pages] */
+    void *workspace;            /* 16-byte aligned, or NULL */
+    size_t workspace_bytes;
+    int64_t q_stride, q_head_stride, y_stride, y_head_stride, table_stride;
+    int32_t sequences, heads;   /* heads: a multiple of kv_heads */
+    int32_t table_pages;
+    int32_t window;             /* 0: all tokens */
+    int32_t dtype;              /* CW_DTYPE_FP16 or BF16; that of the cache unless it is E4M3 */
+    float scale;                /* finite */
+} cw_attend_one_args;
+int32_t cw_attend_one(cw_ctx *ctx, const cw_attend_one_args *args, void *stream);
+/* Workspace that serves every call (32 MiB). */
+size_t cw_attend_one_workspace_bytes(void);
+
+/* Attention of whole prompts, or of parts of them behind their histories, packed one behind the other: queries first[s]..first[s + 1] - 1 see keys
+ * first_k[s]..first_k[s + 1] - 1 of their sequence.  causal: the last query sees all of the sequence's keys, the one before it all but the last, and so on
+ * (query i of n those j <= i + m - n of m keys); with `window` > 0 the last `window` of these.  Else as cw_attend_one, with p in the second product in the values' type.  Rows outside
+ * first[0]..first[sequences] - 1 are not touched. */
+typedef struct {
+    const void *q;              /* [tokens][heads][head_dim], dtype */
+    const void *k, *v;          /* [keys][kv_heads][head_dim], dtype */
+    void *y;                    /* [tokens][heads][head_dim], dtype */
+    float *lse;                 /* [tokens][heads] or NULL */
+    const int32_t *first;       /* [sequences + 1], not falling */
+    const int32_t *first_k;     /* the same of the keys, or NULL: that of the queries */
+    int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride, y_stride, y_head_stride;
+    int32_t tokens, keys, sequences;
+    int32_t heads, kv_heads;    /* heads: a multiple of kv_heads */
+    int32_t head_dim;           /* a multiple of 16, up to CW_ATTEND_MOST_DIM */
+    int32_t causal;             /* 0 or 1 */
+    int32_t window;             /* 0: no bound; else with causal only */
+    int32_t dtype;              /* CW_DTYPE_FP16 or BF16 */
+    float scale;                /* finite */
+} cw_attend_args;
+int32_t cw_attend(cw_ctx *ctx, const cw_attend_args *args, void *stream);
 
 /* Device ordinal the context was created on (-1: planning only). */
 int32_t cw_context_device(cw_ctx *ctx);

@@ -17,8 +17,9 @@ CW_ERR_ALREADY_LOADED, CW_ERR_NO_INPUT, CW_ERR_BAD_BATCH, CW_ERR_BUSY = -5, -6, 
 CW_ERR_UNSUPPORTED, CW_ERR_NO_SLOT, CW_ERR_TOO_LATE, CW_ERR_TIMEOUT = -9, -10, -11, -12
 CW_OP_CONV, CW_OP_MAXPOOL, CW_OP_GAVGPOOL, CW_OP_FC, CW_OP_SOFTMAX, CW_OP_CONCAT = 0, 1, 2, 3, 4, 5
 CW_OP_FC4 = 6
-CW_DTYPE_FP16, CW_DTYPE_BF16, CW_DTYPE_FP32 = 0, 1, 2
+CW_DTYPE_FP16, CW_DTYPE_BF16, CW_DTYPE_FP32, CW_DTYPE_E4M3 = 0, 1, 2, 3
 CW_ANSWER_MOST_TOP, CW_ANSWER_COUNTERS = 64, 1024
+CW_CACHE_MOST_PAGE, CW_ATTEND_MOST_DIM, CW_ATTEND_COUNTERS = 4096, 256, 65536
 DTYPES = {"fp16": CW_DTYPE_FP16, "bf16": CW_DTYPE_BF16}
 CONV_TILES = {"128x128": 0, "128x64": 1, "64x64": 2, "64x32": 3, "32x64": 4, "32x32": 5,
               "128x64w2": 6, "64x128w2": 7, "256x64": 8, "128x128w8": 9,
@@ -48,6 +49,31 @@ class cw_answer_args(Structure):
     _fields_ = [(n, c_void_p) for n in ("logits", "given", "logp", "rank", "entropy", "top_id", "top_logp", "workspace")] + \
                [("workspace_bytes", c_size_t), ("stride", c_int64)] + \
                [(n, c_int32) for n in ("rows", "classes", "top", "dtype")] + [("scale", c_float)]
+
+
+class cw_cache(Structure):
+    _fields_ = [(n, c_void_p) for n in ("k", "v", "k_exp", "v_exp")] + \
+               [(n, c_int64) for n in ("page_stride", "head_stride", "token_stride", "exp_page_stride", "exp_head_stride", "exp_token_stride")] + \
+               [(n, c_int32) for n in ("pages", "kv_heads", "page", "head_dim", "dtype")]
+
+
+class cw_cache_args(Structure):
+    _fields_ = [(n, c_void_p) for n in ("cache", "k", "v", "first", "lengths", "table")] + \
+               [(n, c_int64) for n in ("k_stride", "k_head_stride", "v_stride", "v_head_stride", "table_stride")] + \
+               [(n, c_int32) for n in ("tokens", "sequences", "table_pages", "dtype")]
+
+
+class cw_attend_one_args(Structure):
+    _fields_ = [(n, c_void_p) for n in ("cache", "q", "y", "lse", "lengths", "table", "workspace")] + \
+               [("workspace_bytes", c_size_t)] + \
+               [(n, c_int64) for n in ("q_stride", "q_head_stride", "y_stride", "y_head_stride", "table_stride")] + \
+               [(n, c_int32) for n in ("sequences", "heads", "table_pages", "window", "dtype")] + [("scale", c_float)]
+
+
+class cw_attend_args(Structure):
+    _fields_ = [(n, c_void_p) for n in ("q", "k", "v", "y", "lse", "first", "first_k")] + \
+               [(n, c_int64) for n in ("q_stride", "q_head_stride", "k_stride", "k_head_stride", "v_stride", "v_head_stride", "y_stride", "y_head_stride")] + \
+               [(n, c_int32) for n in ("tokens", "keys", "sequences", "heads", "kv_heads", "head_dim", "causal", "window", "dtype")] + [("scale", c_float)]
 
 
 class cw_profile(Structure):
@@ -112,6 +138,11 @@ SIGNATURES = {
     "cw_fc4": (c_int32, [c_void_p, c_void_p, c_void_p]),
     "cw_answer": (c_int32, [c_void_p, c_void_p, c_void_p]),
     "cw_answer_workspace_bytes": (c_size_t, []),
+    "cw_cache_write": (c_int32, [c_void_p, c_void_p, c_void_p]),
+    "cw_cache_read": (c_int32, [c_void_p, c_void_p, c_void_p]),
+    "cw_attend_one": (c_int32, [c_void_p, c_void_p, c_void_p]),
+    "cw_attend_one_workspace_bytes": (c_size_t, []),
+    "cw_attend": (c_int32, [c_void_p, c_void_p, c_void_p]),
     "cw_release": (c_int32, [c_void_p, c_int32]),
     "cw_exec_duration_ns": (c_int32, [c_void_p, c_int32, POINTER(c_uint64)]),
     "cw_profile_measure": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_uint32, POINTER(cw_profile), c_void_p]),
@@ -198,6 +229,7 @@ def _packed(args):
 
 
 _pack_fc4, _pack_answer = _packed(cw_fc4_args), _packed(cw_answer_args)
+_pack_cache_args, _pack_attend_one, _pack_attend = _packed(cw_cache_args), _packed(cw_attend_one_args), _packed(cw_attend_args)
 
 
 def _refused(error, **numbers):
@@ -221,7 +253,18 @@ class _Types(dict):
         raise TypeError("%s is no element type of this call" % dtype)
 
 
-_element_codes = _Types()
+class _PageTypes(dict):
+    """CW_DTYPE_* of a torch dtype that a cache's pages have."""
+
+    def __missing__(self, dtype):
+        if not self:
+            import torch
+            self.update({torch.float16: CW_DTYPE_FP16, torch.bfloat16: CW_DTYPE_BF16, torch.float8_e4m3fn: CW_DTYPE_E4M3})
+            return self[dtype]
+        raise TypeError("%s is no type of a cache's pages" % dtype)
+
+
+_element_codes, _page_codes = _Types(), _PageTypes()
 _vector_types = {}   # names of torch dtypes
 
 
@@ -249,6 +292,68 @@ def _vector(t, what, device, count, kind):
     if t.numel() != count or _vector_types[dtype] != kind or not t.is_contiguous():
         raise ValueError("%s must be %d contiguous elements of %s" % (what, count, kind))
     return t.data_ptr()
+
+
+def _heads(t, what, device, shape):
+    """(address, row stride, head stride) of [rows][heads][head_dim] on GPU `device` whose last elements are contiguous."""
+    if t.get_device() != device:
+        raise ValueError("%s is not on the context's GPU" % what)
+    if t.shape != shape:
+        raise ValueError("%s is %s, not %s" % (what, tuple(t.shape), tuple(shape)))
+    row, head, step = t.stride()
+    if step != 1:
+        raise ValueError("%s: numbers of a head must be contiguous" % what)
+    return t.data_ptr(), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
+
+
+def _table(table, lengths, device):
+    """(address of the table, its row stride, address of the lengths, sequences, pages a row)."""
+    if table.dim() != 2:
+        raise ValueError("table is %s, not (sequences, pages)" % (tuple(table.shape),))
+    sequences, pages = table.shape
+    at, row = _matrix(table, "table", device, sequences, pages)
+    if table.dtype not in _vector_types:
+        _vector_types[table.dtype] = str(table.dtype)
+    if _vector_types[table.dtype] != "torch.int32":
+        raise ValueError("table holds int32")
+    return at, row if sequences > 1 else 0, _vector(lengths, "lengths", device, sequences, "torch.int32"), sequences, pages
+
+
+class Cache:
+    """Pages of keys and values as the calls over them take them: made by Context.cache, holds the tensors that it names."""
+
+    def __init__(self, device, k, v, k_exp, v_exp):
+        if k.dim() != 4:
+            raise ValueError("k is %s, not (pages, kv_heads, page, head_dim)" % (tuple(k.shape),))
+        if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+            raise ValueError("k and v are laid out differently")
+        pages, kv_heads, page, head_dim = k.shape
+        strides = k.stride()
+        if strides[3] != 1 and head_dim > 1:
+            raise ValueError("numbers of a head must be contiguous")
+        if (k_exp is None) != (v_exp is None):
+            raise ValueError("exponents of both keys and values, or of neither")
+        exps = (0, 0, 0)
+        if k_exp is not None:
+            if k_exp.shape != k.shape[:3] or v_exp.shape != k.shape[:3] or k_exp.stride() != v_exp.stride():
+                raise ValueError("k_exp and v_exp must be %s and laid out alike" % (tuple(k.shape[:3]),))
+            if str(k_exp.dtype) != "torch.uint8" or str(v_exp.dtype) != "torch.uint8":
+                raise TypeError("exponents are bytes")
+            exps = k_exp.stride()
+        for t in (k, v, k_exp, v_exp):
+            if t is not None and t.get_device() != device:
+                raise ValueError("the cache is not on the context's GPU")
+        at = [t.data_ptr() if t is not None else None for t in (k, v, k_exp, v_exp)]
+        try:
+            fields = at + [int(n) for n in (*strides[:3], *exps)]
+            if not all(0 <= n < 1 << 31 for n in k.shape):
+                raise CwError(CW_ERR_UNSUPPORTED, "too large")
+            self._struct = cw_cache(*fields, pages, kv_heads, page, head_dim, _page_codes[k.dtype])
+        except OverflowError:
+            raise CwError(CW_ERR_UNSUPPORTED, "too large") from None
+        self.tensors = (k, v, k_exp, v_exp)
+        self.kv_heads, self.head_dim = kv_heads, head_dim
+        self._address = ctypes.addressof(self._struct)
 
 
 def _host(x, what):
@@ -468,6 +573,83 @@ class Context:
     def answer_workspace_bytes():
         return lib().cw_answer_workspace_bytes()
 
+    # -- a paged cache of keys and values, and attention
+    def cache(self, k, v, k_exp=None, v_exp=None):
+        """Names pages: k, v [pages][kv_heads][page][head_dim] in fp16, bf16 or float8_e4m3fn, the last with exponents [pages][kv_heads][page] (uint8).  Kept
+        as long as the pages are; what the library refuses of them the calls that take it tell."""
+        return Cache(self._device, k, v, k_exp, v_exp)
+
+    def _cache_rows(self, call, cache, k, v, table, lengths, first, stream):
+        if k.dim() != 3:
+            raise ValueError("k is %s, not (tokens, kv_heads, head_dim)" % (tuple(k.shape),))
+        if k.dtype != v.dtype:
+            raise TypeError("k and v are of different types")
+        on, shape = self._device, (k.shape[0], cache.kv_heads, cache.head_dim)
+        tokens = shape[0]
+        kp, ks, kh = _heads(k, "k", on, shape)
+        vp, vs, vh = _heads(v, "v", on, shape)
+        tp, ts, lp, sequences, pages = _table(table, lengths, on)
+        try:
+            args = _pack_cache_args(cache._address, kp, vp, _vector(first, "first", on, sequences + 1, "torch.int32"), lp, tp, ks, kh, vs, vh, ts,
+                                    tokens, sequences, pages, _element_codes[k.dtype])
+        except (struct.error, OverflowError) as e:
+            raise _refused(e, tokens=tokens, sequences=sequences, pages=pages) from None
+        self._check(call(self._h, args, _stream(stream)))
+
+    def cache_write(self, k, v, cache, table, lengths, first=None, stream=None):
+        """Writes rows of k and v [tokens][kv_heads][head_dim] to the pages of `cache` as the last tokens of their sequences: rows first[s]..first[s + 1] - 1 of
+        sequence s, that has lengths[s] tokens with them and its pages in table[s]; without `first` a row each.  torch tensors on the context's GPU, integers int32."""
+        self._cache_rows(lib().cw_cache_write, cache, k, v, table, lengths, first, stream)
+
+    def cache_read(self, cache, table, lengths, k, v, first=None, stream=None):
+        """Reads the same rows back into k and v."""
+        self._cache_rows(lib().cw_cache_read, cache, k, v, table, lengths, first, stream)
+
+    def attend_one(self, q, cache, table, lengths, y, scale, window=0, lse=None, workspace=None, stream=None):
+        """y[sequences][heads][head_dim] = attention of q, a token of each sequence, over the lengths[s] tokens (the last `window`) in the pages table[s] of
+        `cache`; lse [sequences][heads] fp32 is written if there is one.  workspace: uint8, zeros before its first call."""
+        if q.dim() != 3:
+            raise ValueError("q is %s, not (sequences, heads, head_dim)" % (tuple(q.shape),))
+        tp, ts, lp, sequences, pages = _table(table, lengths, self._device)
+        heads, on, shape = q.shape[1], self._device, (sequences, q.shape[1], cache.head_dim)
+        qp, qs, qh = _heads(q, "q", on, shape)
+        yp, ys, yh = _heads(y, "y", on, shape)
+        if y.dtype != q.dtype:
+            raise TypeError("q and y are of different types")
+        space = workspace.numel() if workspace is not None else 0
+        try:
+            args = _pack_attend_one(cache._address, qp, yp, _vector(lse, "lse", on, sequences * heads, "torch.float32"), lp, tp,
+                                    _vector(workspace, "workspace", on, space, "torch.uint8"), space, qs, qh, ys, yh, ts,
+                                    sequences, heads, pages, window, _element_codes[q.dtype], scale)
+        except (struct.error, OverflowError) as e:
+            raise _refused(e, sequences=sequences, heads=heads, window=window, scale=scale) from None
+        self._check(lib().cw_attend_one(self._h, args, _stream(stream)))
+
+    @staticmethod
+    def attend_one_workspace_bytes():
+        return lib().cw_attend_one_workspace_bytes()
+
+    def attend(self, q, k, v, y, first, scale, first_k=None, causal=True, window=0, lse=None, stream=None):
+        """y[tokens][heads][head_dim] = attention of packed queries: rows first[s]..first[s + 1] - 1 of q over rows first_k[s]..first_k[s + 1] - 1 (the same, without
+        first_k) of k and v [keys][kv_heads][head_dim]; lse [tokens][heads] fp32 is written if there is one."""
+        if q.dim() != 3 or k.dim() != 3:
+            raise ValueError("q is %s, k %s, not (tokens, heads, head_dim)" % (tuple(q.shape), tuple(k.shape)))
+        if not q.dtype == k.dtype == v.dtype == y.dtype:
+            raise TypeError("q, k, v and y are of different types")
+        on, shape, keys = self._device, q.shape, (k.shape[0], k.shape[1], q.shape[2])
+        qp, qs, qh = _heads(q, "q", on, shape)
+        kp, ks, kh = _heads(k, "k", on, keys)
+        vp, vs, vh = _heads(v, "v", on, keys)
+        yp, ys, yh = _heads(y, "y", on, shape)
+        sequences = first.numel() - 1
+        try:
+            args = _pack_attend(qp, kp, vp, yp, _vector(lse, "lse", on, shape[0] * shape[1], "torch.float32"), _vector(first, "first", on, sequences + 1, "torch.int32"),
+                                _vector(first_k, "first_k", on, sequences + 1, "torch.int32"), qs, qh, ks, kh, vs, vh, ys, yh,
+                                shape[0], keys[0], sequences, shape[1], keys[1], shape[2], causal, window, _element_codes[q.dtype], scale)
+        except (struct.error, OverflowError) as e:
+            raise _refused(e, tokens=shape[0], keys=keys[0], sequences=sequences, window=window, scale=scale) from None
+        self._check(lib().cw_attend(self._h, args, _stream(stream)))
+
     def release(self, slot):
         self._check(lib().cw_release(self._h, slot))
 
@@ -600,7 +782,7 @@ class Context:
 
 
 __all__ = [n for n in dir() if n.startswith("CW_") or n.startswith("cw_")] + [
-    "Context", "CwError", "lib", "LIB_PATH", "SIGNATURES", "DTYPES", "CONV_TILES"]
+    "Cache", "Context", "CwError", "lib", "LIB_PATH", "SIGNATURES", "DTYPES", "CONV_TILES"]
 
 
 class Executors:

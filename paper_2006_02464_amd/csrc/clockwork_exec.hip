@@ -2,6 +2,7 @@
 #include "../../include/clockwork_exec_introspect.h"
 
 #include <algorithm>
+#include <array>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -1469,6 +1470,178 @@ int32_t cw_answer(cw_ctx *c, const cw_answer_args *r, void *stream) {
     DeviceGuard g(c->device);
     if (!g.ok) return hip_fail(c, hipGetLastError(), "hipSetDevice");
     CW_HIP(c, launch_answer(a, static_cast<hipStream_t>(stream)));
+    return CW_OK;
+}
+
+// Whether no element of [n0][n1][n2][inner] is at the place of another, for strides that nest in some order.
+static bool apart(std::array<std::pair<int64_t, int64_t>, 3> dims, __int128 inner) {
+    std::sort(dims.begin(), dims.end(), [](auto &a, auto &b) { return a.second < b.second; });
+    for (auto [size, stride] : dims) {
+        if (size <= 1) continue;
+        if (stride < inner) return false;
+        inner += (__int128)(size - 1) * stride;
+    }
+    return true;
+}
+
+constexpr int64_t kMostStride = (int64_t)1 << 40;
+// Rows of [tokens][heads][head_dim]: 16 bytes divide their addresses.
+static const char *rows_refusal(const void *p, int64_t stride, int64_t head_stride, int64_t tokens, int64_t heads, int32_t dim, int32_t size, bool written) {
+    if (!p) return "null pointer";
+    const int64_t step = 16 / size;
+    if (stride < 0 || head_stride < 0 || stride > kMostStride || head_stride > kMostStride || (tokens > 1 && stride % step != 0) || (heads > 1 && head_stride % step != 0)) return "bad stride";
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return "misaligned pointer";
+    if (written && !apart({{{tokens, stride}, {heads, head_stride}, {1, 0}}}, dim)) return "rows that are written overlap";
+    return nullptr;
+}
+
+static int32_t head_dim_checks(cw_ctx *c, int32_t head_dim) {
+    if (head_dim < 1) return set_err(c, CW_ERR_INVALID, "bad size");
+    if (head_dim % 16 != 0 || head_dim > kAttendMostDim) return set_err(c, CW_ERR_UNSUPPORTED, "head_dim must be a multiple of 16 up to 256");
+    return CW_OK;
+}
+
+// Checks a cache and takes it over.
+static int32_t cache_view(cw_ctx *c, const cw_cache *r, bool written, CacheView *out) {
+    if (!r) return set_err(c, CW_ERR_INVALID, "null cache");
+    if (r->dtype != DT_F16 && r->dtype != DT_BF16 && r->dtype != DT_E4M3) return set_err(c, CW_ERR_INVALID, "bad dtype of the cache");
+    if (r->pages < 0 || r->kv_heads < 1 || r->page < 1) return set_err(c, CW_ERR_INVALID, "bad size of the cache");
+    if (r->kv_heads > kAttendMostHeads) return set_err(c, CW_ERR_UNSUPPORTED, "too many heads");
+    if (r->page > kCacheMostPage || (r->page & (r->page - 1)) != 0) return set_err(c, CW_ERR_UNSUPPORTED, "a page holds a power of two of tokens, up to 4096");
+    const int32_t rc = head_dim_checks(c, r->head_dim);
+    if (rc != CW_OK) return rc;
+    const bool codes = r->dtype == DT_E4M3;
+    const int64_t step = codes ? 16 : 8;
+    if (r->page_stride < 0 || r->head_stride < 0 || r->token_stride < 0 || r->page_stride > kMostStride || r->head_stride > kMostStride || r->token_stride > kMostStride ||
+        (r->pages > 1 && r->page_stride % step != 0) || (r->kv_heads > 1 && r->head_stride % step != 0) || (r->page > 1 && r->token_stride % step != 0))
+        return set_err(c, CW_ERR_INVALID, "bad stride of the cache");
+    if (codes && (r->exp_page_stride < 0 || r->exp_head_stride < 0 || r->exp_token_stride < 0 || r->exp_page_stride > kMostStride || r->exp_head_stride > kMostStride || r->exp_token_stride > kMostStride))
+        return set_err(c, CW_ERR_INVALID, "bad stride of the cache's exponents");
+    if (codes != (r->k_exp != nullptr) || codes != (r->v_exp != nullptr)) return set_err(c, CW_ERR_INVALID, "a cache has exponents with CW_DTYPE_E4M3, and only then");
+    if (r->pages > 0) {
+        if (!r->k || !r->v) return set_err(c, CW_ERR_INVALID, "null pointer in the cache");
+        if (reinterpret_cast<uintptr_t>(r->k) % 16 != 0 || reinterpret_cast<uintptr_t>(r->v) % 16 != 0) return set_err(c, CW_ERR_INVALID, "misaligned pointer in the cache");
+        if (written && (!apart({{{r->pages, r->page_stride}, {r->kv_heads, r->head_stride}, {r->page, r->token_stride}}}, r->head_dim) ||
+                        (codes && !apart({{{r->pages, r->exp_page_stride}, {r->kv_heads, r->exp_head_stride}, {r->page, r->exp_token_stride}}}, 1))))
+            return set_err(c, CW_ERR_INVALID, "rows of the cache overlap");
+    }
+    int shift = 0;
+    while (1 << shift < r->page) ++shift;
+    *out = CacheView{r->k, r->v, r->k_exp, r->v_exp, r->page_stride, r->head_stride, r->token_stride, r->exp_page_stride, r->exp_head_stride, r->exp_token_stride,
+                     r->pages, r->kv_heads, shift, r->head_dim, (DType)r->dtype};
+    return CW_OK;
+}
+
+// What the calls over a cache refuse in common of their sequences.
+static int32_t sequence_checks(cw_ctx *c, int32_t sequences, int32_t table_pages, int64_t table_stride, const int32_t *table, const int32_t *lengths, int32_t page) {
+    if (sequences < 0 || table_pages < 0 || table_stride < 0 || table_stride > kMostStride) return set_err(c, CW_ERR_INVALID, "bad size");
+    if (sequences > kAttendMostSequences || (int64_t)table_pages * page > INT32_MAX) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
+    if (sequences > 0) {
+        if (!lengths || (table_pages > 0 && !table)) return set_err(c, CW_ERR_INVALID, "null pointer");
+        if (!aligned_to(lengths, DT_F32) || !aligned_to(table, DT_F32)) return set_err(c, CW_ERR_INVALID, "misaligned pointer");
+    }
+    return CW_OK;
+}
+
+static int32_t cache_rows(cw_ctx *c, const cw_cache_args *r, void *stream, bool write) {
+    if (!c) return CW_ERR_INVALID;
+    if (!r) return set_err(c, CW_ERR_INVALID, "null arguments");
+    CacheArgs a{};
+    int32_t rc = cache_view(c, r->cache, write, &a.cache);
+    if (rc != CW_OK) return rc;
+    if (!element_type(r->dtype)) return set_err(c, CW_ERR_INVALID, "bad dtype");
+    if (r->tokens < 0) return set_err(c, CW_ERR_INVALID, "bad size");
+    rc = sequence_checks(c, r->sequences, r->table_pages, r->table_stride, r->table, r->lengths, r->cache->page);
+    if (rc != CW_OK) return rc;
+    if (r->tokens > kAttendMostTokens) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
+    if (!r->first && r->tokens != r->sequences) return set_err(c, CW_ERR_INVALID, "without `first` there is a row for every sequence");
+    if (!aligned_to(r->first, DT_F32)) return set_err(c, CW_ERR_INVALID, "misaligned pointer");
+    if (r->tokens > 0 && r->sequences > 0) {
+        const int32_t size = r->dtype == DT_F32 ? 4 : 2;
+        const char *why = rows_refusal(r->k, r->k_stride, r->k_head_stride, r->tokens, a.cache.kv_heads, a.cache.head_dim, size, !write);
+        if (!why) why = rows_refusal(r->v, r->v_stride, r->v_head_stride, r->tokens, a.cache.kv_heads, a.cache.head_dim, size, !write);
+        if (why) return set_err(c, CW_ERR_INVALID, why);
+    }
+    if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
+    if (r->tokens == 0 || r->sequences == 0) return CW_OK;
+    a.k = r->k; a.v = r->v; a.first = r->first; a.lengths = r->lengths; a.table = r->table;
+    a.k_stride = r->k_stride; a.k_head_stride = r->k_head_stride; a.v_stride = r->v_stride; a.v_head_stride = r->v_head_stride; a.table_stride = r->table_stride;
+    a.tokens = r->tokens; a.sequences = r->sequences; a.table_pages = r->table_pages; a.dtype = (DType)r->dtype;
+    DeviceGuard g(c->device);
+    if (!g.ok) return hip_fail(c, hipGetLastError(), "hipSetDevice");
+    if (write) CW_HIP(c, launch_cache_write(a, static_cast<hipStream_t>(stream)));
+    else CW_HIP(c, launch_cache_read(a, static_cast<hipStream_t>(stream)));
+    return CW_OK;
+}
+
+int32_t cw_cache_write(cw_ctx *c, const cw_cache_args *r, void *stream) { return cache_rows(c, r, stream, true); }
+int32_t cw_cache_read(cw_ctx *c, const cw_cache_args *r, void *stream) { return cache_rows(c, r, stream, false); }
+
+// What both attentions refuse of their heads, type, window and scale.
+static int32_t attention_checks(cw_ctx *c, int32_t heads, int32_t kv_heads, int32_t dtype, int32_t window, float scale) {
+    if (dtype != DT_F16 && dtype != DT_BF16) return set_err(c, CW_ERR_INVALID, "bad dtype");
+    if (kv_heads < 1 || heads < 1 || heads % kv_heads != 0) return set_err(c, CW_ERR_INVALID, "heads must be a multiple of kv_heads");
+    if (heads > kAttendMostHeads) return set_err(c, CW_ERR_UNSUPPORTED, "too many heads");
+    if (window < 0) return set_err(c, CW_ERR_INVALID, "bad window");
+    if (!std::isfinite(scale)) return set_err(c, CW_ERR_INVALID, "scale must be finite");
+    return CW_OK;
+}
+
+size_t cw_attend_one_workspace_bytes(void) { return attend_one_workspace_bytes(); }
+
+int32_t cw_attend_one(cw_ctx *c, const cw_attend_one_args *r, void *stream) {
+    if (!c) return CW_ERR_INVALID;
+    if (!r) return set_err(c, CW_ERR_INVALID, "null arguments");
+    AttendOneArgs a{};
+    int32_t rc = cache_view(c, r->cache, false, &a.cache);
+    if (rc == CW_OK) rc = attention_checks(c, r->heads, a.cache.kv_heads, r->dtype, r->window, r->scale);
+    if (rc == CW_OK) rc = sequence_checks(c, r->sequences, r->table_pages, r->table_stride, r->table, r->lengths, r->cache->page);
+    if (rc != CW_OK) return rc;
+    if (a.cache.dtype != DT_E4M3 && a.cache.dtype != r->dtype) return set_err(c, CW_ERR_INVALID, "the cache has another dtype");
+    if (r->sequences > 0) {
+        const char *why = rows_refusal(r->q, r->q_stride, r->q_head_stride, r->sequences, r->heads, a.cache.head_dim, 2, false);
+        if (!why) why = rows_refusal(r->y, r->y_stride, r->y_head_stride, r->sequences, r->heads, a.cache.head_dim, 2, true);
+        if (why) return set_err(c, CW_ERR_INVALID, why);
+        if (!aligned_to(r->lse, DT_F32) || reinterpret_cast<uintptr_t>(r->workspace) % 16 != 0) return set_err(c, CW_ERR_INVALID, "misaligned pointer");
+    }
+    if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
+    if (r->sequences == 0) return CW_OK;
+    a.q = r->q; a.y = r->y; a.lse = r->lse; a.lengths = r->lengths; a.table = r->table;
+    a.workspace = r->workspace; a.workspace_bytes = r->workspace ? r->workspace_bytes : 0;
+    a.q_stride = r->q_stride; a.q_head_stride = r->q_head_stride; a.y_stride = r->y_stride; a.y_head_stride = r->y_head_stride; a.table_stride = r->table_stride;
+    a.sequences = r->sequences; a.heads = r->heads; a.table_pages = r->table_pages; a.window = r->window; a.dtype = (DType)r->dtype; a.scale = r->scale;
+    DeviceGuard g(c->device);
+    if (!g.ok) return hip_fail(c, hipGetLastError(), "hipSetDevice");
+    CW_HIP(c, launch_attend_one(a, static_cast<hipStream_t>(stream)));
+    return CW_OK;
+}
+
+int32_t cw_attend(cw_ctx *c, const cw_attend_args *r, void *stream) {
+    if (!c) return CW_ERR_INVALID;
+    if (!r) return set_err(c, CW_ERR_INVALID, "null arguments");
+    int32_t rc = attention_checks(c, r->heads, r->kv_heads, r->dtype, r->window, r->scale);
+    if (rc == CW_OK) rc = head_dim_checks(c, r->head_dim);
+    if (rc != CW_OK) return rc;
+    if (r->causal != 0 && r->causal != 1) return set_err(c, CW_ERR_INVALID, "causal must be 0 or 1");
+    if (r->window > 0 && !r->causal) return set_err(c, CW_ERR_INVALID, "a window goes with `causal` only");
+    if (r->tokens < 0 || r->keys < 0 || r->sequences < 0) return set_err(c, CW_ERR_INVALID, "bad size");
+    if (r->tokens > kAttendMostTokens || r->keys > kAttendMostTokens || r->sequences > kAttendMostSequences) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
+    if (r->tokens > 0 && r->sequences > 0) {
+        const char *why = rows_refusal(r->q, r->q_stride, r->q_head_stride, r->tokens, r->heads, r->head_dim, 2, false);
+        if (!why) why = rows_refusal(r->y, r->y_stride, r->y_head_stride, r->tokens, r->heads, r->head_dim, 2, true);
+        if (!why && r->keys > 0) why = rows_refusal(r->k, r->k_stride, r->k_head_stride, r->keys, r->kv_heads, r->head_dim, 2, false);
+        if (!why && r->keys > 0) why = rows_refusal(r->v, r->v_stride, r->v_head_stride, r->keys, r->kv_heads, r->head_dim, 2, false);
+        if (!why && !r->first) why = "null pointer";
+        if (!why && (!aligned_to(r->lse, DT_F32) || !aligned_to(r->first, DT_F32) || !aligned_to(r->first_k, DT_F32))) why = "misaligned pointer";
+        if (why) return set_err(c, CW_ERR_INVALID, why);
+    }
+    if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
+    if (r->tokens == 0 || r->sequences == 0) return CW_OK;
+    AttendArgs a{r->q, r->k, r->v, r->y, r->lse, r->first, r->first_k ? r->first_k : r->first, r->q_stride, r->q_head_stride, r->k_stride, r->k_head_stride, r->v_stride, r->v_head_stride,
+                 r->y_stride, r->y_head_stride, r->tokens, r->keys, r->sequences, r->heads, r->kv_heads, r->head_dim, r->causal, r->window, (DType)r->dtype, r->scale};
+    DeviceGuard g(c->device);
+    if (!g.ok) return hip_fail(c, hipGetLastError(), "hipSetDevice");
+    CW_HIP(c, launch_attend(a, static_cast<hipStream_t>(stream)));
     return CW_OK;
 }
 

@@ -10,7 +10,7 @@ namespace cw {
 typedef _Float16 f16;
 typedef __bf16 bf16;
 
-enum DType : int32_t { DT_F16 = 0, DT_BF16 = 1, DT_F32 = 2 };   // DT_F32: Fc4Args and AnswerArgs only
+enum DType : int32_t { DT_F16 = 0, DT_BF16 = 1, DT_F32 = 2, DT_E4M3 = 3 };   // the last two: single operators only
 
 // Kernel families (cw_launch_info.kind).
 enum Kind : int32_t {
@@ -346,6 +346,49 @@ struct AnswerArgs {
     DType dtype;
     float scale;
 };
+// A paged cache and what is written to, read from and looked at in it (kernels_cache.hip, kernels_attend_one.hip); the fields are those of cw_cache,
+// cw_cache_args and cw_attend_one_args.
+struct CacheView {
+    void *k, *v;
+    uint8_t *k_exp, *v_exp;
+    int64_t page_stride, head_stride, token_stride, exp_page_stride, exp_head_stride, exp_token_stride;
+    int32_t pages, kv_heads, page_shift, head_dim;
+    DType dtype;
+};
+struct CacheArgs {
+    CacheView cache;
+    void *k, *v;
+    const int32_t *first, *lengths, *table;
+    int64_t k_stride, k_head_stride, v_stride, v_head_stride, table_stride;
+    int32_t tokens, sequences, table_pages;
+    DType dtype;
+};
+struct AttendOneArgs {
+    CacheView cache;
+    const void *q;
+    void *y;
+    float *lse;
+    const int32_t *lengths, *table;
+    void *workspace;
+    size_t workspace_bytes;
+    int64_t q_stride, q_head_stride, y_stride, y_head_stride, table_stride;
+    int32_t sequences, heads, table_pages, window;
+    DType dtype;
+    float scale;
+};
+// Attention of packed prompts (kernels_attend.hip); the fields are those of cw_attend_args.
+struct AttendArgs {
+    const void *q, *k, *v;
+    void *y;
+    float *lse;
+    const int32_t *first, *first_k;
+    int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride, y_stride, y_head_stride;
+    int32_t tokens, keys, sequences, heads, kv_heads, head_dim, causal, window;
+    DType dtype;
+    float scale;
+};
+constexpr int kAttendMostDim = 256, kCacheMostPage = 4096, kAttendMostSequences = 1 << 20, kAttendMostHeads = 1 << 12, kAttendMostTokens = 1 << 24;
+
 constexpr int kAnswerMostTop = 64, kAnswerMostClasses = 1 << 24, kAnswerMostRows = 1 << 23;
 
 // Tile shapes the conv kernel is instantiated for (fixed at plan time per layer).
@@ -511,6 +554,11 @@ hipError_t launch_fc4(const Fc4Args &a, hipStream_t s);
 void fc4_grid(const Fc4Args &a, dim3 *grid, int *block);   // of that launch
 hipError_t launch_answer(const AnswerArgs &a, hipStream_t s);
 size_t answer_workspace_bytes();
+hipError_t launch_cache_write(const CacheArgs &a, hipStream_t s);
+hipError_t launch_cache_read(const CacheArgs &a, hipStream_t s);
+hipError_t launch_attend_one(const AttendOneArgs &a, hipStream_t s);
+size_t attend_one_workspace_bytes();
+hipError_t launch_attend(const AttendArgs &a, hipStream_t s);
 // debug read-back: NHWC storage type (ld elements per pixel) -> fp32 NCHW
 hipError_t launch_nhwc_to_nchw_f32(DType dt, const void *src, float *dst, int B, int C, int H,
                                    int W, int ld, hipStream_t s);
