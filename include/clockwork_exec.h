@@ -416,7 +416,7 @@ size_t cw_attend_one_workspace_bytes(void);
  * first[0]..first[sequences] - 1 are not touched. */
 typedef struct {
     const void *q;              /* [tokens][heads][head_dim], dtype */
-    const void *k, *v;          /* [keys][kv_heads][head_dim], dtype */
+    const void *k, *v;          /* [keys][kv_heads][head_dim], dtype; rows at most 2^23 elements apart */
     void *y;                    /* [tokens][heads][head_dim], dtype */
     float *lse;                 /* [tokens][heads] or NULL */
     const int32_t *first;       /* [sequences + 1], not falling */

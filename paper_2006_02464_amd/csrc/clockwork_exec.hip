@@ -1635,10 +1635,12 @@ int32_t cw_attend(cw_ctx *c, const cw_attend_args *r, void *stream) {
         if (!why && (!aligned_to(r->lse, DT_F32) || !aligned_to(r->first, DT_F32) || !aligned_to(r->first_k, DT_F32))) why = "misaligned pointer";
         if (why) return set_err(c, CW_ERR_INVALID, why);
     }
+    if ((r->keys > 1 && (r->k_stride > kAttendMostStride || r->v_stride > kAttendMostStride)) || (int64_t)r->tokens * r->heads + (int64_t)r->sequences * r->kv_heads > INT32_MAX)
+        return set_err(c, CW_ERR_UNSUPPORTED, "too large");
     if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
     if (r->tokens == 0 || r->sequences == 0) return CW_OK;
     AttendArgs a{r->q, r->k, r->v, r->y, r->lse, r->first, r->first_k ? r->first_k : r->first, r->q_stride, r->q_head_stride, r->k_stride, r->k_head_stride, r->v_stride, r->v_head_stride,
-                 r->y_stride, r->y_head_stride, r->tokens, r->keys, r->sequences, r->heads, r->kv_heads, r->head_dim, r->causal, r->window, (DType)r->dtype, r->scale};
+                 r->y_stride, r->y_head_stride, r->tokens, r->keys, r->sequences, r->heads, r->kv_heads, r->head_dim, r->causal, r->window < r->keys ? r->window : 0, (DType)r->dtype, r->scale};   // no sequence has more keys
     DeviceGuard g(c->device);
     if (!g.ok) return hip_fail(c, hipGetLastError(), "hipSetDevice");
     CW_HIP(c, launch_attend(a, static_cast<hipStream_t>(stream)));

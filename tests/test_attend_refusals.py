@@ -133,7 +133,8 @@ def test_attend_one_lets_through(ctx):
     (dict(keys=-1), INVALID), (dict(sequences=-1), INVALID), (dict(tokens=(1 << 24) + 1), UNSUPPORTED), (dict(keys=(1 << 24) + 1), UNSUPPORTED), (dict(sequences=(1 << 20) + 1), UNSUPPORTED),
     (dict(heads=0), INVALID), (dict(heads=5), INVALID), (dict(kv_heads=0), INVALID), (dict(kv_heads=-2), INVALID), (dict(heads=4098), UNSUPPORTED), (dict(head_dim=0), INVALID), (dict(head_dim=72), UNSUPPORTED),
     (dict(head_dim=272), UNSUPPORTED), (dict(causal=2), INVALID), (dict(causal=-1), INVALID), (dict(window=-1), INVALID), (dict(causal=0, window=5), INVALID), (dict(dtype=2), INVALID), (dict(dtype=3), INVALID),
-    (dict(scale=float("inf")), INVALID), (dict(scale=float("nan")), INVALID), (dict(k_stride=(1 << 40) + 8), INVALID)])
+    (dict(scale=float("inf")), INVALID), (dict(scale=float("nan")), INVALID), (dict(k_stride=(1 << 40) + 8), INVALID),
+    (dict(k_stride=(1 << 23) + 8), UNSUPPORTED), (dict(v_stride=1 << 30), UNSUPPORTED), (dict(tokens=1 << 24, heads=128, y_stride=1 << 20, kv_heads=1), UNSUPPORTED)])
 def test_attend_refuses(ctx, change, status):
     st, why = refusal(ctx, "cw_attend", cw.cw_attend_args, PROMPT, change)
     assert st == status and (st, why) != PLANNING
@@ -141,7 +142,8 @@ def test_attend_refuses(ctx, change, status):
 
 @pytest.mark.parametrize("change", [{}, dict(lse=None, first_k=None), dict(tokens=0, q=None, y=None), dict(keys=0, k=None, v=None), dict(sequences=0, first=None), dict(causal=0), dict(window=7),
                                     dict(q_stride=0, k_stride=0, v_stride=0, k_head_stride=0), dict(y_stride=64, y_head_stride=448), dict(heads=4096, kv_heads=4096, y_stride=1 << 18), dict(scale=-1.0),
-                                    dict(dtype=1), dict(tokens=1, q_stride=1)])
+                                    dict(dtype=1), dict(tokens=1, q_stride=1), dict(k_stride=1 << 23, v_stride=1 << 23),
+                                    dict(q_stride=1 << 40), dict(keys=1, k_stride=1 << 40)])
 def test_attend_lets_through(ctx, change):
     assert refusal(ctx, "cw_attend", cw.cw_attend_args, PROMPT, change) == PLANNING
 

@@ -199,15 +199,15 @@ def test_strides(ctx, dtype):
 
 
 def test_rows_far_apart(ctx):
-    """Offsets beyond 32 bits, of elements and of bytes."""
-    q, k, v = data([3], [3], 2, 1, 64, F16, 4)
-    far = (1 << 30) + 64
-    store = torch.empty(far * 2 + 4096, dtype=F16, device="cuda")
-    views = [store.as_strided((3, h, 64), (far, 64, 1), storage_offset=at) for h, at in ((2, 0), (1, 128), (1, 192), (2, 256))]
+    """Offsets beyond 32 bits, of elements and of bytes: queries and results 2^30 elements apart, keys and values 2^23, as far as they may be."""
+    q, k, v = data([3, 0], [300, 3], 2, 1, 64, F16, 4)
+    far, near = (1 << 30) + 64, 1 << 23
+    store = torch.empty(max(far * 2, near * 303) + 4096, dtype=F16, device="cuda")
+    views = [store.as_strided((n, h, 64), (by, 64, 1), storage_offset=at) for n, h, by, at in ((3, 2, far, 0), (303, 1, near, 512), (303, 1, near, 576), (3, 2, far, 256))]
     for to, x in zip(views, (q, k, v)):
         to.copy_(x)
-    ctx.attend(*views, starts([3]).cuda(), 0.125, stream=stream())
-    assert_attention(views[3].cpu(), None, right(q, k, v, [3], [3], 0.125))
+    ctx.attend(*views, starts([3, 0]).cuda(), 0.125, first_k=starts([300, 3]).cuda(), stream=stream())
+    assert_attention(views[3].cpu(), None, right(q, k, v, [3, 0], [300, 3], 0.125))
 
 
 def test_results_of_parts_join(ctx):
