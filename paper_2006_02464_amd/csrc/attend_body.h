@@ -109,7 +109,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
 
     if (tiles > 0) load(0);
     for (int t = 0; t < tiles; ++t) {
-        wait_loads_and_barrier<0>();
+        wait_lds_loads_and_barrier<0>();   // this tile is there, and the reads of the one before, whose place the next one takes, are over
         if (t + 1 < tiles) load(t + 1);
         const int base = wg_low + t * kAttendKeys;
         if (base >= wave_high || base + kAttendKeys <= wave_low) continue;

@@ -1,0 +1,12 @@
+// Attention of one new token over a paged cache, queries in bf16.
+#include <algorithm>
+
+#include "attend_one_body.h"
+
+namespace cw {
+
+hipError_t launch_attend_one_bf16(const AttendOneArgs &a, hipStream_t s) {
+    return a.cache.dtype == DT_E4M3 ? launch_attend_one_typed<bf16, true>(a, s) : launch_attend_one_typed<bf16, false>(a, s);
+}
+
+}  // namespace cw

@@ -12,6 +12,14 @@ static __device__ __forceinline__ void load_to_lds(u32x4 desc, unsigned voff, un
                  : "memory", "m0");
 }
 
+// The same from an address of each lane's own, and a byte, zero-extended to four, to lds_addr + 4*lane.
+static __device__ __forceinline__ void load_to_lds(const void *from, unsigned lds_addr) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(from) : "memory", "m0");
+}
+static __device__ __forceinline__ void load_byte_to_lds(const void *from, unsigned lds_addr) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off" : : "s"(lds_addr), "v"(from) : "memory", "m0");
+}
+
 // Waits until at most N of this thread's loads are outstanding, then the workgroup barrier.
 template <int N>
 static __device__ __forceinline__ void wait_loads_and_barrier() {

@@ -31,8 +31,8 @@ def stream():
 
 
 def p_step(x, kept):
-    """Of a weight in the second product: 11 bits, of bf16 16."""
-    return 2.0 ** -11 if kept == E4M3 or x == F16 else 2.0 ** -16
+    """Of a weight in the second product: 11 bits; of bf16 two parts, the second at most 2^-7 of the first (one bf16 step of it) and off by 2^-8 of itself: 2^-15."""
+    return 2.0 ** -11 if kept == E4M3 or x == F16 else 2.0 ** -15
 
 
 def queries(n, heads, dim, dtype, seed, by=1.0):
