@@ -8,61 +8,67 @@
 namespace cw {
 
 // A workgroup takes kAttendRows rows of one key head, a row being a query of one of the `each` heads that share it (query row / each): heads share the keys that a workgroup loads, and few
-// queries of many heads fill it.  Its waves take 32 rows each and walk the keys that any of these sees, kAttendKeys at a time.  Both products are transposed,
+// queries of many heads fill it.  Its waves take 32 rows each and walk the keys that any of these sees, a tile of 64 or 32 at a time.  Both products are transposed,
 // S^T = K Q^T and O^T = V^T P^T: in an accumulator of the matrix cores a lane has one row of the attention and 4 (lane / 32) + 8 j + 0..3 of the other side, so
 // maxima and sums of the softmax are a lane's own but for one exchange, and the eight numbers that a lane holds of S^T are those that the second product wants of P^T once it
 // takes its keys in that order.  K lies in LDS as it is, V too and is transposed by the reads of LDS that do that.
 // The running maximum follows the scores only where one is 2^8 times above it: weights may be up to 2^8, which costs none of their bits, and most tiles rescale nothing.
-constexpr int kAttendKeys = 64, kAttendWaves = 4, kAttendRows = 32 * kAttendWaves;
+constexpr int kAttendWaves = 4, kAttendRows = 32 * kAttendWaves;
+constexpr int attend_keys(int dp) { return dp <= 128 ? 64 : 32; }   // so that two workgroups fit a CU, by registers (Q and O take 12 dp / 8 a lane) and by LDS
 constexpr float kAttendSlack = 8.f;
 
 struct AttendKernel {
     AttendArgs a;
-    FastDiv each;      // heads that share a key head
-    int32_t group;
+    FastDiv each, kv_heads;
+    int32_t group;     // heads that share a key head
+    int32_t tiles;     // workgroups of a key head
     float c;           // |scale| / ln 2
 };
 
-template <typename T>
-struct Half;
-template <>
-struct Half<f16> {
-    static constexpr unsigned short EXP = 0x7c00;
-};
-template <>
-struct Half<bf16> {
-    static constexpr unsigned short EXP = 0x7f80;
-};
-
 template <typename T, int DP>
-__global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_kernel(const AttendKernel f) {
+__global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const AttendKernel f) {
     typedef typename Mfma<T>::v8 v8;
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) unsigned char lds_char;
-    constexpr int PANELS = DP / 32, PANEL = kAttendKeys * 64, PART = PANELS * PANEL, STAGE = 2 * PART;   // bytes; a panel: 32 numbers of every key, 64 bytes each
+    constexpr int KEYS = attend_keys(DP), BLOCKS = KEYS / 32;
+    constexpr int PANELS = DP / 32, PANEL = KEYS * 64, PART = PANELS * PANEL, STAGE = 2 * PART;   // bytes; a panel: 32 numbers of every key, 64 bytes each
     __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGE];
     const AttendArgs &a = f.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
-    const int kvh = blockIdx.x % a.kv_heads, tile_id = gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads;   // the last queries, which see the most keys, first
-    auto row_of = [&](const int32_t *first, int i, int most) { const int r = first[i]; return r < 0 ? 0 : r > most ? most : r; };
-    auto tile_of = [&](int i) { return (int64_t)row_of(a.first, i, a.tokens) * f.group / kAttendRows + i; };
-    const int s = last_not_above(a.sequences, tile_id, tile_of);
-    const int q0 = row_of(a.first, s, a.tokens), n = row_of(a.first, s + 1, a.tokens) - q0;
-    const int k0 = row_of(a.first_k, s, a.keys), m = max(0, row_of(a.first_k, s + 1, a.keys) - k0);
-    const int64_t row0_64 = (tile_id - tile_of(s)) * kAttendRows, rows_64 = (int64_t)n * f.group;
-    if (n <= 0 || row0_64 < 0 || row0_64 >= rows_64) return;
-    // From the tile's first query on rows fit 32 bits.
-    const int i0 = (int)(row0_64 / f.group), r0 = (int)(row0_64 - (int64_t)i0 * f.group);
-    const int rows = (int)min((int64_t)kAttendRows, rows_64 - row0_64), behind = m - n;
-    auto query_of = [&](int r) { return i0 + (int)fast_div((unsigned)(r0 + min(r, rows - 1)), f.each); };   // of row r of the tile
-    auto high_of = [&](int i) { return a.causal ? max(0, i + behind + 1) : m; };                             // keys [low, high) are what query i sees
+    const int block = fast_div(blockIdx.x, f.kv_heads), kvh = blockIdx.x - block * a.kv_heads, tile_id = f.tiles - 1 - block;   // the last queries, which see the most keys, first
+
+    // The tile's sequence.  Tile tile_of(s) is the first of sequence s: tiles are counted as if the sequences' rows were one behind the other, and one more a sequence.
+    int s, q0, q1, k0, k1;
+    auto clamped = [](int r, int most) { return r < 0 ? 0 : r > most ? most : r; };
+    if (a.sequences < 64) {
+        const int at = min(lane, a.sequences), mine = clamped(a.first[at], a.tokens), mine_k = clamped(a.first_k[at], a.keys);
+        s = max(0, __popcll(__ballot(lane < a.sequences && mine * f.group / kAttendRows + lane <= tile_id)) - 1);
+        q0 = __builtin_amdgcn_readlane(mine, s);
+        q1 = __builtin_amdgcn_readlane(mine, s + 1);
+        k0 = __builtin_amdgcn_readlane(mine_k, s);
+        k1 = __builtin_amdgcn_readlane(mine_k, s + 1);
+    } else {
+        s = last_not_above(a.sequences, tile_id, [&](int i) { return (int64_t)(clamped(a.first[i], a.tokens) * f.group / kAttendRows + i); });
+        q0 = clamped(a.first[s], a.tokens);
+        q1 = clamped(a.first[s + 1], a.tokens);
+        k0 = clamped(a.first_k[s], a.keys);
+        k1 = clamped(a.first_k[s + 1], a.keys);
+    }
+    const int n = q1 - q0, m = max(0, k1 - k0), row0 = (tile_id - (q0 * f.group / kAttendRows + s)) * kAttendRows;
+    if (n <= 0 || row0 < 0 || row0 >= n * f.group) return;
+    const int rows = min(kAttendRows, n * f.group - row0), behind = m - n;
+    auto query_of = [&](int r) { return (int)fast_div((unsigned)(row0 + min(r, rows - 1)), f.each); };   // of row r of the tile
+    auto high_of = [&](int i) { return a.causal ? max(0, i + behind + 1) : m; };                         // keys [low, high) are what query i sees
     auto low_of = [&](int i) { return a.window > 0 ? max(0, i + behind + 1 - a.window) : 0; };
-    const int my_row = wave * 32 + l32, my_query = query_of(my_row), my_head = kvh * f.group + (r0 + min(my_row, rows - 1)) - (my_query - i0) * f.group;
+    const int my_row = wave * 32 + l32, my_query = query_of(my_row), my_head = kvh * f.group + row0 + min(my_row, rows - 1) - my_query * f.group;
     const int my_low = low_of(my_query), my_high = high_of(my_query);
-    const int wg_low = low_of(i0), wg_high = high_of(query_of(kAttendRows - 1));
+    const int wg_low = low_of(query_of(0)), wg_high = high_of(query_of(kAttendRows - 1));
+    const int tiles = wg_high > wg_low ? (wg_high - wg_low + KEYS - 1) / KEYS : 0;
+    // Of this wave: tiles [begin, end) hold keys that some row sees, [all_begin, all_end) of them only such that all rows see.
     const int first_query = query_of(wave * 32), last_query = query_of(wave * 32 + 31);
-    const int wave_low = low_of(first_query), wave_high = high_of(last_query), all_low = low_of(last_query), all_high = high_of(first_query);
-    const int tiles = wg_high > wg_low ? (wg_high - wg_low + kAttendKeys - 1) / kAttendKeys : 0;
+    const int begin = (low_of(first_query) - wg_low) / KEYS, end = (high_of(last_query) - wg_low + KEYS - 1) / KEYS;
+    const int all_begin = (low_of(last_query) - wg_low + KEYS - 1) / KEYS, all_end = (high_of(first_query) - wg_low) / KEYS;
 
     // Q as the second operand; a negative scale is taken by its sign.
     const bool inside = my_row < rows;
@@ -81,20 +87,32 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
 
     // Loads: a wave's share of a tile is 16 rows of every panel of K and of V.  K's 16-byte chunks are exchanged within a panel's row by (row / 4) % 4, so that the 16 rows
     // that a read of an operand takes at once lie in different banks; four rows of V, 256 bytes, are read at once as they are.
-    const unsigned lds_base = (unsigned)(size_t)(lds_char *)lds;
-    const int ld_row = wave * 16 + (lane >> 2), ld_chunk = lane & 3, key_chunk = ld_chunk ^ ((ld_row >> 2) & 3);
+    const unsigned lds_base = (unsigned)(size_t)(lds_char *)lds + wave * 1024;   // loads follow one another through the panels, a KB each
+    const int ld_row = wave % (KEYS / 16) * 16 + (lane >> 2), ld_panel = wave / (KEYS / 16), ld_chunk = lane & 3, key_chunk = ld_chunk ^ ((ld_row >> 2) & 3);
     const unsigned k_off = (unsigned)ld_row * (unsigned)(a.k_stride * 2) + key_chunk * 16, v_off = (unsigned)ld_row * (unsigned)(a.v_stride * 2) + ld_chunk * 16;
     const char *k_at = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + (int64_t)(k0 + wg_low) * a.k_stride + kvh * a.k_head_stride);
     const char *v_at = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + (int64_t)(k0 + wg_low) * a.v_stride + kvh * a.v_head_stride);
-    auto load = [&](int t) {
-        const int left = min(kAttendKeys, m - wg_low - t * kAttendKeys);   // rows beyond the last key are out of the buffers: zeros
-        const u32x4 dk = make_desc(k_at + (int64_t)t * kAttendKeys * a.k_stride * 2, (unsigned)((left - 1) * a.k_stride + a.head_dim) * 2u);
-        const u32x4 dv = make_desc(v_at + (int64_t)t * kAttendKeys * a.v_stride * 2, (unsigned)((left - 1) * a.v_stride + a.head_dim) * 2u);
-        const unsigned to = lds_base + (t & 1) * STAGE + wave * 1024;
+    auto load = [&](int t) {   // tiles one after the other
+        const int left = min(KEYS, m - wg_low - t * KEYS);   // rows beyond the last key are out of the buffers: zeros
+        const u32x4 dk = make_desc(k_at, ((unsigned)(left - 1) * (unsigned)a.k_stride + a.head_dim) * 2u);
+        const u32x4 dv = make_desc(v_at, ((unsigned)(left - 1) * (unsigned)a.v_stride + a.head_dim) * 2u);
+        k_at += (unsigned)a.k_stride * (KEYS * 2u);
+        v_at += (unsigned)a.v_stride * (KEYS * 2u);
+        const unsigned to = lds_base + (t & 1) * STAGE;
 #pragma unroll
-        for (int p = 0; p < PANELS; ++p) load_to_lds(dk, p * 32 + key_chunk * 8 < a.head_dim ? k_off : kOob, p * 64, to + p * PANEL);
+        for (int j = 0; j < PART / (kAttendWaves * 1024); ++j) {
+            const int p = j * (64 / KEYS) + ld_panel;
+            load_to_lds(dk, p * 32 + key_chunk * 8 < a.head_dim ? k_off : kOob, p * 64, to + j * (kAttendWaves * 1024));
+        }
 #pragma unroll
-        for (int p = 0; p < PANELS; ++p) load_to_lds(dv, p * 32 + ld_chunk * 8 < a.head_dim ? v_off : kOob, p * 64, to + PART + p * PANEL);
+        for (int j = 0; j < PART / (kAttendWaves * 1024); ++j) {
+            const int p = j * (64 / KEYS) + ld_panel;
+            load_to_lds(dv, p * 32 + ld_chunk * 8 < a.head_dim ? v_off : kOob, p * 64, to + PART + j * (kAttendWaves * 1024));
+        }
+    };
+    auto next = [&](int t) {
+        wait_lds_loads_and_barrier<0>();   // tile t is there, and the reads of the one before, whose place the next one takes, are over
+        if (t + 1 < tiles) load(t + 1);
     };
 
     f32x16 o[PANELS];
@@ -107,35 +125,31 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
     const unsigned k_read[2] = {(unsigned)(l32 * 64 + ((half ^ key_swz) << 4)), (unsigned)(l32 * 64 + (((2 + half) ^ key_swz) << 4))};
     const unsigned v_read = PART + (4 * half + ((lane & 15) >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
 
-    if (tiles > 0) load(0);
-    for (int t = 0; t < tiles; ++t) {
-        wait_lds_loads_and_barrier<0>();   // this tile is there, and the reads of the one before, whose place the next one takes, are over
-        if (t + 1 < tiles) load(t + 1);
-        const int base = wg_low + t * kAttendKeys;
-        if (base >= wave_high || base + kAttendKeys <= wave_low) continue;
+    unsigned odd_left = 0, odd_right = 0;   // of the tiles with masks before and behind those without: 32 rows see at most two such on a side
+    auto work = [&](int t, auto masked) {
         const lds_char *stage = (const lds_char *)lds + (t & 1) * STAGE;
-        f32x16 x[2];
+        f32x16 x[BLOCKS];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < BLOCKS; ++b) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[b][e] = 0.f;
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i)
                 x[b] = Mfma<T>::mma(*reinterpret_cast<const __attribute__((address_space(3))) v8 *>(stage + k_read[i & 1] + (i >> 1) * PANEL + b * 2048), q[i], x[b]);
         }
-        const bool masked = base < all_low || base + kAttendKeys > all_high;
-        if (masked) {
+        const int base = wg_low + t * KEYS + 4 * half;
+        if constexpr (decltype(masked)::value) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int key = base + b * 32 + 8 * (e / 4) + 4 * half + e % 4;
+                    const int key = base + b * 32 + 8 * (e / 4) + e % 4;
                     if (key < my_low || key >= my_high) x[b][e] = -INFINITY;
                 }
         }
         float most = x[0][0];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) most = fmaxf(most, x[b][e]);
         {
@@ -153,9 +167,9 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
                 for (int e = 0; e < 16; ++e) o[p][e] *= by;
         }
         const float ref = top == -INFINITY ? 0.f : top;
-        v8 w[4];   // P^T, sixteen keys each
+        v8 w[2 * BLOCKS];   // P^T, sixteen keys each
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const float p = __builtin_amdgcn_exp2f(fmaf(x[b][e], f.c, -ref));
@@ -168,46 +182,97 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 512));
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
-        bool odd = false;   // whether a value of a masked tile is no number: its product with a weight of 0 is none either
-        if (masked) {
+        if constexpr (decltype(masked)::value) {
+            // A value that is no number, times a weight of 0, is none either.  Such values have the largest exponents; a tile that has some is left for later.
+            u16x2 largest = {0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 2 * BLOCKS; ++i)
 #pragma unroll
                 for (int p = 0; p < PANELS; ++p) {
-                    const auto v = values(i, p);
+                    const u32x4 v = __builtin_bit_cast(u32x4, values(i, p)) & 0x7fff7fffu;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) odd |= ((unsigned short)v[e] & Half<T>::EXP) == Half<T>::EXP;
-                }
-        }
-        if (__builtin_expect(__any(odd), 0)) {
-            // Key by key, and only into the rows that see it.
-            for (int j = 0; j < kAttendKeys; ++j) {
-                const bool mine = base + j >= my_low && base + j < my_high;
-                const int slot = (j & 3) + ((j >> 3) & 1) * 4, side = (j >> 2) & 1;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (j >> 4 != i) continue;
-#pragma unroll
-                    for (int p = 0; p < PANELS; ++p) {
-                        auto v = values(i, p);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (e != slot || half != side) v[e] = 0;
-                        f32x16 one;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) one[e] = 0.f;
-                        one = Mfma<T>::mma(__builtin_bit_cast(v8, v), w[i], one);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[p][e] += mine ? one[e] : 0.f;
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned two = v[e];   // not v[e] itself: the bits of an element of a vector come out as those of the first
+                        largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, two));
                     }
                 }
+            constexpr unsigned short none = std::is_same<T, f16>::value ? 0x7c00 : 0x7f80;
+            asm volatile("" ::: "memory");   // the values are read again where they are needed: as many registers are not there
+            if (__builtin_expect(__any(largest[0] >= none || largest[1] >= none), 0)) {
+                if (t < all_begin) odd_left |= 1u << (t - begin);
+                else odd_right |= 1u << (end - 1 - t);
+                return;
             }
-            continue;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2 * BLOCKS; ++i)
 #pragma unroll
             for (int p = 0; p < PANELS; ++p) o[p] = Mfma<T>::mma(__builtin_bit_cast(v8, values(i, p)), w[i], o[p]);
+    };
+
+    if (tiles > 0) load(0);
+    // The loop over tiles without masks has no other in it: what shares registers with it over a branch costs copies of them in every tile.
+    for (int t = 0; t < tiles;) {
+        if (t >= all_begin && t < all_end) {
+            do {
+                next(t);
+                work(t, std::false_type{});
+            } while (++t < all_end);
+        } else {
+            next(t);
+            if (t >= begin && t < end) work(t, std::true_type{});
+            ++t;
+        }
+    }
+
+    // What was left: weights once more, from memory, and the values key by key, into the rows that see it only.
+    for (int side = 0; side < 2; ++side) {
+        for (unsigned odd = side ? odd_right : odd_left; odd; odd &= odd - 1) {
+            const int at = __builtin_ctz(odd), t = side ? end - 1 - at : begin + at, base = wg_low + t * KEYS;
+            f32x16 x[BLOCKS];
+            v8 w[2 * BLOCKS];
+            const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                const int key = base + b * 32 + l32;
+                const T *from = static_cast<const T *>(a.k) + (int64_t)(k0 + min(key, m - 1)) * a.k_stride + kvh * a.k_head_stride + half * 8;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[b][e] = 0.f;
+#pragma unroll
+                for (int i = 0; i < DP / 16; ++i) {
+                    u32x4 v = {0u, 0u, 0u, 0u};
+                    if (i * 16 + half * 8 < a.head_dim) v = *reinterpret_cast<const u32x4 *>(from + i * 16);
+                    x[b] = Mfma<T>::mma(__builtin_bit_cast(v8, v), q[i], x[b]);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int mine = base + 4 * half + b * 32 + 8 * (e / 4) + e % 4;
+                    w[b * 2 + e / 8][e % 8] = (T)(mine < my_low || mine >= my_high ? 0.f : __builtin_amdgcn_exp2f(fmaf(x[b][e], f.c, -ref)));
+                }
+            }
+            for (int j = 0; j < KEYS && base + j < m; ++j) {
+                const int slot = (j & 3) + ((j >> 3) & 1) * 4;
+                const bool seen = base + j >= my_low && base + j < my_high, here = ((j >> 2) & 1) == half;
+                v8 weights = w[0];
+#pragma unroll
+                for (int i = 1; i < 2 * BLOCKS; ++i)
+                    if (j >> 4 == i) weights = w[i];
+                const T *from = static_cast<const T *>(a.v) + (int64_t)(k0 + base + j) * a.v_stride + kvh * a.v_head_stride + l32;
+#pragma unroll
+                for (int p = 0; p < PANELS; ++p) {
+                    const T value = here && p * 32 + l32 < a.head_dim ? from[p * 32] : (T)0.f;
+                    v8 v;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = e == slot ? value : (T)0.f;
+                    f32x16 one;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) one[e] = 0.f;
+                    one = Mfma<T>::mma(v, weights, one);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[p][e] += seen ? one[e] : 0.f;
+                }
+            }
+        }
     }
 
     {
@@ -232,19 +297,19 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
                 hi[e] = (T)(empty ? 0.f : o[p][8 * g + 4 + e] * by);
             }
             const u32x2 lo2 = __builtin_bit_cast(u32x2, lo), hi2 = __builtin_bit_cast(u32x2, hi);
-            const auto r0s = __builtin_amdgcn_permlane32_swap(lo2[0], hi2[0], false, false);
-            const auto r1s = __builtin_amdgcn_permlane32_swap(lo2[1], hi2[1], false, false);
+            const auto first2 = __builtin_amdgcn_permlane32_swap(lo2[0], hi2[0], false, false);
+            const auto second2 = __builtin_amdgcn_permlane32_swap(lo2[1], hi2[1], false, false);
             const int d = p * 32 + g * 16 + half * 8;
-            if (d < a.head_dim) *reinterpret_cast<u32x4 *>(to + d) = u32x4{(unsigned)r0s[0], (unsigned)r1s[0], (unsigned)r0s[1], (unsigned)r1s[1]};
+            if (d < a.head_dim) *reinterpret_cast<u32x4 *>(to + d) = u32x4{(unsigned)first2[0], (unsigned)second2[0], (unsigned)first2[1], (unsigned)second2[1]};
         }
 }
 
 template <typename T>
 hipError_t launch_attend_typed(const AttendArgs &a, hipStream_t s) {
-    AttendKernel f{a, make_fast_div((uint32_t)(a.heads / a.kv_heads)), a.heads / a.kv_heads, fminf(fmaxf(fabsf(a.scale) * 1.44269504f, 1e-37f), 3e38f)};
-    const int64_t grid = ((int64_t)a.tokens * f.group / kAttendRows + a.sequences) * a.kv_heads;
-    if (grid > INT32_MAX || a.head_dim % 16 != 0 || a.head_dim > kAttendMostDim) return hipErrorInvalidValue;
-    const dim3 g((unsigned)grid), b(64 * kAttendWaves);
+    if (a.head_dim % 16 != 0 || a.head_dim > kAttendMostDim || (int64_t)a.tokens * a.heads + (int64_t)a.sequences * a.kv_heads > INT32_MAX) return hipErrorInvalidValue;
+    const int group = a.heads / a.kv_heads, tiles = a.tokens * group / kAttendRows + a.sequences;
+    const AttendKernel f{a, make_fast_div((uint32_t)group), make_fast_div((uint32_t)a.kv_heads), group, tiles, fminf(fmaxf(fabsf(a.scale) * 1.44269504f, 1e-37f), 3e38f)};
+    const dim3 g((unsigned)tiles * a.kv_heads), b(64 * kAttendWaves);
     if (a.head_dim <= 64) attend_kernel<T, 64><<<g, b, 0, s>>>(f);
     else if (a.head_dim <= 96) attend_kernel<T, 96><<<g, b, 0, s>>>(f);
     else if (a.head_dim <= 128) attend_kernel<T, 128><<<g, b, 0, s>>>(f);
