@@ -7,14 +7,16 @@
 
 namespace cw {
 
-// A workgroup takes kAttendRows rows of one key head, a row being a query of one of the `each` heads that share it (query row / each): heads share the keys that a workgroup loads, and few
-// queries of many heads fill it.  Its waves take 32 rows each and walk the keys that any of these sees, a tile of 64 or 32 at a time.  Both products are transposed,
+// A workgroup takes up to 128 rows of one key head, a row being a query of one of the `each` heads that share it (query row / each): heads share the keys that a workgroup loads, and few
+// queries of many heads fill it.  Its waves take 32 rows each and walk the keys that any of these sees, a tile at a time.  Both products are transposed,
 // S^T = K Q^T and O^T = V^T P^T: in an accumulator of the matrix cores a lane has one row of the attention and 4 (lane / 32) + 8 j + 0..3 of the other side, so
 // maxima and sums of the softmax are a lane's own but for one exchange, and the eight numbers that a lane holds of S^T are those that the second product wants of P^T once it
 // takes its keys in that order.  K lies in LDS as it is, V too and is transposed by the reads of LDS that do that.
 // The running maximum follows the scores only where one is 2^8 times above it: weights may be up to 2^8, which costs none of their bits, and most tiles rescale nothing.
-constexpr int kAttendWaves = 4, kAttendRows = 32 * kAttendWaves;
-constexpr int attend_keys(int dp) { return dp <= 128 ? 64 : 32; }   // so that two workgroups fit a CU, by registers (Q and O take 12 dp / 8 a lane) and by LDS
+// Where the rows do not fill the GPU, SPLIT waves share 32 of them and take parts of each tile: their results meet in LDS at the end.
+constexpr int kAttendWaves = 4;
+constexpr int attend_rows(int split) { return 32 * kAttendWaves / split; }   // of a workgroup
+constexpr int kAttendKeys = 64;   // of a tile: two of them and their successors fit a CU's LDS up to 128 numbers a head
 constexpr float kAttendSlack = 8.f;
 
 struct AttendKernel {
@@ -25,13 +27,13 @@ struct AttendKernel {
     float c;           // |scale| / ln 2
 };
 
-template <typename T, int DP>
-__global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const AttendKernel f) {
+template <typename T, int DP, int SPLIT>
+__global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_kernel(const AttendKernel f) {
     typedef typename Mfma<T>::v8 v8;
-    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    typedef T T2 __attribute__((ext_vector_type(2)));
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) unsigned char lds_char;
-    constexpr int KEYS = attend_keys(DP), BLOCKS = KEYS / 32;
+    constexpr int ROWS = attend_rows(SPLIT), KEYS = kAttendKeys, BLOCKS = KEYS / (32 * SPLIT);   // BLOCKS of 32 keys of each tile are a wave's
     constexpr int PANELS = DP / 32, PANEL = KEYS * 64, PART = PANELS * PANEL, STAGE = 2 * PART;   // bytes; a panel: 32 numbers of every key, 64 bytes each
     __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGE];
     const AttendArgs &a = f.a;
@@ -43,30 +45,31 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const Atte
     auto clamped = [](int r, int most) { return r < 0 ? 0 : r > most ? most : r; };
     if (a.sequences < 64) {
         const int at = min(lane, a.sequences), mine = clamped(a.first[at], a.tokens), mine_k = clamped(a.first_k[at], a.keys);
-        s = max(0, __popcll(__ballot(lane < a.sequences && mine * f.group / kAttendRows + lane <= tile_id)) - 1);
+        s = max(0, __popcll(__ballot(lane < a.sequences && mine * f.group / ROWS + lane <= tile_id)) - 1);
         q0 = __builtin_amdgcn_readlane(mine, s);
         q1 = __builtin_amdgcn_readlane(mine, s + 1);
         k0 = __builtin_amdgcn_readlane(mine_k, s);
         k1 = __builtin_amdgcn_readlane(mine_k, s + 1);
     } else {
-        s = last_not_above(a.sequences, tile_id, [&](int i) { return (int64_t)(clamped(a.first[i], a.tokens) * f.group / kAttendRows + i); });
+        s = last_not_above(a.sequences, tile_id, [&](int i) { return (int64_t)(clamped(a.first[i], a.tokens) * f.group / ROWS + i); });
         q0 = clamped(a.first[s], a.tokens);
         q1 = clamped(a.first[s + 1], a.tokens);
         k0 = clamped(a.first_k[s], a.keys);
         k1 = clamped(a.first_k[s + 1], a.keys);
     }
-    const int n = q1 - q0, m = max(0, k1 - k0), row0 = (tile_id - (q0 * f.group / kAttendRows + s)) * kAttendRows;
+    const int n = q1 - q0, m = max(0, k1 - k0), row0 = (tile_id - (q0 * f.group / ROWS + s)) * ROWS;
     if (n <= 0 || row0 < 0 || row0 >= n * f.group) return;
-    const int rows = min(kAttendRows, n * f.group - row0), behind = m - n;
+    const int rows = min(ROWS, n * f.group - row0), behind = m - n;
     auto query_of = [&](int r) { return (int)fast_div((unsigned)(row0 + min(r, rows - 1)), f.each); };   // of row r of the tile
     auto high_of = [&](int i) { return a.causal ? max(0, i + behind + 1) : m; };                         // keys [low, high) are what query i sees
     auto low_of = [&](int i) { return a.window > 0 ? max(0, i + behind + 1 - a.window) : 0; };
-    const int my_row = wave * 32 + l32, my_query = query_of(my_row), my_head = kvh * f.group + row0 + min(my_row, rows - 1) - my_query * f.group;
+    const int row_group = wave % (kAttendWaves / SPLIT), key_group = wave / (kAttendWaves / SPLIT);
+    const int my_row = row_group * 32 + l32, my_query = query_of(my_row), my_head = kvh * f.group + row0 + min(my_row, rows - 1) - my_query * f.group;
     const int my_low = low_of(my_query), my_high = high_of(my_query);
-    const int wg_low = low_of(query_of(0)), wg_high = high_of(query_of(kAttendRows - 1));
+    const int wg_low = low_of(query_of(0)), wg_high = high_of(query_of(ROWS - 1));
     const int tiles = wg_high > wg_low ? (wg_high - wg_low + KEYS - 1) / KEYS : 0;
     // Of this wave: tiles [begin, end) hold keys that some row sees, [all_begin, all_end) of them only such that all rows see.
-    const int first_query = query_of(wave * 32), last_query = query_of(wave * 32 + 31);
+    const int first_query = query_of(row_group * 32), last_query = query_of(row_group * 32 + 31);
     const int begin = (low_of(first_query) - wg_low) / KEYS, end = (high_of(last_query) - wg_low + KEYS - 1) / KEYS;
     const int all_begin = (low_of(last_query) - wg_low + KEYS - 1) / KEYS, all_end = (high_of(first_query) - wg_low) / KEYS;
 
@@ -76,19 +79,18 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const Atte
     {
         const T *from = static_cast<const T *>(a.q) + (int64_t)(q0 + my_query) * a.q_stride + (int64_t)my_head * a.q_head_stride + half * 8;
         const unsigned sign = a.scale < 0.f ? 0x80008000u : 0u;
+        u32x4 w[DP / 16];
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i) {
-            u32x4 w = {0u, 0u, 0u, 0u};
-            if (i * 16 + half * 8 < a.head_dim) w = *reinterpret_cast<const u32x4 *>(from + i * 16);
-            w ^= sign;
-            q[i] = __builtin_bit_cast(v8, w);
-        }
+        for (int i = 0; i < DP / 16; ++i) w[i] = *reinterpret_cast<const u32x4 *>(from + (i * 16 + half * 8 < a.head_dim ? i * 16 : -half * 8));
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) q[i] = __builtin_bit_cast(v8, i * 16 + half * 8 < a.head_dim ? w[i] ^ sign : u32x4{0u, 0u, 0u, 0u});
     }
 
-    // Loads: a wave's share of a tile is 16 rows of every panel of K and of V.  K's 16-byte chunks are exchanged within a panel's row by (row / 4) % 4, so that the 16 rows
+    // Loads: a wave takes 16 rows of a panel at a time, a KB.  K's 16-byte chunks are exchanged within a panel's row by (row / 4) % 4, so that the 16 rows
     // that a read of an operand takes at once lie in different banks; four rows of V, 256 bytes, are read at once as they are.
     const unsigned lds_base = (unsigned)(size_t)(lds_char *)lds + wave * 1024;   // loads follow one another through the panels, a KB each
-    const int ld_row = wave % (KEYS / 16) * 16 + (lane >> 2), ld_panel = wave / (KEYS / 16), ld_chunk = lane & 3, key_chunk = ld_chunk ^ ((ld_row >> 2) & 3);
+    static_assert(KEYS == 16 * kAttendWaves, "a wave loads the same rows of every panel");
+    const int ld_row = wave * 16 + (lane >> 2), ld_chunk = lane & 3, key_chunk = ld_chunk ^ ((ld_row >> 2) & 3);
     const unsigned k_off = (unsigned)ld_row * (unsigned)(a.k_stride * 2) + key_chunk * 16, v_off = (unsigned)ld_row * (unsigned)(a.v_stride * 2) + ld_chunk * 16;
     const char *k_at = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + (int64_t)(k0 + wg_low) * a.k_stride + kvh * a.k_head_stride);
     const char *v_at = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + (int64_t)(k0 + wg_low) * a.v_stride + kvh * a.v_head_stride);
@@ -100,15 +102,9 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const Atte
         v_at += (unsigned)a.v_stride * (KEYS * 2u);
         const unsigned to = lds_base + (t & 1) * STAGE;
 #pragma unroll
-        for (int j = 0; j < PART / (kAttendWaves * 1024); ++j) {
-            const int p = j * (64 / KEYS) + ld_panel;
-            load_to_lds(dk, p * 32 + key_chunk * 8 < a.head_dim ? k_off : kOob, p * 64, to + j * (kAttendWaves * 1024));
-        }
+        for (int p = 0; p < PANELS; ++p) load_to_lds(dk, p * 32 + key_chunk * 8 < a.head_dim ? k_off : kOob, p * 64, to + p * PANEL);
 #pragma unroll
-        for (int j = 0; j < PART / (kAttendWaves * 1024); ++j) {
-            const int p = j * (64 / KEYS) + ld_panel;
-            load_to_lds(dv, p * 32 + ld_chunk * 8 < a.head_dim ? v_off : kOob, p * 64, to + PART + j * (kAttendWaves * 1024));
-        }
+        for (int p = 0; p < PANELS; ++p) load_to_lds(dv, p * 32 + ld_chunk * 8 < a.head_dim ? v_off : kOob, p * 64, to + PART + p * PANEL);
     };
     auto next = [&](int t) {
         wait_lds_loads_and_barrier<0>();   // tile t is there, and the reads of the one before, whose place the next one takes, are over
@@ -122,8 +118,9 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const Atte
         for (int e = 0; e < 16; ++e) o[p][e] = 0.f;
     float top = -INFINITY, sum = 0.f;   // the maximum that weights refer to, in units of ln 2, and the sum of this lane's weights
     const int key_swz = (l32 >> 2) & 3;
-    const unsigned k_read[2] = {(unsigned)(l32 * 64 + ((half ^ key_swz) << 4)), (unsigned)(l32 * 64 + (((2 + half) ^ key_swz) << 4))};
-    const unsigned v_read = PART + (4 * half + ((lane & 15) >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    const unsigned mine = key_group * BLOCKS * 2048;   // this wave's keys in a panel
+    const unsigned k_read[2] = {mine + (unsigned)(l32 * 64 + ((half ^ key_swz) << 4)), mine + (unsigned)(l32 * 64 + (((2 + half) ^ key_swz) << 4))};
+    const unsigned v_read = PART + mine + (4 * half + ((lane & 15) >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
 
     unsigned odd_left = 0, odd_right = 0;   // of the tiles with masks before and behind those without: 32 rows see at most two such on a side
     auto work = [&](int t, auto masked) {
@@ -137,15 +134,18 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const Atte
             for (int i = 0; i < DP / 16; ++i)
                 x[b] = Mfma<T>::mma(*reinterpret_cast<const __attribute__((address_space(3))) v8 *>(stage + k_read[i & 1] + (i >> 1) * PANEL + b * 2048), q[i], x[b]);
         }
-        const int base = wg_low + t * KEYS + 4 * half;
         if constexpr (decltype(masked)::value) {
+            const int base = wg_low + t * KEYS + key_group * BLOCKS * 32;
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b)
+            for (int b = 0; b < BLOCKS; ++b) {
+                auto below = [&](int key) { return (unsigned)((1ull << min(max(key - base - b * 32, 0), 32)) - 1); };   // of the block's keys those below one, a bit each
+                const unsigned seen = (below(my_high) & ~below(my_low)) >> (4 * half);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int key = base + b * 32 + 8 * (e / 4) + e % 4;
-                    if (key < my_low || key >= my_high) x[b][e] = -INFINITY;
+                    const unsigned all = __builtin_amdgcn_sbfe(seen, 8 * (e / 4) + e % 4, 1), bits = __builtin_bit_cast(unsigned, (float)x[b][e]);
+                    x[b][e] = __builtin_bit_cast(float, (bits & all) | (0xff800000u & ~all));
                 }
+            }
         }
         float most = x[0][0];
 #pragma unroll
@@ -183,22 +183,22 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const Atte
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
         if constexpr (decltype(masked)::value) {
-            // A value that is no number, times a weight of 0, is none either.  Such values have the largest exponents; a tile that has some is left for later.
-            u16x2 largest = {0, 0};
+            // A value that is no number, times a weight of 0, is none either: 0 times all of them tells.  A tile that has some is left for later.
+            float odd = 0.f;
 #pragma unroll
             for (int i = 0; i < 2 * BLOCKS; ++i)
 #pragma unroll
                 for (int p = 0; p < PANELS; ++p) {
-                    const u32x4 v = __builtin_bit_cast(u32x4, values(i, p)) & 0x7fff7fffu;
+                    const u32x4 v = __builtin_bit_cast(u32x4, values(i, p));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const unsigned two = v[e];   // not v[e] itself: the bits of an element of a vector come out as those of the first
-                        largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, two));
+                        const unsigned two = v[e];   // not v[e] itself: of an element of a vector __builtin_bit_cast takes the first
+                        if constexpr (std::is_same<T, f16>::value) odd = __builtin_amdgcn_fdot2(__builtin_bit_cast(T2, two), T2{0, 0}, odd, false);
+                        else odd = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(T2, two), T2{0, 0}, odd, false);
                     }
                 }
-            constexpr unsigned short none = std::is_same<T, f16>::value ? 0x7c00 : 0x7f80;
             asm volatile("" ::: "memory");   // the values are read again where they are needed: as many registers are not there
-            if (__builtin_expect(__any(largest[0] >= none || largest[1] >= none), 0)) {
+            if (__builtin_expect(__any(odd != 0.f), 0)) {
                 if (t < all_begin) odd_left |= 1u << (t - begin);
                 else odd_right |= 1u << (end - 1 - t);
                 return;
@@ -216,6 +216,10 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const Atte
         if (t >= all_begin && t < all_end) {
             do {
                 next(t);
+                if constexpr (DP > 128) {   // what the vector registers do not hold stays in the others over the loop
+#pragma unroll
+                    for (int p = 0; p < PANELS; ++p) asm volatile("" : "+a"(o[p]));
+                }
                 work(t, std::false_type{});
             } while (++t < all_end);
         } else {
@@ -228,7 +232,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const Atte
     // What was left: weights once more, from memory, and the values key by key, into the rows that see it only.
     for (int side = 0; side < 2; ++side) {
         for (unsigned odd = side ? odd_right : odd_left; odd; odd &= odd - 1) {
-            const int at = __builtin_ctz(odd), t = side ? end - 1 - at : begin + at, base = wg_low + t * KEYS;
+            const int at = __builtin_ctz(odd), t = side ? end - 1 - at : begin + at, base = wg_low + t * KEYS + key_group * BLOCKS * 32;
             f32x16 x[BLOCKS];
             v8 w[2 * BLOCKS];
             const float ref = top == -INFINITY ? 0.f : top;
@@ -250,7 +254,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const Atte
                     w[b * 2 + e / 8][e % 8] = (T)(mine < my_low || mine >= my_high ? 0.f : __builtin_amdgcn_exp2f(fmaf(x[b][e], f.c, -ref)));
                 }
             }
-            for (int j = 0; j < KEYS && base + j < m; ++j) {
+            for (int j = 0; j < BLOCKS * 32 && base + j < m; ++j) {
                 const int slot = (j & 3) + ((j >> 3) & 1) * 4;
                 const bool seen = base + j >= my_low && base + j < my_high, here = ((j >> 2) & 1) == half;
                 v8 weights = w[0];
@@ -280,6 +284,39 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const Atte
         const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
         sum = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
     }
+    if constexpr (SPLIT > 1) {
+        // The waves that share rows meet: all but the first group leave theirs in LDS, lane by lane.
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        constexpr int BOX = (PANELS * 4 * 16 + 8) * 64;
+        static_assert((kAttendWaves - kAttendWaves / SPLIT) * BOX <= 2 * STAGE, "results fit where the tiles were");
+        auto box = [&](int group, int at) { return (__attribute__((address_space(3))) f32x4 *)((lds_char *)lds + ((group - 1) * (kAttendWaves / SPLIT) + row_group) * BOX + (at * 64 + lane) * 16); };
+        auto tail = [&](int group) { return (__attribute__((address_space(3))) float *)((lds_char *)lds + ((group - 1) * (kAttendWaves / SPLIT) + row_group) * BOX + PANELS * 4 * 1024 + lane * 8); };
+        wait_lds_loads_and_barrier<0>();
+        if (key_group > 0) {
+#pragma unroll
+            for (int p = 0; p < PANELS; ++p)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) *box(key_group, p * 4 + e) = f32x4{o[p][4 * e], o[p][4 * e + 1], o[p][4 * e + 2], o[p][4 * e + 3]};
+            tail(key_group)[0] = top;
+            tail(key_group)[1] = sum;
+        }
+        wait_lds_and_barrier();
+        if (key_group > 0) return;
+        for (int g = 1; g < SPLIT; ++g) {
+            const float other = tail(g)[0], now = fmaxf(top, other), ref = now == -INFINITY ? 0.f : now;
+            const float by = __builtin_amdgcn_exp2f(top - ref), by_other = __builtin_amdgcn_exp2f(other - ref);
+            top = now;
+            sum = sum * by + tail(g)[1] * by_other;
+#pragma unroll
+            for (int p = 0; p < PANELS; ++p)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x4 v = *box(g, p * 4 + e);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[p][4 * e + i] = o[p][4 * e + i] * by + v[i] * by_other;
+                }
+        }
+    }
     const bool empty = sum == 0.f;
     const float by = empty ? 0.f : 1.f / sum;
     if (!inside) return;
@@ -304,18 +341,31 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(const Atte
         }
 }
 
+template <typename T, int DP, int SPLIT>
+hipError_t launch_attend_as(const AttendArgs &a, hipStream_t s) {
+    const int group = a.heads / a.kv_heads, tiles = (int)((int64_t)a.tokens * group / attend_rows(SPLIT) + a.sequences);
+    const AttendKernel f{a, make_fast_div((uint32_t)group), make_fast_div((uint32_t)a.kv_heads), group, tiles, fminf(fmaxf(fabsf(a.scale) * 1.44269504f, 1e-37f), 3e38f)};
+    attend_kernel<T, DP, SPLIT><<<dim3((unsigned)tiles * a.kv_heads), dim3(64 * kAttendWaves), 0, s>>>(f);
+    return hipGetLastError();
+}
+
+template <typename T, int DP>
+hipError_t launch_attend_dim(const AttendArgs &a, hipStream_t s) {
+    // Waves share rows where there are few workgroups of 128: 500 queries of 32 heads over 8 of 128 bf16 (133 workgroups) 15.0 -> 11.8 us, eight prompts of 290 to 680 behind 215 keys, 8 heads (306)
+    // 33.2 -> 27.2; but four of 301 to 1024 behind 2500, 16 heads over 4 of 96 (347) 58 -> 65, 39 of 80 to 149, 8 heads over 4 (434) 13.5 -> 16.4.
+    const int64_t workgroups = (int64_t)a.tokens * a.heads / attend_rows(1) + (int64_t)a.sequences * a.kv_heads;
+    return workgroups <= 320 ? launch_attend_as<T, DP, 2>(a, s) : launch_attend_as<T, DP, 1>(a, s);
+}
+
 template <typename T>
 hipError_t launch_attend_typed(const AttendArgs &a, hipStream_t s) {
-    if (a.head_dim % 16 != 0 || a.head_dim > kAttendMostDim || (int64_t)a.tokens * a.heads + (int64_t)a.sequences * a.kv_heads > INT32_MAX) return hipErrorInvalidValue;
-    const int group = a.heads / a.kv_heads, tiles = a.tokens * group / kAttendRows + a.sequences;
-    const AttendKernel f{a, make_fast_div((uint32_t)group), make_fast_div((uint32_t)a.kv_heads), group, tiles, fminf(fmaxf(fabsf(a.scale) * 1.44269504f, 1e-37f), 3e38f)};
-    const dim3 g((unsigned)tiles * a.kv_heads), b(64 * kAttendWaves);
-    if (a.head_dim <= 64) attend_kernel<T, 64><<<g, b, 0, s>>>(f);
-    else if (a.head_dim <= 96) attend_kernel<T, 96><<<g, b, 0, s>>>(f);
-    else if (a.head_dim <= 128) attend_kernel<T, 128><<<g, b, 0, s>>>(f);
-    else if (a.head_dim <= 192) attend_kernel<T, 192><<<g, b, 0, s>>>(f);
-    else attend_kernel<T, 256><<<g, b, 0, s>>>(f);
-    return hipGetLastError();
+    if (a.head_dim % 16 != 0 || a.head_dim > kAttendMostDim || (int64_t)a.tokens * a.heads + (int64_t)a.sequences * a.kv_heads > INT32_MAX)
+        return hipErrorInvalidValue;
+    if (a.head_dim <= 64) return launch_attend_dim<T, 64>(a, s);
+    if (a.head_dim <= 96) return launch_attend_dim<T, 96>(a, s);
+    if (a.head_dim <= 128) return launch_attend_dim<T, 128>(a, s);
+    if (a.head_dim <= 192) return launch_attend_dim<T, 192>(a, s);
+    return launch_attend_dim<T, 256>(a, s);
 }
 
 }  // namespace cw
