@@ -8,25 +8,25 @@
 namespace cw {
 
 // Reading keys and values is what this costs: everything serves to keep enough of their bytes under way.  A workgroup takes up to 16 of the query heads that share a key head, and a part of a
-// sequence's tokens; its waves walk shares of that by themselves, 32 tokens a step, K and V of the next step on their way straight to the wave's own LDS while this one is worked on.
+// sequence's tokens; its waves walk shares of that by themselves, 32 tokens a step (16 of large rows), K and V of the next step on their way straight to the wave's own LDS while this one is worked on.
 // Products are transposed, on 16 x 16 tiles of the matrix cores: S^T = K Q^T, whose lanes have a query and tokens 4 (lane / 16) + 0..3 of each half of the step, just what the second product,
 // O^T = V^T P^T, wants of P^T with its tokens in that order; V is transposed by the reads of LDS that do that.  Tokens that are not seen come from a line of zeros.
 // Codes of 8 bits become numbers of the queries' type for the first product and fp16 for the second, exactly; a key's exponent goes to its score, a value's to its weight before that is rounded:
 // weights refer to a maximum of their own.  bf16 weights go into the second product in two parts.
-constexpr int kOneTokens = 32;
+constexpr int one_tokens(int row_bytes) { return row_bytes > 256 ? 16 : 32; }   // of a step: 16 KB at most
 constexpr int kOneHeads = 16;
 constexpr float kOneSlack = 8.f;   // maxima follow beyond 2^8
-constexpr int kOneMostParts = 64;
+constexpr int kOneMostParts = 64;   // a lane each where they meet
 constexpr int kOneCounters = 65536 / 4;
 
 struct AttendOneKernel {
     AttendOneArgs a;
     int32_t group, blocks;   // query heads of a key head, blocks of kOneHeads of them
-    int32_t parts;
+    FastDiv by_parts, by_kv_heads, by_blocks, by_chunks;   // chunks: 16 bytes of a head's results in fp32
+    int32_t parts, fewest;   // of a sequence at most, and steps that are worth one
     float c;                 // |scale| / ln 2
 };
 
-constexpr int one_waves(int row_bytes) { return row_bytes > 256 ? 2 : 4; }
 // Where 16-byte chunk c of row r lies: what is read at once lies in different banks.  K: 16 rows, one chunk; V: 8 rows, two chunks (16 bits) or rows 0..7 and 16..23, one (codes).
 template <int RB>
 __device__ static inline int k_key(int r) { return RB >= 256 ? r & 15 : RB == 128 ? (r >> 1) & 7 : (r >> 2) & 3; }
@@ -59,9 +59,15 @@ __device__ static inline float of_four(float v, F f) {
     return f(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
 }
 
+__device__ static inline float max3(float a, float b, float c) {   // as the instruction has it: a NaN loses
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // T: queries; CODES: pages of e4m3, else of T.  RB: bytes of a row in LDS, at least those of a head.
-template <typename T, bool CODES, int RB>
-__global__ __launch_bounds__(64 * one_waves(RB)) void attend_one_kernel(const AttendOneKernel f) {
+template <typename T, bool CODES, int RB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, RB / (CODES ? 1 : 2) <= 128 ? 2 : 1) void attend_one_kernel(const AttendOneKernel f) {
     typedef typename std::conditional<CODES, f16, T>::type VT;    // of the second product
     typedef typename Mfma<T>::v8 v8;
     typedef typename Mfma<VT>::v8 w8;
@@ -70,30 +76,28 @@ __global__ __launch_bounds__(64 * one_waves(RB)) void attend_one_kernel(const At
     typedef int i32x4 __attribute__((ext_vector_type(4)));
     typedef float f32x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) unsigned char lds_char;
-    constexpr int WAVES = one_waves(RB), THREADS = 64 * WAVES, SIZE = CODES ? 1 : 2, DP = RB / SIZE;
-    constexpr int PART = kOneTokens * RB, EXPS = CODES ? 256 : 0, STAGE = 2 * PART + EXPS, LOADS = PART / 1024;
+    constexpr int THREADS = 64 * WAVES, SIZE = CODES ? 1 : 2, DP = RB / SIZE, TOKENS = one_tokens(RB), HALVES = TOKENS / 16, STAGES = 2;
+    constexpr int PART = TOKENS * RB, EXPS = CODES ? 256 : 0, STAGE = 2 * PART + EXPS, LOADS = PART / 1024;
+    constexpr unsigned ALL = TOKENS == 32 ? 0xffffffffu : (1u << TOKENS) - 1u;
+    static_assert(!CODES || TOKENS == 32, "codes' exponents: a lane each of keys and of values");
     constexpr bool TWO = std::is_same<VT, bf16>::value;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * WAVES * STAGE];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[STAGES * WAVES * STAGE];
     __shared__ float tops[WAVES][kOneHeads], sums[WAVES][kOneHeads];
     __shared__ int last;
     const AttendOneArgs &a = f.a;
     const CacheView &c = a.cache;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quad = lane >> 4;
-    int b = blockIdx.x;
-    const int part = b % f.parts;
-    b /= f.parts;
-    const int item = b, kvh = b % c.kv_heads;
-    b /= c.kv_heads;
-    const int block = b % f.blocks, s = b / f.blocks;
+    const int item = fast_div(blockIdx.x, f.by_parts), part = blockIdx.x - item * f.parts;
+    const int below = fast_div(item, f.by_kv_heads), kvh = item - below * c.kv_heads, s = fast_div(below, f.by_blocks), block = below - s * f.blocks;
     const int heads = min(kOneHeads, f.group - block * kOneHeads), head0 = kvh * f.group + block * kOneHeads;
 
     const int full = max(a.lengths[s], 0), from = a.window > 0 ? max(0, full - a.window) : 0, len = min(full, a.table_pages << c.page_shift);
-    const int step0 = from / kOneTokens, steps = len > from ? (len + kOneTokens - 1) / kOneTokens - step0 : 0;
-    const int parts = max(1, min(f.parts, steps / (2 * WAVES)));   // as many as have two steps for every wave
+    const int step0 = from / TOKENS, steps = len > from ? (len + TOKENS - 1) / TOKENS - step0 : 0;
+    const int parts = max(1, min(f.parts, steps / f.fewest));
     if (part >= parts) return;
-    const int unit = part * WAVES + wave, units = parts * WAVES;
-    int step = step0 + (int)((int64_t)steps * unit / units);
-    const int end = step0 + (int)((int64_t)steps * (unit + 1) / units);
+    const int each = (int)((unsigned)(steps + parts * WAVES - 1) / (unsigned)(parts * WAVES));   // steps of a wave
+    int step = step0 + (part * WAVES + wave) * each;
+    const int end = min(step + each, step0 + steps);
 
     // Q as the second operand of the first product: with codes 16 numbers of a head in a row, whose halves two steps of the product take.
     v8 q[DP / 32];
@@ -110,62 +114,91 @@ __global__ __launch_bounds__(64 * one_waves(RB)) void attend_one_kernel(const At
         }
     }
 
-    lds_char *const mine = (lds_char *)lds + wave * 2 * STAGE;
+    lds_char *const mine = (lds_char *)lds + wave * STAGES * STAGE;
     const unsigned mine_at = (unsigned)(size_t)mine;
     const int32_t *table = a.table + s * a.table_stride;
     const char *k_head = static_cast<const char *>(c.k) + kvh * c.head_stride * SIZE, *v_head = static_cast<const char *>(c.v) + kvh * c.head_stride * SIZE;
     int table_base = 0, entries = -1;    // a lane's page of the sequence's pages table_base..table_base + 63
     bool have_table = false;
-    unsigned seen = 0, seen_next = 0;    // tokens of the step at hand and of the next one, a bit each
-    auto load = [&](int st) {
-        const int t0 = st * kOneTokens, token = t0 + (lane & 31);
-        if (!have_table || ((t0 + kOneTokens - 1) >> c.page_shift) - table_base >= 64) {
+    unsigned seen[STAGES];    // tokens of the step at hand and of those under way, a bit each
+    constexpr int LOAD_ROWS = 1024 / RB;    // that a load covers
+    const bool regular = c.head_dim * SIZE == RB && c.page_shift >= 4 && c.token_stride <= (1 << 24);   // 16 rows lie in a page
+    unsigned k_off[LOADS], v_off[LOADS];    // of this lane's 16 bytes behind the first row of the 16 that its load is among
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+        const int r = (j * 64 + lane) * 16 / RB, pos = lane & (RB / 16 - 1);
+        const unsigned row = (unsigned)(r & 15) * (unsigned)c.token_stride * SIZE;
+        k_off[j] = row + (pos ^ k_key<RB>(r)) * 16;
+        v_off[j] = row + (pos ^ v_key<RB, CODES>(r)) * 16;
+    }
+    // Loads the tokens of a step, tells which of them are seen.
+    auto load = [&](int st, int place) {
+        const int t0 = st * TOKENS, token = t0 + (lane & (TOKENS - 1));
+        if (!have_table || ((t0 + TOKENS - 1) >> c.page_shift) - table_base >= 64) {
             have_table = true;
             table_base = t0 >> c.page_shift;
             const int at = table_base + lane;
             const int page = at < a.table_pages ? table[at] : -1;
             entries = (unsigned)page < (unsigned)c.pages ? page : -1;
         }
-        const int page = __shfl(entries, (token >> c.page_shift) - table_base), in = token & ((1 << c.page_shift) - 1);
+        const int in = token & ((1 << c.page_shift) - 1), page = __shfl(entries, (token >> c.page_shift) - table_base);
         const bool ok = page >= 0 && token >= from && token < len;
-        seen_next = (unsigned)__ballot(ok);
-        const int64_t row = ok ? (page * c.page_stride + in * c.token_stride) * SIZE : -1;
-        const int row_lo = (int)row, row_hi = (int)(row >> 32);
-        const unsigned to = mine_at + (st & 1) * STAGE;
+        const unsigned bits = (unsigned)__ballot(ok) & ALL, to = mine_at + place * STAGE;
+        if (bits == ALL && regular) {
+            // One address for all lanes.
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const int r = (j * 64 + lane) * 16 / RB, pos = lane & (RB / 16 - 1);
-            const int kc = pos ^ k_key<RB>(r), vc = pos ^ v_key<RB, CODES>(r);
-            const int64_t at = (int64_t)__shfl(row_hi, r) << 32 | (unsigned)__shfl(row_lo, r);
-            const char *zero = reinterpret_cast<const char *>(one_zeros);
-            load_to_lds(at >= 0 && kc * 16 < c.head_dim * SIZE ? k_head + at + kc * 16 : zero, to + j * 1024);
-            load_to_lds(at >= 0 && vc * 16 < c.head_dim * SIZE ? v_head + at + vc * 16 : zero, to + PART + j * 1024);
+            for (int h = 0; h < HALVES; ++h) {
+                const int t = t0 + h * 16, first = __builtin_amdgcn_readlane(page, h * 16);
+                const int64_t at = ((int64_t)(unsigned)first * c.page_stride + (t & ((1 << c.page_shift) - 1)) * c.token_stride) * SIZE;
+#pragma unroll
+                for (int j = h * LOADS / HALVES; j < (h + 1) * LOADS / HALVES; ++j) {
+                    load_to_lds(k_head + at, k_off[j], to + j * 1024);
+                    load_to_lds(v_head + at, v_off[j], to + PART + j * 1024);
+                }
+            }
+        } else {
+            const int64_t row = ok ? (page * c.page_stride + in * c.token_stride) * SIZE : -1;
+            const int row_lo = (int)row, row_hi = (int)(row >> 32);
+            int64_t at[LOADS];
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                const int r = (j * 64 + lane) * 16 / RB;
+                at[j] = (int64_t)__shfl(row_hi, r) << 32 | (unsigned)__shfl(row_lo, r);
+            }
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                const int r = (j * 64 + lane) * 16 / RB, pos = lane & (RB / 16 - 1), kc = pos ^ k_key<RB>(r), vc = pos ^ v_key<RB, CODES>(r);
+                const char *zero = reinterpret_cast<const char *>(one_zeros);
+                load_to_lds(at[j] >= 0 && kc * 16 < c.head_dim * SIZE ? k_head + at[j] + kc * 16 : zero, to + j * 1024);
+                load_to_lds(at[j] >= 0 && vc * 16 < c.head_dim * SIZE ? v_head + at[j] + vc * 16 : zero, to + PART + j * 1024);
+            }
         }
         if constexpr (CODES) {
             const char *e = reinterpret_cast<const char *>(lane < 32 ? c.k_exp : c.v_exp) + page * c.exp_page_stride + kvh * c.exp_head_stride + in * c.exp_token_stride;
             load_byte_to_lds(ok ? e : reinterpret_cast<const char *>(one_zeros), to + 2 * PART);
         }
+        return bits;
     };
 
     f32x4 o[DP / 16];
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float top = -INFINITY, sum = 0.f, top_w = -INFINITY;   // maxima in units of ln 2: of the scores, and of what the weights refer to
-    const auto larger = [](float p, float q) { return fmaxf(p, q); };
-    if (step < end) load(step);
+    const auto larger = [](float p, float q) { return max3(p, q, q); };
+    unsigned seen_next = step < end ? load(step, step & 1) : 0u;    // of the next step's tokens, a bit each
     for (; step < end; ++step) {
-        seen = seen_next;
+        const unsigned seen = seen_next;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the reads of the step before, whose place the next one takes, are over
         if (step + 1 < end) {
-            load(step + 1);
+            seen_next = load(step + 1, (step + 1) & 1);
             asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * LOADS + CODES) : "memory");
         } else {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
         const lds_char *stage = mine + (step & 1) * STAGE;
-        f32x4 x[2];
+        f32x4 x[HALVES];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < HALVES; ++h) {
             x[h] = f32x4{0.f, 0.f, 0.f, 0.f};
             const int r = h * 16 + col;
             if constexpr (CODES) {
@@ -182,9 +215,9 @@ __global__ __launch_bounds__(64 * one_waves(RB)) void attend_one_kernel(const At
             }
         }
         // Scores in units of ln 2, those of codes with their key's exponent; z[h]: with the value's too.
-        f32x4 z[2];
+        f32x4 z[HALVES];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < HALVES; ++h) {
             if constexpr (CODES) {
                 const i32x4 ke = *reinterpret_cast<const __attribute__((address_space(3))) i32x4 *>(stage + 2 * PART + (h * 16 + quad * 4) * 4);
                 const i32x4 ve = *reinterpret_cast<const __attribute__((address_space(3))) i32x4 *>(stage + 2 * PART + 128 + (h * 16 + quad * 4) * 4);
@@ -198,9 +231,10 @@ __global__ __launch_bounds__(64 * one_waves(RB)) void attend_one_kernel(const At
                 for (int e = 0; e < 4; ++e) x[h][e] *= f.c;
             }
         }
-        if (seen != 0xffffffffu) {
+        if (__builtin_expect(seen != ALL, 0)) {
+            asm volatile("");   // a branch: few steps take it
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < HALVES; ++h)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (!(seen >> (h * 16 + quad * 4 + e) & 1)) {
@@ -208,11 +242,17 @@ __global__ __launch_bounds__(64 * one_waves(RB)) void attend_one_kernel(const At
                         if constexpr (CODES) z[h][e] = -INFINITY;
                     }
         }
-        const float most = of_four(fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3]))), larger);
+        auto most_of = [&](const f32x4 (&v)[HALVES]) {
+            float m = max3(v[0][0], v[0][1], v[0][2]);
+            if constexpr (HALVES == 2) m = max3(max3(m, v[0][3], v[1][0]), max3(v[1][1], v[1][2], v[1][3]), m);
+            else m = max3(m, v[0][3], m);
+            return of_four(m, larger);
+        };
+        const float most = most_of(x);
         bool follow = most > top + kOneSlack || (top == -INFINITY && most > top);
         float most_w = most;
         if constexpr (CODES) {
-            most_w = of_four(fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3]))), larger);
+            most_w = most_of(z);
             follow |= most_w > top_w + kOneSlack || (top_w == -INFINITY && most_w > top_w);
         }
         if (__any(follow)) {
@@ -229,9 +269,9 @@ __global__ __launch_bounds__(64 * one_waves(RB)) void attend_one_kernel(const At
             for (int i = 0; i < DP / 16; ++i) o[i] *= by_w;
         }
         const float ref = top == -INFINITY ? 0.f : top, ref_w = top_w == -INFINITY ? 0.f : top_w;
-        w8 w, rest;
+        w8 w = {}, rest = {};
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < HALVES; ++h)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float p = __builtin_amdgcn_exp2f(x[h][e] - ref);
@@ -254,9 +294,9 @@ __global__ __launch_bounds__(64 * one_waves(RB)) void attend_one_kernel(const At
                 const i32x2 codes = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(stage + PART + r * RB + ((i ^ v_key<RB, true>(r)) << 4) + (col & 1) * 8));
                 v = decode8<f16>(codes[0], codes[1]);
             } else {
-                s16x4 t[2];
+                s16x4 t[2] = {};
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < HALVES; ++h) {
                     const int r = h * 16 + quad * 4 + (col >> 2);
                     t[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                         (__attribute__((address_space(3))) s16x4 *)(stage + PART + r * RB + (((i * 2 + (col >> 1 & 1)) ^ v_key<RB, false>(r)) << 4) + (col & 1) * 8));
@@ -279,7 +319,7 @@ __global__ __launch_bounds__(64 * one_waves(RB)) void attend_one_kernel(const At
         tops[wave][col] = top;
         sums[wave][col] = sum;
     }
-    static_assert(kOneHeads * DP * 4 <= 2 * STAGE, "a wave's results fit where its tokens were");
+    static_assert(kOneHeads * DP * 4 <= STAGES * STAGE, "a wave's results fit where its tokens were");
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i)   // [head][DP], chunks of 16 bytes exchanged by the head
@@ -312,16 +352,16 @@ __global__ __launch_bounds__(64 * one_waves(RB)) void attend_one_kernel(const At
             total += sums[w][h] * by[w];
         }
     };
-    const int record = heads * (c.head_dim + 2);   // numbers: results, then a maximum and a sum for each head
+    const int items = heads * chunks, record = heads * (c.head_dim + 2);   // numbers of a part's record: results, then a maximum and a sum for each head
     float *const records = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + kOneCounters * 4) + ((int64_t)item * f.parts) * (min(f.group, kOneHeads) * (c.head_dim + 2));
-    for (int i = tid; i < heads * chunks; i += THREADS) {
-        const int h = i / chunks, d4 = i - h * chunks;
+    for (int i = tid; i < items; i += THREADS) {
+        const int h = fast_div(i, f.by_chunks), d4 = i - h * chunks;
         float m, total, by[WAVES];
         of_waves(h, m, total, by);
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w)
-            v += by[w] * *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>((lds_char *)lds + w * 2 * STAGE + h * (DP * 4) + ((d4 ^ (h & 7)) << 4));
+            v += by[w] * *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>((lds_char *)lds + w * STAGES * STAGE + h * (DP * 4) + ((d4 ^ (h & 7)) << 4));
         if (parts == 1) {
             store(h, d4, v, total);
             if (d4 == 0) store_lse(h, m, total);
@@ -353,45 +393,109 @@ __global__ __launch_bounds__(64 * one_waves(RB)) void attend_one_kernel(const At
     auto get = [&](int p, int at) {
         return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<uint64_t *>(records + (int64_t)p * record + at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
     };
-    for (int i = tid; i < heads * chunks; i += THREADS) {
-        const int h = i / chunks, d4 = i - h * chunks;
-        float m = -INFINITY, total = 0.f;
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int p = 0; p < parts; ++p) {
-            const f32x2 ms = get(p, heads * c.head_dim + 2 * h), lo = get(p, h * c.head_dim + d4 * 4), hi = get(p, h * c.head_dim + d4 * 4 + 2);
-            const float pm = ms[0], pt = ms[1];
-            const f32x4 pv = {lo[0], lo[1], hi[0], hi[1]};
-            const float now = fmaxf(m, pm), r = now == -INFINITY ? 0.f : now, bo = __builtin_amdgcn_exp2f(m - r), bn = __builtin_amdgcn_exp2f(pm - r);
-            m = now;
-            total = total * bo + pt * bn;
-            v = v * bo + pv * bn;
+    // A trip to memory takes longer than all the arithmetic: where a head's results are fewer than the threads, groups of these take every so manieth part, and the first
+    // eight of each thread are under way while the parts' weights are made, a lane a part.
+    constexpr int BATCH = 8;
+    const int groups = items < THREADS ? (int)((THREADS + 0.5f) * __builtin_amdgcn_rcpf((float)items)) : 1;
+    const int g = groups > 1 ? (int)((tid + 0.5f) * __builtin_amdgcn_rcpf((float)items)) : 0, i0 = tid - g * items * (groups > 1);
+    f32x2 lo[BATCH], hi[BATCH];
+    auto fetch = [&](int i, int from) {
+        const int h = fast_div(i, f.by_chunks), at = h * c.head_dim + (i - h * chunks) * 4;
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+            const int p = min(from + j * groups, parts - 1);
+            lo[j] = get(p, at);
+            hi[j] = get(p, at + 2);
         }
-        store(h, d4, v, total);
-        if (d4 == 0) store_lse(h, m, total);
+    };
+    const bool some = i0 < items && g < groups;
+    if (some) fetch(i0, g);
+    typedef __attribute__((address_space(3))) float lds_float;
+    lds_float *const weights = (lds_float *)(lds_char *)lds;           // [head][kOneMostParts]
+    lds_float *const heads_of = weights + kOneHeads * kOneMostParts;   // a maximum and a sum for each head
+    static_assert((kOneHeads * kOneMostParts + 2 * kOneHeads + 4 * THREADS) * 4 <= STAGES * WAVES * STAGE, "weights and sums fit where the tokens were");
+#pragma unroll 4
+    for (int h = wave; h < heads; h += WAVES) {
+        const f32x2 ms = get(min(lane, parts - 1), heads * c.head_dim + 2 * h);
+        float m = lane < parts ? ms[0] : -INFINITY;
+        const float mine_m = m;
+#pragma unroll
+        for (int j = 1; j < 64; j *= 2) m = fmaxf(m, __shfl_xor(m, j));
+        const float w = __builtin_amdgcn_exp2f(mine_m - (m == -INFINITY ? 0.f : m));
+        float total = lane < parts ? ms[1] * w : 0.f;
+#pragma unroll
+        for (int j = 1; j < 64; j *= 2) total += __shfl_xor(total, j);
+        weights[h * kOneMostParts + lane] = w;
+        if (lane == 0) {
+            heads_of[2 * h] = m;
+            heads_of[2 * h + 1] = total;
+        }
     }
+    __syncthreads();
+    for (int i = i0; i < items; i += THREADS) {
+        if (!some) break;
+        const int h = fast_div(i, f.by_chunks), d4 = i - h * chunks;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int from = g; from < parts; from += BATCH * groups) {
+            if (i != i0 || from != g) fetch(i, from);
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int p = from + j * groups;
+                const float w = p < parts ? weights[h * kOneMostParts + p] : 0.f;
+                if (w > 0.f) v += w * f32x4{lo[j][0], lo[j][1], hi[j][0], hi[j][1]};
+                else if (w != w) v = f32x4{NAN, NAN, NAN, NAN};
+            }
+        }
+        if (groups > 1) {
+            *reinterpret_cast<__attribute__((address_space(3))) f32x4 *>(heads_of + 2 * kOneHeads + 4 * tid) = v;
+            break;
+        }
+        store(h, d4, v, heads_of[2 * h + 1]);
+        if (d4 == 0) store_lse(h, heads_of[2 * h], heads_of[2 * h + 1]);
+    }
+    if (groups == 1) return;
+    __syncthreads();
+    if (tid >= items) return;
+    const int h = fast_div(tid, f.by_chunks), d4 = tid - h * chunks;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < groups; ++j) v += *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(heads_of + 2 * kOneHeads + 4 * (j * items + tid));
+    store(h, d4, v, heads_of[2 * h + 1]);
+    if (d4 == 0) store_lse(h, heads_of[2 * h], heads_of[2 * h + 1]);
+}
+
+template <typename T, bool CODES, int RB, int WAVES>
+hipError_t launch_attend_one_as(const AttendOneArgs &a, int64_t items, int64_t steps, int64_t parts, int fewest, hipStream_t s) {
+    AttendOneKernel f{};
+    f.a = a;
+    f.group = a.heads / a.cache.kv_heads;
+    f.blocks = (f.group + kOneHeads - 1) / kOneHeads;
+    const int64_t record = (int64_t)std::min(f.group, kOneHeads) * (a.cache.head_dim + 2) * 4;
+    parts = std::min({parts, (int64_t)kOneMostParts, steps / fewest});
+    if (items > kOneCounters || a.workspace_bytes <= kOneCounters * 4) parts = 1;
+    else parts = std::min(parts, (int64_t)((a.workspace_bytes - kOneCounters * 4) / (record * items)));
+    f.parts = (int)std::max<int64_t>(parts, 1);
+    f.fewest = fewest;
+    if (items * f.parts > INT32_MAX) return hipErrorInvalidValue;
+    f.by_parts = make_fast_div((uint32_t)f.parts);
+    f.by_kv_heads = make_fast_div((uint32_t)a.cache.kv_heads);
+    f.by_blocks = make_fast_div((uint32_t)f.blocks);
+    f.by_chunks = make_fast_div((uint32_t)a.cache.head_dim / 4);
+    f.c = fminf(fmaxf(fabsf(a.scale) * 1.44269504f, 1e-37f), 3e38f);
+    attend_one_kernel<T, CODES, RB, WAVES><<<dim3((unsigned)(items * f.parts)), 64 * WAVES, 0, s>>>(f);
+    return hipGetLastError();
 }
 
 template <typename T, bool CODES, int RB>
-hipError_t launch_attend_one_as(const AttendOneArgs &a, hipStream_t s) {
-    constexpr int WAVES = one_waves(RB);
-    AttendOneKernel f{a, a.heads / a.cache.kv_heads, 0, 1, fminf(fmaxf(fabsf(a.scale) * 1.44269504f, 1e-37f), 3e38f)};
-    f.blocks = (f.group + kOneHeads - 1) / kOneHeads;
-    const int64_t items = (int64_t)a.sequences * f.blocks * a.cache.kv_heads;
-    // Parts: one round of workgroups where the items are few, several where they are many, so that long sequences do not end alone.
-    const int64_t slots = 256 * (kOneTokens * RB * 2 * 2 * WAVES > 64 * 1024 ? 1 : 2);
-    const int64_t steps = (((int64_t)a.table_pages << a.cache.page_shift) + kOneTokens - 1) / kOneTokens;
-    if (items < 8 * slots && items <= kOneCounters) {
-        int64_t parts = items <= slots ? slots / items : (8 * slots + items - 1) / items;
-        parts = std::min({parts, (int64_t)kOneMostParts, steps / (2 * WAVES)});
-        const int64_t record = (int64_t)std::min(f.group, kOneHeads) * (a.cache.head_dim + 2) * 4;
-        if (a.workspace_bytes > kOneCounters * 4) parts = std::min(parts, (int64_t)((a.workspace_bytes - kOneCounters * 4) / (record * items)));
-        else parts = 1;
-        f.parts = (int)std::max<int64_t>(parts, 1);
-    }
-    if (items * f.parts > INT32_MAX) return hipErrorInvalidValue;
-    attend_one_kernel<T, CODES, RB><<<dim3((unsigned)(items * f.parts)), 64 * WAVES, 0, s>>>(f);
-    return hipGetLastError();
+hipError_t launch_attend_one_row(const AttendOneArgs &a, hipStream_t s) {
+    constexpr int TOKENS = one_tokens(RB), WAVES = 4;
+    const int64_t items = (int64_t)a.sequences * ((a.heads / a.cache.kv_heads + kOneHeads - 1) / kOneHeads) * a.cache.kv_heads;
+    int64_t tokens = (int64_t)a.table_pages << a.cache.page_shift;
+    if (a.window > 0) tokens = std::min<int64_t>(tokens, (int64_t)a.window + TOKENS - 1);
+    const int64_t steps = (tokens + TOKENS - 1) / TOKENS;
+    if (items >= 288 && tokens <= 1024) return launch_attend_one_as<T, CODES, RB, 1>(a, items, steps, (4096 + items - 1) / items, 512 / TOKENS, s);
+    constexpr int64_t slots = 2 * WAVES * (2 * TOKENS * RB + 256) > 80 * 1024 ? 256 : 512;
+    if (items <= slots) return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, slots / items, 64 / TOKENS * WAVES, s);
+    return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, (4 * slots + items - 1) / items, 64 / TOKENS * WAVES, s);
 }
 
 template <typename T, bool CODES>
@@ -399,13 +503,13 @@ hipError_t launch_attend_one_typed(const AttendOneArgs &a, hipStream_t s) {
     const int bytes = a.cache.head_dim * (CODES ? 1 : 2);
     if (a.cache.head_dim % 16 != 0 || a.cache.head_dim > kAttendMostDim) return hipErrorInvalidValue;
     if constexpr (CODES) {
-        if (bytes <= 64) return launch_attend_one_as<T, CODES, 64>(a, s);
-        if (bytes <= 128) return launch_attend_one_as<T, CODES, 128>(a, s);
-        return launch_attend_one_as<T, CODES, 256>(a, s);
+        if (bytes <= 64) return launch_attend_one_row<T, CODES, 64>(a, s);
+        if (bytes <= 128) return launch_attend_one_row<T, CODES, 128>(a, s);
+        return launch_attend_one_row<T, CODES, 256>(a, s);
     } else {
-        if (bytes <= 128) return launch_attend_one_as<T, CODES, 128>(a, s);
-        if (bytes <= 256) return launch_attend_one_as<T, CODES, 256>(a, s);
-        return launch_attend_one_as<T, CODES, 512>(a, s);
+        if (bytes <= 128) return launch_attend_one_row<T, CODES, 128>(a, s);
+        if (bytes <= 256) return launch_attend_one_row<T, CODES, 256>(a, s);
+        return launch_attend_one_row<T, CODES, 512>(a, s);
     }
 }
 

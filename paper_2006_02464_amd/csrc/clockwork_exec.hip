@@ -1535,7 +1535,7 @@ static int32_t cache_view(cw_ctx *c, const cw_cache *r, bool written, CacheView 
 // What the calls over a cache refuse in common of their sequences.
 static int32_t sequence_checks(cw_ctx *c, int32_t sequences, int32_t table_pages, int64_t table_stride, const int32_t *table, const int32_t *lengths, int32_t page) {
     if (sequences < 0 || table_pages < 0 || table_stride < 0 || table_stride > kMostStride) return set_err(c, CW_ERR_INVALID, "bad size");
-    if (sequences > kAttendMostSequences || (int64_t)table_pages * page > INT32_MAX) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
+    if (sequences > kAttendMostSequences || (int64_t)table_pages * page > kCacheMostTokens) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
     if (sequences > 0) {
         if (!lengths || (table_pages > 0 && !table)) return set_err(c, CW_ERR_INVALID, "null pointer");
         if (!aligned_to(lengths, DT_F32) || !aligned_to(table, DT_F32)) return set_err(c, CW_ERR_INVALID, "misaligned pointer");

@@ -12,9 +12,12 @@ static __device__ __forceinline__ void load_to_lds(u32x4 desc, unsigned voff, un
                  : "memory", "m0");
 }
 
-// The same from an address of each lane's own, and a byte, zero-extended to four, to lds_addr + 4*lane.
+// The same from an address of each lane's own; from an offset of its own behind one address; and a byte, zero-extended to four, to lds_addr + 4*lane.
 static __device__ __forceinline__ void load_to_lds(const void *from, unsigned lds_addr) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(from) : "memory", "m0");
+}
+static __device__ __forceinline__ void load_to_lds(const void *base, unsigned offset, unsigned lds_addr) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_addr), "v"(offset), "s"(base) : "memory", "m0");
 }
 static __device__ __forceinline__ void load_byte_to_lds(const void *from, unsigned lds_addr) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off" : : "s"(lds_addr), "v"(from) : "memory", "m0");
