@@ -177,6 +177,7 @@ SIGNATURES = {
 }
 
 _lib = None
+_int32 = _float32 = None    # torch's
 
 
 def lib():
@@ -195,6 +196,8 @@ def lib():
         for name, (res, args) in SIGNATURES.items():
             fn = getattr(l, name)
             fn.restype, fn.argtypes = res, args
+        global _int32, _float32
+        _int32, _float32 = torch.int32, torch.float32
         _lib = l
     return _lib
 
@@ -306,17 +309,40 @@ def _heads(t, what, device, shape):
     return t.data_ptr(), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
 
 
-def _table(table, lengths, device):
-    """(address of the table, its row stride, address of the lengths, sequences, pages a row)."""
+def _ints(t, what, device, count):
+    """Address of `count` contiguous elements of int32 there."""
+    if t.dtype is _int32 and t.get_device() == device and t.numel() == count and t.is_contiguous():
+        return t.data_ptr()
+    return _vector(t, what, device, count, "torch.int32")
+
+
+def _floats(t, what, device, count):
+    """The same of fp32, or 0."""
+    if t is None:
+        return 0
+    if t.dtype is _float32 and t.get_device() == device and t.numel() == count and t.is_contiguous():
+        return t.data_ptr()
+    return _vector(t, what, device, count, "torch.float32")
+
+
+def _table(table, device):
+    """(address of the table, its row stride, sequences, pages a row)."""
     if table.dim() != 2:
         raise ValueError("table is %s, not (sequences, pages)" % (tuple(table.shape),))
-    sequences, pages = table.shape
-    at, row = _matrix(table, "table", device, sequences, pages)
-    if table.dtype not in _vector_types:
-        _vector_types[table.dtype] = str(table.dtype)
-    if _vector_types[table.dtype] != "torch.int32":
+    if table.dtype is not _int32:
         raise ValueError("table holds int32")
-    return at, row if sequences > 1 else 0, _vector(lengths, "lengths", device, sequences, "torch.int32"), sequences, pages
+    if table.get_device() != device:
+        raise ValueError("table is not on the context's GPU")
+    sequences, pages = table.shape
+    row, step = table.stride()
+    if step != 1 and pages > 1:
+        raise ValueError("table: elements of a row must be contiguous")
+    return table.data_ptr(), row if sequences > 1 else 0, sequences, pages
+
+
+def _on(stream):
+    """Handle of a stream as a number."""
+    return 0 if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
 
 
 class Cache:
@@ -353,7 +379,7 @@ class Cache:
             raise CwError(CW_ERR_UNSUPPORTED, "too large") from None
         self.tensors = (k, v, k_exp, v_exp)
         self.kv_heads, self.head_dim = kv_heads, head_dim
-        self._address = ctypes.addressof(self._struct)
+        self.address = ctypes.addressof(self._struct)
 
 
 def _host(x, what):
@@ -582,48 +608,53 @@ class Context:
     def _cache_rows(self, call, cache, k, v, table, lengths, first, stream):
         if k.dim() != 3:
             raise ValueError("k is %s, not (tokens, kv_heads, head_dim)" % (tuple(k.shape),))
-        if k.dtype != v.dtype:
+        dtype, on, tokens = k.dtype, self._device, k.shape[0]
+        if dtype is not v.dtype:
             raise TypeError("k and v are of different types")
-        on, shape = self._device, (k.shape[0], cache.kv_heads, cache.head_dim)
-        tokens = shape[0]
+        shape = (tokens, cache.kv_heads, cache.head_dim)
         kp, ks, kh = _heads(k, "k", on, shape)
         vp, vs, vh = _heads(v, "v", on, shape)
-        tp, ts, lp, sequences, pages = _table(table, lengths, on)
+        tp, ts, sequences, pages = _table(table, on)
         try:
-            args = _pack_cache_args(cache._address, kp, vp, _vector(first, "first", on, sequences + 1, "torch.int32"), lp, tp, ks, kh, vs, vh, ts,
-                                    tokens, sequences, pages, _element_codes[k.dtype])
+            args = _pack_cache_args(cache.address, kp, vp, 0 if first is None else _ints(first, "first", on, sequences + 1), _ints(lengths, "lengths", on, sequences), tp,
+                                    ks, kh, vs, vh, ts, tokens, sequences, pages, _element_codes[dtype])
         except (struct.error, OverflowError) as e:
             raise _refused(e, tokens=tokens, sequences=sequences, pages=pages) from None
-        self._check(call(self._h, args, _stream(stream)))
+        status = call(self._h, args, _on(stream))
+        if status < 0:
+            self._check(status)
 
     def cache_write(self, k, v, cache, table, lengths, first=None, stream=None):
         """Writes rows of k and v [tokens][kv_heads][head_dim] to the pages of `cache` as the last tokens of their sequences: rows first[s]..first[s + 1] - 1 of
         sequence s, that has lengths[s] tokens with them and its pages in table[s]; without `first` a row each.  torch tensors on the context's GPU, integers int32."""
-        self._cache_rows(lib().cw_cache_write, cache, k, v, table, lengths, first, stream)
+        self._cache_rows(_lib.cw_cache_write, cache, k, v, table, lengths, first, stream)
 
     def cache_read(self, cache, table, lengths, k, v, first=None, stream=None):
         """Reads the same rows back into k and v."""
-        self._cache_rows(lib().cw_cache_read, cache, k, v, table, lengths, first, stream)
+        self._cache_rows(_lib.cw_cache_read, cache, k, v, table, lengths, first, stream)
 
     def attend_one(self, q, cache, table, lengths, y, scale, window=0, lse=None, workspace=None, stream=None):
         """y[sequences][heads][head_dim] = attention of q, a token of each sequence, over the lengths[s] tokens (the last `window`) in the pages table[s] of
         `cache`; lse [sequences][heads] fp32 is written if there is one.  workspace: uint8, zeros before its first call."""
         if q.dim() != 3:
             raise ValueError("q is %s, not (sequences, heads, head_dim)" % (tuple(q.shape),))
-        tp, ts, lp, sequences, pages = _table(table, lengths, self._device)
-        heads, on, shape = q.shape[1], self._device, (sequences, q.shape[1], cache.head_dim)
+        on, dtype, heads = self._device, q.dtype, q.shape[1]
+        if y.dtype is not dtype:
+            raise TypeError("q and y are of different types")
+        tp, ts, sequences, pages = _table(table, on)
+        shape = (sequences, heads, cache.head_dim)
         qp, qs, qh = _heads(q, "q", on, shape)
         yp, ys, yh = _heads(y, "y", on, shape)
-        if y.dtype != q.dtype:
-            raise TypeError("q and y are of different types")
         space = workspace.numel() if workspace is not None else 0
         try:
-            args = _pack_attend_one(cache._address, qp, yp, _vector(lse, "lse", on, sequences * heads, "torch.float32"), lp, tp,
+            args = _pack_attend_one(cache.address, qp, yp, _floats(lse, "lse", on, sequences * heads), _ints(lengths, "lengths", on, sequences), tp,
                                     _vector(workspace, "workspace", on, space, "torch.uint8"), space, qs, qh, ys, yh, ts,
-                                    sequences, heads, pages, window, _element_codes[q.dtype], scale)
+                                    sequences, heads, pages, window, _element_codes[dtype], scale)
         except (struct.error, OverflowError) as e:
             raise _refused(e, sequences=sequences, heads=heads, window=window, scale=scale) from None
-        self._check(lib().cw_attend_one(self._h, args, _stream(stream)))
+        status = _lib.cw_attend_one(self._h, args, _on(stream))
+        if status < 0:
+            self._check(status)
 
     @staticmethod
     def attend_one_workspace_bytes():
@@ -634,21 +665,24 @@ class Context:
         first_k) of k and v [keys][kv_heads][head_dim]; lse [tokens][heads] fp32 is written if there is one."""
         if q.dim() != 3 or k.dim() != 3:
             raise ValueError("q is %s, k %s, not (tokens, heads, head_dim)" % (tuple(q.shape), tuple(k.shape)))
-        if not q.dtype == k.dtype == v.dtype == y.dtype:
+        dtype, on, shape, sequences = q.dtype, self._device, q.shape, first.numel() - 1
+        if k.dtype is not dtype or v.dtype is not dtype or y.dtype is not dtype:
             raise TypeError("q, k, v and y are of different types")
-        on, shape, keys = self._device, q.shape, (k.shape[0], k.shape[1], q.shape[2])
+        tokens, heads, head_dim = shape
+        keys = (k.shape[0], k.shape[1], head_dim)
         qp, qs, qh = _heads(q, "q", on, shape)
         kp, ks, kh = _heads(k, "k", on, keys)
         vp, vs, vh = _heads(v, "v", on, keys)
         yp, ys, yh = _heads(y, "y", on, shape)
-        sequences = first.numel() - 1
         try:
-            args = _pack_attend(qp, kp, vp, yp, _vector(lse, "lse", on, shape[0] * shape[1], "torch.float32"), _vector(first, "first", on, sequences + 1, "torch.int32"),
-                                _vector(first_k, "first_k", on, sequences + 1, "torch.int32"), qs, qh, ks, kh, vs, vh, ys, yh,
-                                shape[0], keys[0], sequences, shape[1], keys[1], shape[2], causal, window, _element_codes[q.dtype], scale)
+            args = _pack_attend(qp, kp, vp, yp, _floats(lse, "lse", on, tokens * heads), _ints(first, "first", on, sequences + 1),
+                                0 if first_k is None else _ints(first_k, "first_k", on, sequences + 1), qs, qh, ks, kh, vs, vh, ys, yh,
+                                tokens, keys[0], sequences, heads, keys[1], head_dim, causal, window, _element_codes[dtype], scale)
         except (struct.error, OverflowError) as e:
-            raise _refused(e, tokens=shape[0], keys=keys[0], sequences=sequences, window=window, scale=scale) from None
-        self._check(lib().cw_attend(self._h, args, _stream(stream)))
+            raise _refused(e, tokens=tokens, keys=keys[0], sequences=sequences, window=window, scale=scale) from None
+        status = _lib.cw_attend(self._h, args, _on(stream))
+        if status < 0:
+            self._check(status)
 
     def release(self, slot):
         self._check(lib().cw_release(self._h, slot))
