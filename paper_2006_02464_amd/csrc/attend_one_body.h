@@ -22,7 +22,8 @@ constexpr int kOneCounters = 65536 / 4;
 struct AttendOneKernel {
     AttendOneArgs a;
     int32_t group, blocks;   // query heads of a key head, blocks of kOneHeads of them
-    FastDiv by_parts, by_kv_heads, by_blocks, by_chunks;   // chunks: 16 bytes of a head's results in fp32
+    int32_t items;           // of a sequence: key heads times blocks
+    FastDiv by_parts, by_kv_heads, by_items, by_chunks;   // chunks: 16 bytes of a head's results in fp32
     int32_t parts, fewest;   // of a sequence at most, and steps that are worth one
     float c;                 // |scale| / ln 2
 };
@@ -65,9 +66,29 @@ __device__ static inline float max3(float a, float b, float c) {   // as the ins
     return r;
 }
 
+// The tokens of a sequence that are looked at, and the steps that they take.
+struct OneRange {
+    int from, len, step0, steps;
+};
+template <int TOKENS>
+__device__ static inline OneRange one_range(const AttendOneArgs &a, int length) {
+    const int full = max(length, 0), from = a.window > 0 ? max(0, full - a.window) : 0, len = min(full, a.table_pages << a.cache.page_shift), step0 = from / TOKENS;
+    return {from, len, step0, len > from ? (len + TOKENS - 1) / TOKENS - step0 : 0};
+}
+
+// What a workgroup keeps in LDS.
+template <bool CODES, int RB, int WAVES>
+struct OneShared {
+    static constexpr int TOKENS = one_tokens(RB), STAGES = 2, STAGE = 2 * TOKENS * RB + (CODES ? 256 : 0);
+    __attribute__((aligned(1024))) unsigned char lds[STAGES * WAVES * STAGE];
+    float tops[WAVES][kOneHeads], sums[WAVES][kOneHeads];
+    int last;
+};
+
+// Part `part` of `parts` of the attention of sequence s and heads hh: this wave's steps of it are step..end - 1 of the range.  Part p leaves its record at first + p.
 // T: queries; CODES: pages of e4m3, else of T.  RB: bytes of a row in LDS, at least those of a head.
 template <typename T, bool CODES, int RB, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, RB / (CODES ? 1 : 2) <= 128 ? 2 : 1) void attend_one_kernel(const AttendOneKernel f) {
+__device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f, OneShared<CODES, RB, WAVES> &shared, int s, int hh, const OneRange range, int step, int end, int part, int parts, int first) {
     typedef typename std::conditional<CODES, f16, T>::type VT;    // of the second product
     typedef typename Mfma<T>::v8 v8;
     typedef typename Mfma<VT>::v8 w8;
@@ -76,28 +97,21 @@ __global__ __launch_bounds__(64 * WAVES, RB / (CODES ? 1 : 2) <= 128 ? 2 : 1) vo
     typedef int i32x4 __attribute__((ext_vector_type(4)));
     typedef float f32x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) unsigned char lds_char;
-    constexpr int THREADS = 64 * WAVES, SIZE = CODES ? 1 : 2, DP = RB / SIZE, TOKENS = one_tokens(RB), HALVES = TOKENS / 16, STAGES = 2;
-    constexpr int PART = TOKENS * RB, EXPS = CODES ? 256 : 0, STAGE = 2 * PART + EXPS, LOADS = PART / 1024;
+    typedef OneShared<CODES, RB, WAVES> Shared;
+    constexpr int THREADS = 64 * WAVES, SIZE = CODES ? 1 : 2, DP = RB / SIZE, TOKENS = Shared::TOKENS, HALVES = TOKENS / 16, STAGES = Shared::STAGES;
+    constexpr int PART = TOKENS * RB, STAGE = Shared::STAGE, LOADS = PART / 1024;
     constexpr unsigned ALL = TOKENS == 32 ? 0xffffffffu : (1u << TOKENS) - 1u;
     static_assert(!CODES || TOKENS == 32, "codes' exponents: a lane each of keys and of values");
     constexpr bool TWO = std::is_same<VT, bf16>::value;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[STAGES * WAVES * STAGE];
-    __shared__ float tops[WAVES][kOneHeads], sums[WAVES][kOneHeads];
-    __shared__ int last;
+    auto &lds = shared.lds;
+    auto &tops = shared.tops;
+    auto &sums = shared.sums;
     const AttendOneArgs &a = f.a;
     const CacheView &c = a.cache;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quad = lane >> 4;
-    const int item = fast_div(blockIdx.x, f.by_parts), part = blockIdx.x - item * f.parts;
-    const int below = fast_div(item, f.by_kv_heads), kvh = item - below * c.kv_heads, s = fast_div(below, f.by_blocks), block = below - s * f.blocks;
+    const int block = fast_div(hh, f.by_kv_heads), kvh = hh - block * c.kv_heads;
     const int heads = min(kOneHeads, f.group - block * kOneHeads), head0 = kvh * f.group + block * kOneHeads;
-
-    const int full = max(a.lengths[s], 0), from = a.window > 0 ? max(0, full - a.window) : 0, len = min(full, a.table_pages << c.page_shift);
-    const int step0 = from / TOKENS, steps = len > from ? (len + TOKENS - 1) / TOKENS - step0 : 0;
-    const int parts = max(1, min(f.parts, steps / f.fewest));
-    if (part >= parts) return;
-    const int each = (int)((unsigned)(steps + parts * WAVES - 1) / (unsigned)(parts * WAVES));   // steps of a wave
-    int step = step0 + (part * WAVES + wave) * each;
-    const int end = min(step + each, step0 + steps);
+    const int from = range.from, len = range.len;
 
     // Q as the second operand of the first product: with codes 16 numbers of a head in a row, whose halves two steps of the product take.
     v8 q[DP / 32];
@@ -120,7 +134,6 @@ __global__ __launch_bounds__(64 * WAVES, RB / (CODES ? 1 : 2) <= 128 ? 2 : 1) vo
     const char *k_head = static_cast<const char *>(c.k) + kvh * c.head_stride * SIZE, *v_head = static_cast<const char *>(c.v) + kvh * c.head_stride * SIZE;
     int table_base = 0, entries = -1;    // a lane's page of the sequence's pages table_base..table_base + 63
     bool have_table = false;
-    unsigned seen[STAGES];    // tokens of the step at hand and of those under way, a bit each
     constexpr int LOAD_ROWS = 1024 / RB;    // that a load covers
     const bool regular = c.head_dim * SIZE == RB && c.page_shift >= 4 && c.token_stride <= (1 << 24);   // 16 rows lie in a page
     unsigned k_off[LOADS], v_off[LOADS];    // of this lane's 16 bytes behind the first row of the 16 that its load is among
@@ -352,8 +365,11 @@ __global__ __launch_bounds__(64 * WAVES, RB / (CODES ? 1 : 2) <= 128 ? 2 : 1) vo
             total += sums[w][h] * by[w];
         }
     };
-    const int items = heads * chunks, record = heads * (c.head_dim + 2);   // numbers of a part's record: results, then a maximum and a sum for each head
-    float *const records = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + kOneCounters * 4) + ((int64_t)item * f.parts) * (min(f.group, kOneHeads) * (c.head_dim + 2));
+    const int items = heads * chunks;
+    // A part's record: results, then a maximum and a sum for each head.
+    auto record_of = [&](int p) {
+        return reinterpret_cast<float *>(static_cast<char *>(a.workspace) + kOneCounters * 4) + (int64_t)(first + p) * (min(f.group, kOneHeads) * (c.head_dim + 2));
+    };
     for (int i = tid; i < items; i += THREADS) {
         const int h = fast_div(i, f.by_chunks), d4 = i - h * chunks;
         float m, total, by[WAVES];
@@ -366,7 +382,7 @@ __global__ __launch_bounds__(64 * WAVES, RB / (CODES ? 1 : 2) <= 128 ? 2 : 1) vo
             store(h, d4, v, total);
             if (d4 == 0) store_lse(h, m, total);
         } else {
-            float *to = records + (int64_t)part * record;
+            float *to = record_of(part);
             auto put = [&](int at, float p, float q) {
                 const uint64_t two = (uint64_t)__builtin_bit_cast(unsigned, q) << 32 | __builtin_bit_cast(unsigned, p);
                 __hip_atomic_store(reinterpret_cast<uint64_t *>(to + at), two, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -383,15 +399,15 @@ __global__ __launch_bounds__(64 * WAVES, RB / (CODES ? 1 : 2) <= 128 ? 2 : 1) vo
     __builtin_amdgcn_s_waitcnt(0);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     __syncthreads();
-    int *counter = static_cast<int *>(a.workspace) + item;
-    if (tid == 0) last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+    int *counter = static_cast<int *>(a.workspace) + s * (f.blocks * c.kv_heads) + hh;
+    if (tid == 0) shared.last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
     __syncthreads();
-    if (!last) return;
+    if (!shared.last) return;
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
     if (tid == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     auto get = [&](int p, int at) {
-        return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<uint64_t *>(records + (int64_t)p * record + at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+        return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<uint64_t *>(record_of(p) + at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
     };
     // A trip to memory takes longer than all the arithmetic: where a head's results are fewer than the threads, groups of these take every so manieth part, and the first
     // eight of each thread are under way while the parts' weights are made, a lane a part.
@@ -463,24 +479,49 @@ __global__ __launch_bounds__(64 * WAVES, RB / (CODES ? 1 : 2) <= 128 ? 2 : 1) vo
     if (d4 == 0) store_lse(h, heads_of[2 * h], heads_of[2 * h + 1]);
 }
 
+constexpr int one_waves(bool codes, int rb) { return rb / (codes ? 1 : 2) <= 128 ? 2 : 1; }   // of a SIMD, at least
+
+// A grid of parts of items, items being sequences and their heads.
 template <typename T, bool CODES, int RB, int WAVES>
-hipError_t launch_attend_one_as(const AttendOneArgs &a, int64_t items, int64_t steps, int64_t parts, int fewest, hipStream_t s) {
+__global__ __launch_bounds__(64 * WAVES, one_waves(CODES, RB)) void attend_one_kernel(const AttendOneKernel f) {
+    __shared__ OneShared<CODES, RB, WAVES> shared;
+    const int item = fast_div(blockIdx.x, f.by_parts), part = blockIdx.x - item * f.parts, s = fast_div(item, f.by_items), hh = item - s * f.items;
+    const OneRange range = one_range<one_tokens(RB)>(f.a, f.a.lengths[s]);
+    const int parts = max(1, min(f.parts, range.steps / f.fewest));
+    if (part >= parts) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int each = (int)((unsigned)(range.steps + parts * WAVES - 1) / (unsigned)(parts * WAVES));   // steps of a wave
+    const int step = range.step0 + (part * WAVES + wave) * each;
+    attend_one_part<T, CODES, RB, WAVES>(f, shared, s, hh, range, step, min(step + each, range.step0 + range.steps), part, parts, item * f.parts);
+}
+
+inline AttendOneKernel one_kernel(const AttendOneArgs &a, int64_t parts, int fewest) {
     AttendOneKernel f{};
     f.a = a;
     f.group = a.heads / a.cache.kv_heads;
     f.blocks = (f.group + kOneHeads - 1) / kOneHeads;
-    const int64_t record = (int64_t)std::min(f.group, kOneHeads) * (a.cache.head_dim + 2) * 4;
-    parts = std::min({parts, (int64_t)kOneMostParts, steps / fewest});
-    if (items > kOneCounters || a.workspace_bytes <= kOneCounters * 4) parts = 1;
-    else parts = std::min(parts, (int64_t)((a.workspace_bytes - kOneCounters * 4) / (record * items)));
+    f.items = f.blocks * a.cache.kv_heads;
     f.parts = (int)std::max<int64_t>(parts, 1);
     f.fewest = fewest;
-    if (items * f.parts > INT32_MAX) return hipErrorInvalidValue;
     f.by_parts = make_fast_div((uint32_t)f.parts);
     f.by_kv_heads = make_fast_div((uint32_t)a.cache.kv_heads);
-    f.by_blocks = make_fast_div((uint32_t)f.blocks);
+    f.by_items = make_fast_div((uint32_t)f.items);
     f.by_chunks = make_fast_div((uint32_t)a.cache.head_dim / 4);
     f.c = fminf(fmaxf(fabsf(a.scale) * 1.44269504f, 1e-37f), 3e38f);
+    return f;
+}
+
+// Records that the workspace has room for.
+inline int64_t one_records(const AttendOneArgs &a, int64_t items) {
+    if (items > kOneCounters || a.workspace_bytes <= kOneCounters * 4) return 0;
+    return (int64_t)(a.workspace_bytes - kOneCounters * 4) / ((int64_t)std::min(a.heads / a.cache.kv_heads, kOneHeads) * (a.cache.head_dim + 2) * 4);
+}
+
+template <typename T, bool CODES, int RB, int WAVES>
+hipError_t launch_attend_one_as(const AttendOneArgs &a, int64_t items, int64_t steps, int64_t parts, int fewest, hipStream_t s) {
+    parts = std::min({parts, (int64_t)kOneMostParts, steps / fewest, one_records(a, items) / items});
+    const AttendOneKernel f = one_kernel(a, parts, fewest);
+    if (items * f.parts > INT32_MAX) return hipErrorInvalidValue;
     attend_one_kernel<T, CODES, RB, WAVES><<<dim3((unsigned)(items * f.parts)), 64 * WAVES, 0, s>>>(f);
     return hipGetLastError();
 }
