@@ -1553,7 +1553,7 @@ static int32_t cache_rows(cw_ctx *c, const cw_cache_args *r, void *stream, bool 
     if (r->tokens < 0) return set_err(c, CW_ERR_INVALID, "bad size");
     rc = sequence_checks(c, r->sequences, r->table_pages, r->table_stride, r->table, r->lengths, r->cache->page);
     if (rc != CW_OK) return rc;
-    if (r->tokens > kAttendMostTokens || (int64_t)r->tokens * 2 * a.cache.kv_heads > INT32_MAX) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
+    if (r->tokens > kAttendMostTokens || (int64_t)r->tokens * 2 * a.cache.kv_heads > kCacheMostRows) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
     if (!r->first && r->tokens != r->sequences) return set_err(c, CW_ERR_INVALID, "without `first` there is a row for every sequence");
     if (!aligned_to(r->first, DT_F32)) return set_err(c, CW_ERR_INVALID, "misaligned pointer");
     if (r->tokens > 0 && r->sequences > 0) {

@@ -238,7 +238,7 @@ static hipError_t launch_cache_as(const CacheArgs &a, hipStream_t s) {
 
 template <bool WRITE>
 static hipError_t launch_cache(const CacheArgs &a, hipStream_t s) {
-    if (a.tokens < 1 || a.sequences < 1 || a.cache.head_dim % 16 != 0 || a.cache.head_dim > kAttendMostDim || (int64_t)a.tokens * 2 * a.cache.kv_heads > INT32_MAX) return hipErrorInvalidValue;
+    if (a.tokens < 1 || a.sequences < 1 || a.cache.head_dim % 16 != 0 || a.cache.head_dim > kAttendMostDim || (int64_t)a.tokens * 2 * a.cache.kv_heads > kCacheMostRows) return hipErrorInvalidValue;
     if (a.dtype == DT_F32) return launch_cache_as<float, WRITE>(a, s);
     return a.dtype == DT_F16 ? launch_cache_as<f16, WRITE>(a, s) : launch_cache_as<bf16, WRITE>(a, s);
 }

@@ -216,3 +216,13 @@ def test_binding_refuses_tensors_that_do_not_fit(ctx):
     assert raises(cw.CwError, prompt, window=1 << 40).status == UNSUPPORTED
     assert raises(cw.CwError, prompt, causal=False, window=3).status == INVALID
     assert raises(cw.CwError, prompt, scale=float("nan")).status == INVALID
+
+
+@pytest.mark.parametrize("call", ["cw_cache_write", "cw_cache_read"])
+@pytest.mark.parametrize("tokens, let_through", [(13944699, False), (13944274, False), (13944273, True)])
+def test_rows_that_32_bits_count(ctx, call, tokens, let_through):
+    """Twice 77 rows a token: 2^31 - 2 of them, and one token on either side of what is left for the last workgroup's waves."""
+    cache = dict(kv_heads=77, page_stride=77 * 16 * 64)
+    change = dict(tokens=tokens, k_stride=77 * 64, v_stride=77 * 64)
+    st, why = refusal(ctx, call, cw.cw_cache_args, ROWS, change, cache)
+    assert (st, why) == PLANNING if let_through else st == UNSUPPORTED
