@@ -297,16 +297,16 @@ def _vector(t, what, device, count, kind):
     return t.data_ptr()
 
 
-def _heads(t, what, device, shape):
-    """(address, row stride, head stride) of [rows][heads][head_dim] on GPU `device` whose last elements are contiguous."""
+def _heads(t, what, device, rows, heads, shape=None):
+    """(address, row stride, head stride) of [rows][heads][head_dim], which is `shape` if that is not known yet, on GPU `device` whose last elements are contiguous."""
     if t.get_device() != device:
         raise ValueError("%s is not on the context's GPU" % what)
-    if t.shape != shape:
+    if shape is not None and t.shape != shape:
         raise ValueError("%s is %s, not %s" % (what, tuple(t.shape), tuple(shape)))
     row, head, step = t.stride()
     if step != 1:
         raise ValueError("%s: numbers of a head must be contiguous" % what)
-    return t.data_ptr(), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
+    return t.data_ptr(), row if rows > 1 else 0, head if heads > 1 else 0
 
 
 def _ints(t, what, device, count):
@@ -327,13 +327,14 @@ def _floats(t, what, device, count):
 
 def _table(table, device):
     """(address of the table, its row stride, sequences, pages a row)."""
-    if table.dim() != 2:
-        raise ValueError("table is %s, not (sequences, pages)" % (tuple(table.shape),))
+    shape = table.shape
+    if len(shape) != 2:
+        raise ValueError("table is %s, not (sequences, pages)" % (tuple(shape),))
     if table.dtype is not _int32:
         raise ValueError("table holds int32")
     if table.get_device() != device:
         raise ValueError("table is not on the context's GPU")
-    sequences, pages = table.shape
+    sequences, pages = shape
     row, step = table.stride()
     if step != 1 and pages > 1:
         raise ValueError("table: elements of a row must be contiguous")
@@ -606,14 +607,14 @@ class Context:
         return Cache(self._device, k, v, k_exp, v_exp)
 
     def _cache_rows(self, call, cache, k, v, table, lengths, first, stream):
-        if k.dim() != 3:
-            raise ValueError("k is %s, not (tokens, kv_heads, head_dim)" % (tuple(k.shape),))
-        dtype, on, tokens = k.dtype, self._device, k.shape[0]
+        shape, heads = k.shape, cache.kv_heads
+        if len(shape) != 3 or shape[1] != heads or shape[2] != cache.head_dim:
+            raise ValueError("k is %s, not (tokens, %d, %d)" % (tuple(shape), heads, cache.head_dim))
+        dtype, on, tokens = k.dtype, self._device, shape[0]
         if dtype is not v.dtype:
             raise TypeError("k and v are of different types")
-        shape = (tokens, cache.kv_heads, cache.head_dim)
-        kp, ks, kh = _heads(k, "k", on, shape)
-        vp, vs, vh = _heads(v, "v", on, shape)
+        kp, ks, kh = _heads(k, "k", on, tokens, heads)
+        vp, vs, vh = _heads(v, "v", on, tokens, heads, shape)
         tp, ts, sequences, pages = _table(table, on)
         try:
             args = _pack_cache_args(cache.address, kp, vp, 0 if first is None else _ints(first, "first", on, sequences + 1), _ints(lengths, "lengths", on, sequences), tp,
@@ -636,15 +637,15 @@ class Context:
     def attend_one(self, q, cache, table, lengths, y, scale, window=0, lse=None, workspace=None, stream=None):
         """y[sequences][heads][head_dim] = attention of q, a token of each sequence, over the lengths[s] tokens (the last `window`) in the pages table[s] of
         `cache`; lse [sequences][heads] fp32 is written if there is one.  workspace: uint8, zeros before its first call."""
-        if q.dim() != 3:
-            raise ValueError("q is %s, not (sequences, heads, head_dim)" % (tuple(q.shape),))
-        on, dtype, heads = self._device, q.dtype, q.shape[1]
+        on, dtype, shape = self._device, q.dtype, q.shape
+        tp, ts, sequences, pages = _table(table, on)
+        if len(shape) != 3 or shape[0] != sequences or shape[2] != cache.head_dim:
+            raise ValueError("q is %s, not (%d, heads, %d)" % (tuple(shape), sequences, cache.head_dim))
         if y.dtype is not dtype:
             raise TypeError("q and y are of different types")
-        tp, ts, sequences, pages = _table(table, on)
-        shape = (sequences, heads, cache.head_dim)
-        qp, qs, qh = _heads(q, "q", on, shape)
-        yp, ys, yh = _heads(y, "y", on, shape)
+        heads = shape[1]
+        qp, qs, qh = _heads(q, "q", on, sequences, heads)
+        yp, ys, yh = _heads(y, "y", on, sequences, heads, shape)
         space = workspace.numel() if workspace is not None else 0
         try:
             args = _pack_attend_one(cache.address, qp, yp, _floats(lse, "lse", on, sequences * heads), _ints(lengths, "lengths", on, sequences), tp,
@@ -663,23 +664,23 @@ class Context:
     def attend(self, q, k, v, y, first, scale, first_k=None, causal=True, window=0, lse=None, stream=None):
         """y[tokens][heads][head_dim] = attention of packed queries: rows first[s]..first[s + 1] - 1 of q over rows first_k[s]..first_k[s + 1] - 1 (the same, without
         first_k) of k and v [keys][kv_heads][head_dim]; lse [tokens][heads] fp32 is written if there is one."""
-        if q.dim() != 3 or k.dim() != 3:
-            raise ValueError("q is %s, k %s, not (tokens, heads, head_dim)" % (tuple(q.shape), tuple(k.shape)))
-        dtype, on, shape, sequences = q.dtype, self._device, q.shape, first.numel() - 1
+        dtype, on, shape, shape_k, sequences = q.dtype, self._device, q.shape, k.shape, first.numel() - 1
+        if len(shape) != 3 or len(shape_k) != 3 or shape[2] != shape_k[2]:
+            raise ValueError("q is %s, k %s, not (tokens, heads, head_dim)" % (tuple(shape), tuple(shape_k)))
         if k.dtype is not dtype or v.dtype is not dtype or y.dtype is not dtype:
             raise TypeError("q, k, v and y are of different types")
         tokens, heads, head_dim = shape
-        keys = (k.shape[0], k.shape[1], head_dim)
-        qp, qs, qh = _heads(q, "q", on, shape)
-        kp, ks, kh = _heads(k, "k", on, keys)
-        vp, vs, vh = _heads(v, "v", on, keys)
-        yp, ys, yh = _heads(y, "y", on, shape)
+        keys, kv_heads, _ = shape_k
+        qp, qs, qh = _heads(q, "q", on, tokens, heads)
+        kp, ks, kh = _heads(k, "k", on, keys, kv_heads)
+        vp, vs, vh = _heads(v, "v", on, keys, kv_heads, shape_k)
+        yp, ys, yh = _heads(y, "y", on, tokens, heads, shape)
         try:
             args = _pack_attend(qp, kp, vp, yp, _floats(lse, "lse", on, tokens * heads), _ints(first, "first", on, sequences + 1),
                                 0 if first_k is None else _ints(first_k, "first_k", on, sequences + 1), qs, qh, ks, kh, vs, vh, ys, yh,
-                                tokens, keys[0], sequences, heads, keys[1], head_dim, causal, window, _element_codes[dtype], scale)
+                                tokens, keys, sequences, heads, kv_heads, head_dim, causal, window, _element_codes[dtype], scale)
         except (struct.error, OverflowError) as e:
-            raise _refused(e, tokens=tokens, keys=keys[0], sequences=sequences, window=window, scale=scale) from None
+            raise _refused(e, tokens=tokens, keys=keys, sequences=sequences, window=window, scale=scale) from None
         status = _lib.cw_attend(self._h, args, _on(stream))
         if status < 0:
             self._check(status)
