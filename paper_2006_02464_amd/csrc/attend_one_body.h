@@ -23,7 +23,8 @@ struct AttendOneKernel {
     AttendOneArgs a;
     int32_t group, blocks;   // query heads of a key head, blocks of kOneHeads of them
     int32_t items;           // of a sequence: key heads times blocks
-    FastDiv by_parts, by_kv_heads, by_items, by_chunks;   // chunks: 16 bytes of a head's results in fp32
+    int32_t inner, parts_outer;   // of the grid: what follows within the other, items within parts or parts within items
+    FastDiv by_inner, by_kv_heads, by_items, by_chunks;   // chunks: 16 bytes of a head's results in fp32
     int32_t parts, fewest;   // of a sequence at most, and steps that are worth one
     float c;                 // |scale| / ln 2
 };
@@ -485,7 +486,7 @@ constexpr int one_waves(bool codes, int rb) { return rb / (codes ? 1 : 2) <= 128
 template <typename T, bool CODES, int RB, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, one_waves(CODES, RB)) void attend_one_kernel(const AttendOneKernel f) {
     __shared__ OneShared<CODES, RB, WAVES> shared;
-    const int item = fast_div(blockIdx.x, f.by_parts), part = blockIdx.x - item * f.parts, s = fast_div(item, f.by_items), hh = item - s * f.items;
+    const int outer = fast_div(blockIdx.x, f.by_inner), inner = blockIdx.x - outer * f.inner, item = f.parts_outer ? inner : outer, part = f.parts_outer ? outer : inner, s = fast_div(item, f.by_items), hh = item - s * f.items;
     const OneRange range = one_range<one_tokens(RB)>(f.a, f.a.lengths[s]);
     const int parts = max(1, min(f.parts, range.steps / f.fewest));
     if (part >= parts) return;
@@ -495,7 +496,7 @@ __global__ __launch_bounds__(64 * WAVES, one_waves(CODES, RB)) void attend_one_k
     attend_one_part<T, CODES, RB, WAVES>(f, shared, s, hh, range, step, min(step + each, range.step0 + range.steps), part, parts, item * f.parts);
 }
 
-inline AttendOneKernel one_kernel(const AttendOneArgs &a, int64_t parts, int fewest) {
+inline AttendOneKernel one_kernel(const AttendOneArgs &a, int64_t parts, int fewest, bool parts_outer) {
     AttendOneKernel f{};
     f.a = a;
     f.group = a.heads / a.cache.kv_heads;
@@ -503,7 +504,9 @@ inline AttendOneKernel one_kernel(const AttendOneArgs &a, int64_t parts, int few
     f.items = f.blocks * a.cache.kv_heads;
     f.parts = (int)std::max<int64_t>(parts, 1);
     f.fewest = fewest;
-    f.by_parts = make_fast_div((uint32_t)f.parts);
+    f.parts_outer = parts_outer;
+    f.inner = parts_outer ? (int)std::min<int64_t>((int64_t)a.sequences * f.items, INT32_MAX) : f.parts;   // more items are refused
+    f.by_inner = make_fast_div((uint32_t)f.inner);
     f.by_kv_heads = make_fast_div((uint32_t)a.cache.kv_heads);
     f.by_items = make_fast_div((uint32_t)f.items);
     f.by_chunks = make_fast_div((uint32_t)a.cache.head_dim / 4);
@@ -518,9 +521,9 @@ inline int64_t one_records(const AttendOneArgs &a, int64_t items) {
 }
 
 template <typename T, bool CODES, int RB, int WAVES>
-hipError_t launch_attend_one_as(const AttendOneArgs &a, int64_t items, int64_t steps, int64_t parts, int fewest, hipStream_t s) {
+hipError_t launch_attend_one_as(const AttendOneArgs &a, int64_t items, int64_t steps, int64_t parts, int fewest, bool parts_outer, hipStream_t s) {
     parts = std::min({parts, (int64_t)kOneMostParts, steps / fewest, one_records(a, items) / items});
-    const AttendOneKernel f = one_kernel(a, parts, fewest);
+    const AttendOneKernel f = one_kernel(a, parts, fewest, parts_outer);
     if (items * f.parts > INT32_MAX) return hipErrorInvalidValue;
     attend_one_kernel<T, CODES, RB, WAVES><<<dim3((unsigned)(items * f.parts)), 64 * WAVES, 0, s>>>(f);
     return hipGetLastError();
@@ -533,10 +536,15 @@ hipError_t launch_attend_one_row(const AttendOneArgs &a, hipStream_t s) {
     int64_t tokens = (int64_t)a.table_pages << a.cache.page_shift;
     if (a.window > 0) tokens = std::min<int64_t>(tokens, (int64_t)a.window + TOKENS - 1);
     const int64_t steps = (tokens + TOKENS - 1) / TOKENS;
-    if (items >= 288 && tokens <= 1024) return launch_attend_one_as<T, CODES, RB, 1>(a, items, steps, (4096 + items - 1) / items, 512 / TOKENS, s);
+    // `slots` workgroups of four waves run at once, as LDS has it.  Up to as many items: parts fill them, of 256 tokens at least (4 sequences of 810 to 1999, 4 heads of 80 bf16 11.4 us, of 512 tokens 15.0; but
+    // 2 of 1486 and 5604, 64 heads over 4 in e4m3, 17.3 and 16.8), an item's behind one another: neighbours go to different XCDs (9 of 100 to 9000, 16 heads of 64 40.5 us, with all items' parts p behind one another 45.2).
     constexpr int64_t slots = 2 * WAVES * (2 * TOKENS * RB + 256) > 80 * 1024 ? 256 : 512;
-    if (items <= slots) return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, slots / items, 64 / TOKENS * WAVES, s);
-    return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, (4 * slots + items - 1) / items, 64 / TOKENS * WAVES, s);
+    if (items <= slots) return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, slots / items, 64 / TOKENS * WAVES, false, s);
+    // More, of few tokens, get a wave each: 200 of 30 to 150, 8 heads of 128 18.5 us for 28.8, 150 of 30 to 300 29.5 for 34.1, 40 of 3 to 30 5.0 for 8.2; but 34 of 30 to 300 (272 items) 14.1 for 10.0, 60 of 30 to 400 17.6 for 14.8.
+    if (tokens <= 128 || (tokens <= 320 && items > 2 * slots)) return launch_attend_one_as<T, CODES, RB, 1>(a, items, steps, 1, 1, true, s);
+    // Else what a workgroup spends before its tokens, behind them and on meeting others is made up for by long parts only: 200 of up to 4096 in e4m3, 8 heads, 175 us, in parts of 256 tokens 187; 36 of up to 16000 219, whole
+    // 239.  All items' first parts come first: of two parts behind one another the second is empty for all but the longest, which leaves every other XCD without work (64 of up to 8192 284 us for 228).
+    return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, (4 * slots + items - 1) / items, 2048 / TOKENS, true, s);
 }
 
 template <typename T, bool CODES>
