@@ -27,7 +27,7 @@ struct AttendOneKernel {
     int32_t items;           // of a sequence: key heads times blocks
     int32_t inner, parts_outer;   // of the grid: what follows within the other, items within parts or parts within items
     FastDiv by_inner, by_kv_heads, by_items, by_chunks;   // chunks: 16 bytes of a head's results in fp32
-    int32_t parts, fewest;   // of a sequence at most, and steps that are worth one
+    int32_t parts, fewest, from;   // of a sequence at most; steps of a part at least; steps of a sequence that is worth parts
     float c;                 // |scale| / ln 2
 };
 
@@ -115,6 +115,7 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
     const int block = fast_div(hh, f.by_kv_heads), kvh = hh - block * c.kv_heads;
     const int heads = min(kOneHeads, f.group - block * kOneHeads), head0 = kvh * f.group + block * kOneHeads;
     const int from = range.from, len = range.len;
+    const bool whole = WAVES == 1 || parts == 1;   // a single wave has all of a sequence
 
     // Q as the second operand of the first product: with codes 16 numbers of a head in a row, whose halves two steps of the product take.
     v8 q[DP / 32];
@@ -381,7 +382,7 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
 #pragma unroll
         for (int w = 0; w < WAVES; ++w)
             v += by[w] * *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>((lds_char *)lds + w * STAGES * STAGE + h * (DP * 4) + ((d4 ^ (h & 7)) << 4));
-        if (parts == 1) {
+        if (whole) {
             store(h, d4, v, total);
             if (d4 == 0) store_lse(h, m, total);
         } else {
@@ -395,7 +396,7 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
             if (d4 == 0) put(heads * c.head_dim + 2 * h, m, total);
         }
     }
-    if (parts == 1) return;
+    if (whole) return;
 
     // Parts meet in memory: each stores past its XCD's own L2, then counts; the last one to come joins them in their order.  A store counts as outstanding until it is where loads of that
     // scope look, which is what makes the relaxed accesses enough, as in the answer over logits.
@@ -490,7 +491,7 @@ __global__ __launch_bounds__(64 * WAVES, one_waves(CODES, RB)) void attend_one_k
     __shared__ OneShared<CODES, RB, WAVES> shared;
     const int outer = fast_div(blockIdx.x, f.by_inner), inner = blockIdx.x - outer * f.inner, item = f.parts_outer ? inner : outer, part = f.parts_outer ? outer : inner, s = fast_div(item, f.by_items), hh = item - s * f.items;
     const OneRange range = one_range<one_tokens(RB)>(f.a, f.a.lengths[s]);
-    const int parts = max(1, min(f.parts, range.steps / f.fewest));
+    const int parts = WAVES == 1 || range.steps < f.from ? 1 : max(1, min(f.parts, range.steps / f.fewest));
     if (part >= parts) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int each = (int)((unsigned)(range.steps + parts * WAVES - 1) / (unsigned)(parts * WAVES));   // steps of a wave
@@ -498,7 +499,7 @@ __global__ __launch_bounds__(64 * WAVES, one_waves(CODES, RB)) void attend_one_k
     attend_one_part<T, CODES, RB, WAVES>(f, shared, s, hh, range, step, min(step + each, range.step0 + range.steps), part, parts, item * f.parts);
 }
 
-inline AttendOneKernel one_kernel(const AttendOneArgs &a, int64_t parts, int fewest, bool parts_outer) {
+inline AttendOneKernel one_kernel(const AttendOneArgs &a, int64_t parts, int fewest, int from, bool parts_outer) {
     AttendOneKernel f{};
     f.a = a;
     f.group = a.heads / a.cache.kv_heads;
@@ -506,6 +507,7 @@ inline AttendOneKernel one_kernel(const AttendOneArgs &a, int64_t parts, int few
     f.items = f.blocks * a.cache.kv_heads;
     f.parts = (int)std::max<int64_t>(parts, 1);
     f.fewest = fewest;
+    f.from = from;
     f.parts_outer = parts_outer;
     f.inner = parts_outer ? (int)std::min<int64_t>((int64_t)a.sequences * f.items, INT32_MAX) : f.parts;   // more items are refused
     f.by_inner = make_fast_div((uint32_t)f.inner);
@@ -523,9 +525,9 @@ inline int64_t one_records(const AttendOneArgs &a, int64_t items) {
 }
 
 template <typename T, bool CODES, int RB, int WAVES>
-hipError_t launch_attend_one_as(const AttendOneArgs &a, int64_t items, int64_t steps, int64_t parts, int fewest, bool parts_outer, hipStream_t s) {
+hipError_t launch_attend_one_as(const AttendOneArgs &a, int64_t items, int64_t steps, int64_t parts, int fewest, int from, bool parts_outer, hipStream_t s) {
     parts = std::min({parts, (int64_t)kOneMostParts, steps / fewest, one_records(a, items) / items});
-    const AttendOneKernel f = one_kernel(a, parts, fewest, parts_outer);
+    const AttendOneKernel f = one_kernel(a, parts, fewest, from, parts_outer);
     if (items * f.parts > INT32_MAX) return hipErrorInvalidValue;
     attend_one_kernel<T, CODES, RB, WAVES><<<dim3((unsigned)(items * f.parts)), 64 * WAVES, 0, s>>>(f);
     return hipGetLastError();
@@ -539,14 +541,14 @@ hipError_t launch_attend_one_row(const AttendOneArgs &a, hipStream_t s) {
     if (a.window > 0) tokens = std::min<int64_t>(tokens, (int64_t)a.window + TOKENS - 1);
     const int64_t steps = (tokens + TOKENS - 1) / TOKENS;
     // `slots` workgroups of four waves run at once, as LDS has it.  Up to as many items: parts fill them, of 256 tokens at least (4 sequences of 810 to 1999, 4 heads of 80 bf16 11.4 us, of 512 tokens 15.0; but
-    // 2 of 1486 and 5604, 64 heads over 4 in e4m3, 17.3 and 16.8), an item's behind one another: neighbours go to different XCDs (9 of 100 to 9000, 16 heads of 64 40.5 us, with all items' parts p behind one another 45.2).
+    // 2 of 1486 and 5604, 64 heads over 4 in e4m3, 17.3 and 16.8), of sequences from 704 on (one of 600, 32 heads over 8 of 128 fp16, 8.3 us whole, 9.6 in two; one of 1000 11.6 whole, 9.1 in three), an item's behind one another: neighbours go to different XCDs (9 of 100 to 9000, 16 heads of 64 40.5 us, with all items' parts p behind one another 45.2).
     constexpr int64_t slots = 2 * WAVES * (2 * TOKENS * RB + 256) > 80 * 1024 ? 256 : 512;
-    if (items <= slots) return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, slots / items, 64 / TOKENS * WAVES, false, s);
+    if (items <= slots) return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, slots / items, 256 / TOKENS, 704 / TOKENS, false, s);
     // More, of few tokens, get a wave each: 200 of 30 to 150, 8 heads of 128 18.5 us for 28.8, 150 of 30 to 300 29.5 for 34.1, 40 of 3 to 30 5.0 for 8.2; but 34 of 30 to 300 (272 items) 14.1 for 10.0, 60 of 30 to 400 17.6 for 14.8.
-    if (tokens <= 128 || (tokens <= 320 && items > 2 * slots)) return launch_attend_one_as<T, CODES, RB, 1>(a, items, steps, 1, 1, true, s);
+    if (tokens <= 128 || (tokens <= 320 && items > 2 * slots)) return launch_attend_one_as<T, CODES, RB, 1>(a, items, steps, 1, 1, 0, true, s);
     // Else what a workgroup spends before its tokens, behind them and on meeting others is made up for by long parts only: 200 of up to 4096 in e4m3, 8 heads, 175 us, in parts of 256 tokens 187; 36 of up to 16000 219, whole
     // 239.  All items' first parts come first: of two parts behind one another the second is empty for all but the longest, which leaves every other XCD without work (64 of up to 8192 284 us for 228).
-    return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, (4 * slots + items - 1) / items, 2048 / TOKENS, true, s);
+    return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, (4 * slots + items - 1) / items, 2048 / TOKENS, 0, true, s);
 }
 
 template <typename T, bool CODES>

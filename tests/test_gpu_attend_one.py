@@ -82,6 +82,17 @@ def test_long(ctx, space, x, kept, length, sequences, heads, kv_heads, dim):
     check(ctx, space, pool, queries(sequences, heads, dim, x, 4))
 
 
+@pytest.mark.parametrize("x, kept, sequences, longest, dim", [(BF16, BF16, 140, (5000, 9001, 4096), 128), (F16, E4M3, 270, (4500, 2047), 64), (F16, F16, 140, (200,), 128), (BF16, BF16, 140, (321,), 256),
+                                                              (BF16, E4M3, 300, (128,), 64), (F16, F16, 300, (320, 319), 128)])
+def test_more_sequences_than_run_at_once(ctx, space, x, kept, sequences, longest, dim):
+    """Short ones, empty ones among them, and a few long ones: in parts, whole, or a wave each."""
+    lengths = [i * 7 % 41 for i in range(sequences)]
+    for i, n in enumerate(longest):
+        lengths[(i * 97 + 5) % sequences] = n
+    pool = Pages(lengths, 2, 16, dim, kept, seed=11).fill(9)
+    check(ctx, space, pool, queries(sequences, 6, dim, x, 2))
+
+
 @pytest.mark.parametrize("window", [1, 15, 16, 33, 64, 100, 512, 5000])
 @pytest.mark.parametrize("kept", [BF16, E4M3])
 def test_windows(ctx, space, window, kept):
