@@ -29,6 +29,7 @@ struct AttendOneKernel {
     FastDiv by_inner, by_kv_heads, by_items, by_chunks;   // chunks: 16 bytes of a head's results in fp32
     int32_t parts, fewest, from;   // of a sequence at most; steps of a part at least; steps of a sequence that is worth parts
     float c;                 // |scale| / ln 2
+    int32_t most;            // EVEN: parts of all sequences together
 };
 
 // Where 16-byte chunk c of row r lies: what is read at once lies in different banks.  K: 16 rows, one chunk; V: 8 rows, two chunks (16 bits) or rows 0..7 and 16..23, one (codes).
@@ -485,18 +486,58 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
 
 constexpr int one_waves(bool codes, int rb) { return rb / (codes ? 1 : 2) <= 128 ? 2 : 1; }   // of a SIMD, at least
 
-// A grid of parts of items, items being sequences and their heads.
-template <typename T, bool CODES, int RB, int WAVES>
+// A grid of parts of items, items being sequences and their heads.  EVEN: parts of up to 64 sequences, of the same steps whatever these have; a kernel of its own, as small calls feel the code that they skip (0.1 us of 4.6).
+template <typename T, bool CODES, int RB, int WAVES, bool EVEN>
 __global__ __launch_bounds__(64 * WAVES, one_waves(CODES, RB)) void attend_one_kernel(const AttendOneKernel f) {
     __shared__ OneShared<CODES, RB, WAVES> shared;
-    const int outer = fast_div(blockIdx.x, f.by_inner), inner = blockIdx.x - outer * f.inner, item = f.parts_outer ? inner : outer, part = f.parts_outer ? outer : inner, s = fast_div(item, f.by_items), hh = item - s * f.items;
-    const OneRange range = one_range<one_tokens(RB)>(f.a, f.a.lengths[s]);
-    const int parts = WAVES == 1 || range.steps < f.from ? 1 : max(1, min(f.parts, range.steps / f.fewest));
-    if (part >= parts) return;
+    int s, hh, part, parts, first;
+    OneRange range;
+    if constexpr (EVEN) {
+        // The steps of a part are the fewest with which all parts run at once, found by halving: a lane a sequence.
+        const int lane = threadIdx.x & 63, outer = fast_div(blockIdx.x, f.by_items);
+        const int mine = lane < f.a.sequences ? one_range<one_tokens(RB)>(f.a, f.a.lengths[lane]).steps : 0;
+        auto reduce = [&](int v, auto op) {
+            auto dpp = [](int x, auto control, auto mask) { return __builtin_amdgcn_update_dpp(0, x, decltype(control)::value, decltype(mask)::value, 0xf, false); };
+            v = op(v, dpp(v, std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{}));
+            v = op(v, dpp(v, std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{}));
+            v = op(v, dpp(v, std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{}));
+            v = op(v, dpp(v, std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{}));
+            v = op(v, dpp(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{}));
+            return op(v, dpp(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{}));   // lane i: of lanes 0..i where op is a sum
+        };
+        auto sum = [](int p, int q) { return p + q; };
+        auto parts_of = [&](int steps) { return lane >= f.a.sequences ? 0 : mine < f.from ? 1 : min(kOneMostParts, (int)ceilf((float)mine / (float)steps)); };   // rounded, the quotient is not above the next whole number
+        const int longest = __builtin_amdgcn_readlane(reduce(mine, [](int p, int q) { return max(p, q); }), 63);
+        int low = f.fewest - 1, high = max(longest, f.fewest);   // too few, and enough
+        for (int i = 0; i < 8 && high - low > 1; ++i) {
+            const int mid = i == 0 ? low + 1 : low + (high - low) / 2;
+            if (__builtin_amdgcn_readlane(reduce(parts_of(mid), sum), 63) <= f.most) high = mid;
+            else low = mid;
+        }
+        const int of_lane = parts_of(high), up = reduce(of_lane, sum);
+        const uint64_t here = __ballot(up - of_lane <= outer && outer < up);
+        if (!here) return;
+        s = __builtin_ctzll(here);
+        parts = __builtin_amdgcn_readlane(of_lane, s);
+        const int base = __builtin_amdgcn_readlane(up, s) - parts;
+        hh = blockIdx.x - outer * f.items;
+        part = outer - base;
+        first = base * f.items + hh * parts;
+        range = one_range<one_tokens(RB)>(f.a, f.a.lengths[s]);
+    } else {
+        const int outer = fast_div(blockIdx.x, f.by_inner), inner = blockIdx.x - outer * f.inner, item = f.parts_outer ? inner : outer;
+        part = f.parts_outer ? outer : inner;
+        s = fast_div(item, f.by_items);
+        hh = item - s * f.items;
+        first = item * f.parts;
+        range = one_range<one_tokens(RB)>(f.a, f.a.lengths[s]);
+        parts = WAVES == 1 || range.steps < f.from ? 1 : max(1, min(f.parts, range.steps / f.fewest));
+        if (part >= parts) return;
+    }
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int each = (int)((unsigned)(range.steps + parts * WAVES - 1) / (unsigned)(parts * WAVES));   // steps of a wave
     const int step = range.step0 + (part * WAVES + wave) * each;
-    attend_one_part<T, CODES, RB, WAVES>(f, shared, s, hh, range, step, min(step + each, range.step0 + range.steps), part, parts, item * f.parts);
+    attend_one_part<T, CODES, RB, WAVES>(f, shared, s, hh, range, step, min(step + each, range.step0 + range.steps), part, parts, first);
 }
 
 inline AttendOneKernel one_kernel(const AttendOneArgs &a, int64_t parts, int fewest, int from, bool parts_outer) {
@@ -529,7 +570,7 @@ hipError_t launch_attend_one_as(const AttendOneArgs &a, int64_t items, int64_t s
     parts = std::min({parts, (int64_t)kOneMostParts, steps / fewest, one_records(a, items) / items});
     const AttendOneKernel f = one_kernel(a, parts, fewest, from, parts_outer);
     if (items * f.parts > INT32_MAX) return hipErrorInvalidValue;
-    attend_one_kernel<T, CODES, RB, WAVES><<<dim3((unsigned)(items * f.parts)), 64 * WAVES, 0, s>>>(f);
+    attend_one_kernel<T, CODES, RB, WAVES, false><<<dim3((unsigned)(items * f.parts)), 64 * WAVES, 0, s>>>(f);
     return hipGetLastError();
 }
 
@@ -543,6 +584,16 @@ hipError_t launch_attend_one_row(const AttendOneArgs &a, hipStream_t s) {
     // `slots` workgroups of four waves run at once, as LDS has it.  Up to as many items: parts fill them, of 256 tokens at least (4 sequences of 810 to 1999, 4 heads of 80 bf16 11.4 us, of 512 tokens 15.0; but
     // 2 of 1486 and 5604, 64 heads over 4 in e4m3, 17.3 and 16.8), of sequences from 704 on (one of 600, 32 heads over 8 of 128 fp16, 8.3 us whole, 9.6 in two; one of 1000 11.6 whole, 9.1 in three), an item's behind one another: neighbours go to different XCDs (9 of 100 to 9000, 16 heads of 64 40.5 us, with all items' parts p behind one another 45.2).
     constexpr int64_t slots = 2 * WAVES * (2 * TOKENS * RB + 256) > 80 * 1024 ? 256 : 512;
+    // Parts of the same steps whatever the lengths, no more than run at once, an item's neighbours those of the other heads: 6 of 9661 to 38277, 64 heads over 8 of 256 bf16, 218 us, as many parts of every sequence 240;
+    // 5 of 100 to 20000, 32 heads over 8 of 128 42.7 and 50.5, 12 of 30 to 5000 29.7 and 36.2; 14 of 3726 to 4520, 80 over 5 of 256, 73.5 and 71.3. Where a record is large a part is too: 7 of 2441 to 6183, 32 heads over 2 of 128,
+    // 23.8 us with parts of 256 tokens, 18.9 of 512.
+    if (items <= slots && a.sequences > 1 && a.sequences <= 64 && tokens >= 704) {
+        const int64_t grid = std::max(items, std::min(slots, one_records(a, items)));
+        AttendOneKernel f = one_kernel(a, 1, (std::min(a.heads / a.cache.kv_heads, kOneHeads) * a.cache.head_dim > 1024 ? 512 : 256) / TOKENS, 704 / TOKENS, false);
+        f.most = (int)(grid / f.items);
+        attend_one_kernel<T, CODES, RB, WAVES, true><<<dim3((unsigned)grid), 64 * WAVES, 0, s>>>(f);
+        return hipGetLastError();
+    }
     if (items <= slots) return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, slots / items, 256 / TOKENS, 704 / TOKENS, false, s);
     // More, of few tokens, get a wave each: 200 of 30 to 150, 8 heads of 128 18.5 us for 28.8, 150 of 30 to 300 29.5 for 34.1, 40 of 3 to 30 5.0 for 8.2; but 34 of 30 to 300 (272 items) 14.1 for 10.0, 60 of 30 to 400 17.6 for 14.8.
     if (tokens <= 128 || (tokens <= 320 && items > 2 * slots)) return launch_attend_one_as<T, CODES, RB, 1>(a, items, steps, 1, 1, 0, true, s);

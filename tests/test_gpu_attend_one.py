@@ -93,6 +93,13 @@ def test_more_sequences_than_run_at_once(ctx, space, x, kept, sequences, longest
     check(ctx, space, pool, queries(sequences, 6, dim, x, 2))
 
 
+@pytest.mark.parametrize("x, kept, lengths, heads, dim", [(BF16, BF16, [i * 37 % 900 for i in range(63)] + [3000], 6, 128), (F16, F16, [i * 37 % 900 for i in range(64)] + [3000], 6, 64),
+                                                          (BF16, E4M3, [0] * 40 + [9000] + [0] * 20, 34, 128), (F16, F16, [703, 704, 705, 735, 736, 737] * 10, 2, 256), (F16, E4M3, [20000, 1], 32, 64)])
+def test_parts_of_the_same_steps(ctx, space, x, kept, lengths, heads, dim):
+    pool = Pages(lengths, 2, 16, dim, kept, seed=12).fill(8)
+    check(ctx, space, pool, queries(len(lengths), heads, dim, x, 2))
+
+
 @pytest.mark.parametrize("window", [1, 15, 16, 33, 64, 100, 512, 5000])
 @pytest.mark.parametrize("kept", [BF16, E4M3])
 def test_windows(ctx, space, window, kept):
