@@ -567,7 +567,7 @@ inline int64_t one_records(const AttendOneArgs &a, int64_t items) {
 
 template <typename T, bool CODES, int RB, int WAVES>
 hipError_t launch_attend_one_as(const AttendOneArgs &a, int64_t items, int64_t steps, int64_t parts, int fewest, int from, bool parts_outer, hipStream_t s) {
-    parts = std::min({parts, (int64_t)kOneMostParts, steps / fewest, one_records(a, items) / items});
+    parts = steps < from ? 1 : std::min({parts, (int64_t)kOneMostParts, steps / fewest, one_records(a, items) / items});
     const AttendOneKernel f = one_kernel(a, parts, fewest, from, parts_outer);
     if (items * f.parts > INT32_MAX) return hipErrorInvalidValue;
     attend_one_kernel<T, CODES, RB, WAVES, false><<<dim3((unsigned)(items * f.parts)), 64 * WAVES, 0, s>>>(f);
