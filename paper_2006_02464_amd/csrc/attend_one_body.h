@@ -415,8 +415,9 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
         return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<uint64_t *>(record_of(p) + at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
     };
     // A trip to memory takes longer than all the arithmetic: where a head's results are fewer than the threads, groups of these take every so manieth part, and the first
-    // eight of each thread are under way while the parts' weights are made, a lane a part.
-    constexpr int BATCH = 8;
+    // four of each thread are under way while the parts' weights are made, a lane a part.  Eight at a time load more than there is where the parts are few, past the L2 and so slowly, and their code is longer: one sequence of 1000,
+    // 32 heads over 8 of 128, 9.0 us for 8.4, 25 of 100 to 4000 26.5 for 25.4; but one of 65000, 64 heads over 4 in e4m3 (64 parts), 36.3 for 39.7.
+    constexpr int BATCH = 4;
     const int groups = items < THREADS ? (int)((THREADS + 0.5f) * __builtin_amdgcn_rcpf((float)items)) : 1;
     const int g = groups > 1 ? (int)((tid + 0.5f) * __builtin_amdgcn_rcpf((float)items)) : 0, i0 = tid - g * items * (groups > 1);
     f32x2 lo[BATCH], hi[BATCH];
