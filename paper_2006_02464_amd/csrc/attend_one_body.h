@@ -583,7 +583,7 @@ hipError_t launch_attend_one_row(const AttendOneArgs &a, hipStream_t s) {
     if (a.window > 0) tokens = std::min<int64_t>(tokens, (int64_t)a.window + TOKENS - 1);
     const int64_t steps = (tokens + TOKENS - 1) / TOKENS;
     // `slots` workgroups of four waves run at once, as LDS has it.  Up to as many items: parts fill them, of 256 tokens at least (4 sequences of 810 to 1999, 4 heads of 80 bf16 11.4 us, of 512 tokens 15.0; but
-    // 2 of 1486 and 5604, 64 heads over 4 in e4m3, 17.3 and 16.8), of sequences from 704 on (one of 600, 32 heads over 8 of 128 fp16, 8.3 us whole, 9.6 in two; one of 1000 11.6 whole, 9.1 in three), an item's behind one another: neighbours go to different XCDs (9 of 100 to 9000, 16 heads of 64 40.5 us, with all items' parts p behind one another 45.2).
+    // 2 of 1486 and 5604, 64 heads over 4 in e4m3, 17.3 and 16.8), of sequences from 704 on (one of 600, 32 heads over 8 of 128 fp16, 8.3 us whole, 9.6 in two; one of 1000 11.6 whole, 8.4 in three), an item's behind one another: neighbours go to different XCDs (9 of 100 to 9000, 16 heads of 64 40.5 us, with all items' parts p behind one another 45.2).
     constexpr int64_t slots = 2 * WAVES * (2 * TOKENS * RB + 256) > 80 * 1024 ? 256 : 512;
     // Parts of the same steps whatever the lengths, no more than run at once, an item's neighbours those of the other heads: 6 of 9661 to 38277, 64 heads over 8 of 256 bf16, 218 us, as many parts of every sequence 240;
     // 5 of 100 to 20000, 32 heads over 8 of 128 42.7 and 50.5, 12 of 30 to 5000 29.7 and 36.2; 14 of 3726 to 4520, 80 over 5 of 256, 73.5 and 71.3. Where a record is large a part is too: 7 of 2441 to 6183, 32 heads over 2 of 128,
