@@ -412,8 +412,8 @@ size_t cw_attend_one_workspace_bytes(void);
 
 /* Attention of whole prompts, or of parts of them behind their histories, packed one behind the other: queries first[s]..first[s + 1] - 1 see keys
  * first_k[s]..first_k[s + 1] - 1 of their sequence.  causal: the last query sees all of the sequence's keys, the one before it all but the last, and so on
- * (query i of n those j <= i + m - n of m keys); with `window` > 0 the last `window` of these.  Else as cw_attend_one, with p in the second product in the values' type.  Rows outside
- * first[0]..first[sequences] - 1 are not touched. */
+ * (query i of n those j <= i + m - n of m keys); with `window` > 0 the last `window` of these.  Else as cw_attend_one, with p in the second product in the values' type, of fp16
+ * off by 2^-36 of the row's largest p at most where that is more than half a step.  Rows outside first[0]..first[sequences] - 1 are not touched. */
 typedef struct {
     const void *q;              /* [tokens][heads][head_dim], dtype */
     const void *k, *v;          /* [keys][kv_heads][head_dim], dtype; rows at most 2^23 elements apart */

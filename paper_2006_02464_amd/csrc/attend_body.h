@@ -12,7 +12,10 @@ namespace cw {
 // S^T = K Q^T and O^T = V^T P^T: in an accumulator of the matrix cores a lane has one row of the attention and 4 (lane / 32) + 8 j + 0..3 of the other side, so
 // maxima and sums of the softmax are a lane's own but for one exchange, and the eight numbers that a lane holds of S^T are those that the second product wants of P^T once it
 // takes its keys in that order.  K lies in LDS as it is, V too and is transposed by the reads of LDS that do that.
-// The running maximum follows the scores only where one is 2^8 times above it: weights may be up to 2^8, which costs none of their bits, and most tiles rescale nothing.
+// The running maximum follows the scores only where one is more than kSlack above it, so that most tiles rescale nothing.  Weights go into the second product in the values' type, half a step
+// of each, which leaves the result about a quarter further from the formula than its own rounding does: weights of two parts take half as many matrix instructions again and a third more time (8192 tokens of 32 heads over
+// 8 of 128 fp16 564 us and 757, 16 prompts of 33 to 2048 bf16 267 and 338).  fp16 ends early, so its weights refer to kShift below the maximum: the largest is 2^11 to 2^15, and what the type cannot hold
+// of a weight is at most 2^-36 of the largest, where it would be 2^-25 with the maximum itself.
 // The matrix cores and the card's power bound it: 8192 tokens of 32 heads over 8 of 128 fp16, causal, in 540 to 560 us, 980 to 1020 TFLOP/s at 1.7 GHz, where a library's product of 8192^3 reaches 1093; short prompts
 // what comes before and behind the tiles: 16 prompts of 33 to 2048 tokens, bf16, in 250 to 262 us, 740 to 780 TFLOP/s.  A third tile under way in LDS is no faster (9 prompts of 1737 to 2121, 40 heads over 5 of 80 352 us and 353, one of 2468 and one head 33 and 42), nor are
 // three waves a SIMD, whose registers spill (44 and 78 us for 60 prompts of 99 to 167, 32 heads over 8 of 80).
@@ -20,7 +23,10 @@ namespace cw {
 constexpr int kAttendWaves = 4;
 constexpr int attend_rows(int split) { return 32 * kAttendWaves / split; }   // of a workgroup
 constexpr int kAttendKeys = 64;   // of a tile: two of them and their successors fit a CU's LDS up to 128 numbers a head
-constexpr float kAttendSlack = 8.f;
+template <typename T>
+struct AttendWeights {   // in units of ln 2
+    static constexpr float kSlack = std::is_same<T, f16>::value ? 4.f : 8.f, kShift = std::is_same<T, f16>::value ? 11.f : 0.f;
+};
 
 struct AttendKernel {
     AttendArgs a;
@@ -33,6 +39,7 @@ struct AttendKernel {
 template <typename T, int DP, int SPLIT>
 __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_kernel(const AttendKernel f) {
     typedef typename Mfma<T>::v8 v8;
+    typedef AttendWeights<T> Weights;
     typedef T T2 __attribute__((ext_vector_type(2)));
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) unsigned char lds_char;
@@ -119,7 +126,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
     for (int p = 0; p < PANELS; ++p)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[p][e] = 0.f;
-    float top = -INFINITY, sum = 0.f;   // the maximum that weights refer to, in units of ln 2, and the sum of this lane's weights
+    float top = -INFINITY, sum = 0.f;   // the maximum, in units of ln 2, and the sum of this lane's weights, which refer to kShift less
     const int key_swz = (l32 >> 2) & 3;
     const unsigned mine = key_group * BLOCKS * 2048;   // this wave's keys in a panel
     const unsigned k_read[2] = {mine + (unsigned)(l32 * 64 + ((half ^ key_swz) << 4)), mine + (unsigned)(l32 * 64 + (((2 + half) ^ key_swz) << 4))};
@@ -160,7 +167,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
             const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
             most = fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1])) * f.c;
         }
-        if (__any(most > top + kAttendSlack || (top == -INFINITY && most > top))) {
+        if (__any(most > top + Weights::kSlack || (top == -INFINITY && most > top))) {
             const float now = fmaxf(top, most), by = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.f : now));
             top = now;
             sum *= by;
@@ -169,7 +176,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[p][e] *= by;
         }
-        const float ref = top == -INFINITY ? 0.f : top;
+        const float ref = top == -INFINITY ? 0.f : top - Weights::kShift;
         v8 w[2 * BLOCKS];   // P^T, sixteen keys each
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b)
@@ -238,7 +245,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
             const int at = __builtin_ctz(odd), t = side ? end - 1 - at : begin + at, base = wg_low + t * KEYS + key_group * BLOCKS * 32;
             f32x16 x[BLOCKS];
             v8 w[2 * BLOCKS];
-            const float ref = top == -INFINITY ? 0.f : top;
+            const float ref = top == -INFINITY ? 0.f : top - Weights::kShift;
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) {
                 const int key = base + b * 32 + l32;
@@ -323,7 +330,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
     const bool empty = sum == 0.f;
     const float by = empty ? 0.f : 1.f / sum;
     if (!inside) return;
-    if (a.lse && half == 0) a.lse[(int64_t)(q0 + my_query) * a.heads + my_head] = empty ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
+    if (a.lse && half == 0) a.lse[(int64_t)(q0 + my_query) * a.heads + my_head] = empty ? -INFINITY : (top - Weights::kShift + __builtin_amdgcn_logf(sum)) * 0.693147181f;
     T *to = static_cast<T *>(a.y) + (int64_t)(q0 + my_query) * a.y_stride + (int64_t)my_head * a.y_head_stride;
 #pragma unroll
     for (int p = 0; p < PANELS; ++p)
