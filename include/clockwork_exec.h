@@ -384,7 +384,8 @@ int32_t cw_cache_read(cw_ctx *ctx, const cw_cache_args *args, void *stream);
  *   y[s][h] = sum over t of p[t] * v[t][h'],  p = softmax over t of scale * q[s][h] . k[t][h'],  h' = h / (heads / kv_heads)
  * over the tokens t < lengths[s], with `window` > 0 the last `window` of them.  lse is the logarithm of the softmax's denominator, with which results over parts of a
  * sequence can be joined.  A row that sees no token has y 0 and lse -inf.  Products with the numbers as they are stored are exact, sums and the softmax fp32; of
- * fp16, and of E4M3, p goes into the second product in 11 bits, of bf16 in 15; the result is rounded once.  Scores of +inf or NaN make their row NaN; numbers of tokens that
+ * fp16, and of E4M3, p goes into the second product in 11 bits, off by 2^-36 of the row's largest at most where that is more (of p times the power of two of its token's value, with E4M3), of bf16 in 15; the
+ * result is rounded once.  An infinite value whose p is that small makes the result NaN.  Scores of +inf or NaN make their row NaN; numbers of tokens that
  * are not seen have no effect whatever they are.
  * Sequences are shared by several workgroups, which meet in `workspace`: its first CW_ATTEND_COUNTERS bytes must be zero before the first call and are zero behind every call.  Calls
  * that may overlap in time need a workspace each.  Without one (NULL), or with less than cw_attend_one_workspace_bytes(), a sequence's heads are shared less or not at all; the results

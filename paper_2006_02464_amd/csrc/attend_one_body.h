@@ -12,12 +12,13 @@ namespace cw {
 // Products are transposed, on 16 x 16 tiles of the matrix cores: S^T = K Q^T, whose lanes have a query and tokens 4 (lane / 16) + 0..3 of each half of the step, just what the second product,
 // O^T = V^T P^T, wants of P^T with its tokens in that order; V is transposed by the reads of LDS that do that.  Tokens that are not seen come from a line of zeros.
 // Codes of 8 bits become numbers of the queries' type for the first product and fp16 for the second, exactly; a key's exponent goes to its score, a value's to its weight before that is rounded:
-// weights refer to a maximum of their own.  bf16 weights go into the second product in two parts.
+// weights refer to a maximum of their own, which follows where one is 2^kSlack times above it.  bf16 weights go into the second product in two parts, 15 bits, which their loads hide; fp16 weights in one of 11 bits: a second
+// one leaves an error that is a tenth less and costs a call 8 to 18 % where little is read (one sequence of 1000 tokens, 32 heads over 8 of 128 fp16, 8.4 us and 9.3, of 300 6.2 and 7.3), 200 of up to 4096 in e4m3 173 us and 177.
+// fp16 ends early, so its weights refer to 2^11 below the maximum: what the type cannot hold of a weight is at most 2^-36 of the largest.
 // 64 sequences of 133 to 8192 tokens, 32 heads over 8 of 128 bf16, take 199 to 204 us, 5.4 TB/s; 200 of up to 4096, 64 heads over 8 in e4m3, 164 to 174; one of 32001 31, 4.2 TB/s, of which about 12 go to the launch, the first
 // bytes and the meeting.  Where the loads are all there is, more of them under way (four steps, smaller ones) gave nothing.
 constexpr int one_tokens(int row_bytes) { return row_bytes > 256 ? 16 : 32; }   // of a step: 16 KB at most
 constexpr int kOneHeads = 16;
-constexpr float kOneSlack = 8.f;   // maxima follow beyond 2^8
 constexpr int kOneMostParts = 64;   // a lane each where they meet
 constexpr int kOneCounters = 65536 / 4;
 
@@ -107,6 +108,7 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
     constexpr unsigned ALL = TOKENS == 32 ? 0xffffffffu : (1u << TOKENS) - 1u;
     static_assert(!CODES || TOKENS == 32, "codes' exponents: a lane each of keys and of values");
     constexpr bool TWO = std::is_same<VT, bf16>::value;
+    constexpr float kSlack = TWO ? 8.f : 4.f, kShift = TWO ? 0.f : 11.f;   // in units of ln 2
     auto &lds = shared.lds;
     auto &tops = shared.tops;
     auto &sums = shared.sums;
@@ -201,7 +203,7 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
     f32x4 o[DP / 16];
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float top = -INFINITY, sum = 0.f, top_w = -INFINITY;   // maxima in units of ln 2: of the scores, and of what the weights refer to
+    float top = -INFINITY, sum = 0.f, top_w = -INFINITY;   // maxima in units of ln 2: of the scores, and with codes of the scores with their values' exponents
     const auto larger = [](float p, float q) { return max3(p, q, q); };
     unsigned seen_next = step < end ? load(step, step & 1) : 0u;    // of the next step's tokens, a bit each
     for (; step < end; ++step) {
@@ -267,11 +269,11 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
             return of_four(m, larger);
         };
         const float most = most_of(x);
-        bool follow = most > top + kOneSlack || (top == -INFINITY && most > top);
+        bool follow = most > top + kSlack || (top == -INFINITY && most > top);
         float most_w = most;
         if constexpr (CODES) {
             most_w = most_of(z);
-            follow |= most_w > top_w + kOneSlack || (top_w == -INFINITY && most_w > top_w);
+            follow |= most_w > top_w + kSlack || (top_w == -INFINITY && most_w > top_w);
         }
         if (__any(follow)) {
             const float now = fmaxf(top, most), by = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.f : now));
@@ -286,7 +288,7 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) o[i] *= by_w;
         }
-        const float ref = top == -INFINITY ? 0.f : top, ref_w = top_w == -INFINITY ? 0.f : top_w;
+        const float ref = top == -INFINITY ? 0.f : top - (CODES ? 0.f : kShift), ref_w = top_w == -INFINITY ? 0.f : top_w - kShift;
         w8 w = {}, rest = {};
 #pragma unroll
         for (int h = 0; h < HALVES; ++h)
@@ -327,12 +329,16 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
     }
     sum = of_four(sum, [](float p, float q) { return p + q; });
 
-    // The waves meet in LDS, each in its own part of it.
+    // Results and their sum, both relative to `top`.
     if constexpr (CODES) {
-        const float by = __builtin_amdgcn_exp2f(top_w == -INFINITY ? 0.f : top_w - top);
+        const float by = __builtin_amdgcn_exp2f(top_w == -INFINITY ? 0.f : top_w - kShift - top);
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) o[i] *= by;
+    } else {
+        top -= kShift;
     }
+
+    // The waves meet in LDS, each in its own part of it.
     if (quad == 0) {
         tops[wave][col] = top;
         sums[wave][col] = sum;
