@@ -469,9 +469,7 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
 #pragma unroll
             for (int j = 0; j < BATCH; ++j) {
                 const int p = from + j * groups;
-                const float w = p < parts ? weights[h * kOneMostParts + p] : 0.f;
-                if (w > 0.f) v += w * f32x4{lo[j][0], lo[j][1], hi[j][0], hi[j][1]};
-                else if (w != w) v = f32x4{NAN, NAN, NAN, NAN};
+                if (p < parts) v += weights[h * kOneMostParts + p] * f32x4{lo[j][0], lo[j][1], hi[j][0], hi[j][1]};   // 0 times what is no number is none, as within a part
             }
         }
         if (groups > 1) {

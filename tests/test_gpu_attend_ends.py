@@ -1,0 +1,60 @@
+"""cw_attend_one and cw_attend at the ends of the numbers: values that are none beside weights of 0, exponents from end to end, scales next to 0."""
+import math
+
+import pytest
+import torch
+
+import paper_2006_02464_amd as cw
+from attend_bounds import assert_close, attention
+from attend_refs import BF16, E4M3, F16, F32, HALF_STEP, INF, NAN, Pages, seen_causal
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = cw.Context(workspace_bytes=16 << 20, io_bytes=1 << 20, weight_pool_bytes=16 << 20, load_staging_bytes=1 << 20)
+    yield c
+    c.destroy()
+
+
+@pytest.fixture(scope="module")
+def space(ctx):
+    return torch.zeros(ctx.attend_one_workspace_bytes(), dtype=torch.uint8, device="cuda")
+
+
+def stream():
+    return torch.cuda.current_stream()
+
+
+def one(ctx, pool, q, scale, workspace):
+    handle, gpu = pool.cuda(ctx)
+    y, lse = torch.zeros(q.shape, dtype=q.dtype, device="cuda"), torch.zeros(q.shape[:2], device="cuda")
+    ctx.attend_one(q.cuda(), handle, pool.table.cuda(), torch.tensor(pool.lengths, dtype=torch.int32).cuda(), y, scale, lse=lse, workspace=workspace, stream=stream())
+    return y.cpu(), lse.cpu()
+
+
+@pytest.mark.parametrize("kept", [F16, BF16, E4M3])
+@pytest.mark.parametrize("value", [NAN, INF])
+@pytest.mark.parametrize("lengths", [[3000], [3000, 2500], [3000] + [40] * 70])
+def test_values_that_are_none_beside_weights_of_0(ctx, space, kept, value, lengths):
+    """A seen value that is no number makes its number of the result NaN however far its weight is below the largest (2^-200 here), whether parts of the sequence meet or one workgroup has it all."""
+    x = F16 if kept == E4M3 else kept
+    pool = Pages(lengths, 2, 16, 64, kept, seed=2).fill(5, loud=False)
+    page, at = int(pool.table[0, 2990 // 16]), 2990 % 16
+    k = torch.zeros(1, 2, 64, dtype=x)
+    k[..., 0] = 200.0
+    rest = Pages([1], 2, 16, 64, kept, spare=0)
+    rest.write(0, k, k, 1)
+    pool.k[page, :, at] = rest.k[0, :, 0]
+    if kept == E4M3:
+        pool.k_exp[page, :, at] = rest.k_exp[0, :, 0]
+    pool.v[int(pool.table[0, 0]), 1, 5, 7] = value if kept != E4M3 else 0x7f
+    q = torch.zeros(len(lengths), 4, 64, dtype=x)
+    q[..., 0] = 1.0
+    for workspace in (space, None):
+        y, lse = one(ctx, pool, q, 1.0, workspace)
+        want = torch.zeros(y.shape, dtype=torch.bool)
+        want[0, 2:, 7] = True
+        assert torch.equal(y.isnan(), want), workspace is not None
+        assert bool(y[~want].isfinite().all()) and bool(lse.isfinite().all())
