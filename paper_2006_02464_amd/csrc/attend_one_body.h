@@ -331,9 +331,10 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
 
     // Results and their sum, both relative to `top`.
     if constexpr (CODES) {
-        const float by = __builtin_amdgcn_exp2f(top_w == -INFINITY ? 0.f : top_w - kShift - top);
+        // In two steps: the power may lie beyond fp32's where the result does not, and the instruction gives 0 below 2^-126.
+        const float by = __builtin_amdgcn_exp2f(top_w == -INFINITY ? 0.f : (top_w - kShift - top) * 0.5f);
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i) o[i] *= by;
+        for (int i = 0; i < DP / 16; ++i) o[i] = o[i] * by * by;
     } else {
         top -= kShift;
     }

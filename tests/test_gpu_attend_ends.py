@@ -58,3 +58,26 @@ def test_values_that_are_none_beside_weights_of_0(ctx, space, kept, value, lengt
         want[0, 2:, 7] = True
         assert torch.equal(y.isnan(), want), workspace is not None
         assert bool(y[~want].isfinite().all()) and bool(lse.isfinite().all())
+
+
+@pytest.mark.parametrize("x", [F16, BF16])
+@pytest.mark.parametrize("e_k, e_v", [(127, 0), (127, 3), (120, 60), (127, 127), (127, 200), (110, 230), (0, 127), (140, 225)])
+@pytest.mark.parametrize("lengths", [[40, 1, 3], [2500, 300]])
+def test_exponents_from_end_to_end(ctx, space, x, e_k, e_v, lengths):
+    """Codes times 2^-127 up to 2^103, of keys as far as their scores are numbers.  Results of fp16 end in 0 or infinity, those of bf16 are ordinary numbers, or its smallest."""
+    pool = Pages(lengths, 2, 16, 64, E4M3, seed=2).fill(5, loud=False)
+    pool.k_exp[pool.k_exp < 255] = e_k
+    pool.v_exp[pool.v_exp < 255] = e_v
+    q = (torch.randn(len(lengths), 4, 64, generator=torch.Generator().manual_seed(3))).to(x)
+    scale = 2.0 ** -8 * 2.0 ** min(100, max(-20, 127 - e_k))      # codes are up to 448
+    refs = []
+    for i, n in enumerate(lengths):
+        k, v, _ = pool.read(i, 0, n)
+        refs.append(attention(q[i:i + 1], k, v, scale, torch.ones(1, n, dtype=torch.bool), 2.0 ** -11, 2.0 ** -36))
+    ry, rl, off_y, off_l = (torch.cat([r[j] for r in refs]) for j in range(4))
+    for workspace in (space, None):
+        y, lse = one(ctx, pool, q, scale, workspace)
+        ends = ry.abs() >= torch.finfo(x).max
+        assert bool((y.isinf() | (y.abs() == torch.finfo(x).max))[ends].all())
+        off = off_y + 2.0 ** -149 * 2                        # fp32's own end, of the result and of a sum
+        assert_close(torch.where(ends, torch.zeros_like(y), y), lse, (torch.where(ends, 0.0, ry), rl, off, off_l), workspace is not None)
