@@ -405,7 +405,7 @@ typedef struct {
     int32_t table_pages;
     int32_t window;             /* 0: all tokens */
     int32_t dtype;              /* CW_DTYPE_FP16 or BF16; that of the cache unless it is E4M3 */
-    float scale;                /* finite */
+    float scale;                /* finite, 2^127 in magnitude at most */
 } cw_attend_one_args;
 int32_t cw_attend_one(cw_ctx *ctx, const cw_attend_one_args *args, void *stream);
 /* Workspace that serves every call (32 MiB). */
@@ -429,7 +429,7 @@ typedef struct {
     int32_t causal;             /* 0 or 1 */
     int32_t window;             /* 0: no bound; else with causal only */
     int32_t dtype;              /* CW_DTYPE_FP16 or BF16 */
-    float scale;                /* finite */
+    float scale;                /* finite, 2^127 in magnitude at most */
 } cw_attend_args;
 int32_t cw_attend(cw_ctx *ctx, const cw_attend_args *args, void *stream);
 

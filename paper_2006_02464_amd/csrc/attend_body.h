@@ -33,7 +33,7 @@ struct AttendKernel {
     FastDiv each, kv_heads;
     int32_t group;     // heads that share a key head
     int32_t tiles;     // workgroups of a key head
-    float c;           // |scale| / ln 2
+    float c;           // |scale| / ln 2, above 0
 };
 
 template <typename T, int DP, int SPLIT>
@@ -354,7 +354,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DP <= 128 ? 2 : 1) void attend_k
 template <typename T, int DP, int SPLIT>
 hipError_t launch_attend_as(const AttendArgs &a, hipStream_t s) {
     const int group = a.heads / a.kv_heads, tiles = (int)((int64_t)a.tokens * group / attend_rows(SPLIT) + a.sequences);
-    const AttendKernel f{a, make_fast_div((uint32_t)group), make_fast_div((uint32_t)a.kv_heads), group, tiles, fminf(fmaxf(fabsf(a.scale) * 1.44269504f, 1e-37f), 3e38f)};
+    const AttendKernel f{a, make_fast_div((uint32_t)group), make_fast_div((uint32_t)a.kv_heads), group, tiles, fmaxf(fabsf(a.scale) * 1.44269504f, 0x1p-149f)};   // not 0: it is multiplied with the -inf of masks, too
     attend_kernel<T, DP, SPLIT><<<dim3((unsigned)tiles * a.kv_heads), dim3(64 * kAttendWaves), 0, s>>>(f);
     return hipGetLastError();
 }

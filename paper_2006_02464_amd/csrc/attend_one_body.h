@@ -561,7 +561,7 @@ inline AttendOneKernel one_kernel(const AttendOneArgs &a, int64_t parts, int few
     f.by_kv_heads = make_fast_div((uint32_t)a.cache.kv_heads);
     f.by_items = make_fast_div((uint32_t)f.items);
     f.by_chunks = make_fast_div((uint32_t)a.cache.head_dim / 4);
-    f.c = fminf(fmaxf(fabsf(a.scale) * 1.44269504f, 1e-37f), 3e38f);
+    f.c = fabsf(a.scale) * 1.44269504f;
     return f;
 }
 

@@ -1583,7 +1583,7 @@ static int32_t attention_checks(cw_ctx *c, int32_t heads, int32_t kv_heads, int3
     if (kv_heads < 1 || heads < 1 || heads % kv_heads != 0) return set_err(c, CW_ERR_INVALID, "heads must be a multiple of kv_heads");
     if (heads > kAttendMostHeads) return set_err(c, CW_ERR_UNSUPPORTED, "too many heads");
     if (window < 0) return set_err(c, CW_ERR_INVALID, "bad window");
-    if (!std::isfinite(scale)) return set_err(c, CW_ERR_INVALID, "scale must be finite");
+    if (!(std::fabs(scale) <= kAttendMostScale)) return set_err(c, CW_ERR_INVALID, "scale must be finite, 2^127 in magnitude at most");
     return CW_OK;
 }
 

@@ -389,6 +389,7 @@ struct AttendArgs {
 };
 constexpr int kAttendMostDim = 256, kCacheMostPage = 4096, kCacheMostTokens = 1 << 30, kAttendMostSequences = 1 << 20, kAttendMostHeads = 1 << 12, kAttendMostTokens = 1 << 24;
 constexpr int64_t kCacheMostRows = INT32_MAX - (1 << 16);   // of a call that writes or reads: the last workgroup's waves count beyond them
+constexpr float kAttendMostScale = 0x1p127f;   // divided by ln 2 it is a number still
 constexpr int64_t kAttendMostStride = 1 << 23;   // of cw_attend's keys and values: 64 rows of them fit a buffer
 
 constexpr int kAnswerMostTop = 64, kAnswerMostClasses = 1 << 24, kAnswerMostRows = 1 << 23;

@@ -226,3 +226,11 @@ def test_rows_that_32_bits_count(ctx, call, tokens, let_through):
     change = dict(tokens=tokens, k_stride=77 * 64, v_stride=77 * 64)
     st, why = refusal(ctx, call, cw.cw_cache_args, ROWS, change, cache)
     assert (st, why) == PLANNING if let_through else st == UNSUPPORTED
+
+
+def test_scales_at_their_end(ctx):
+    """Scores are in units of ln 2: scale / ln 2 is a number of fp32."""
+    for scale, status in ((2.0 ** 127, None), (-2.0 ** 127, None), (1e-45, None), (-0.0, None), (2.0 ** 127 * 1.001, INVALID), (-3.4e38, INVALID)):
+        for call, kind, defaults, cache in (("cw_attend", cw.cw_attend_args, PROMPT, None), ("cw_attend_one", cw.cw_attend_one_args, ONE, {})):
+            st, why = refusal(ctx, call, kind, defaults, dict(scale=scale), cache)
+            assert (st, why) == PLANNING if status is None else st == status and (st, why) != PLANNING, (call, scale)

@@ -81,3 +81,35 @@ def test_exponents_from_end_to_end(ctx, space, x, e_k, e_v, lengths):
         assert bool((y.isinf() | (y.abs() == torch.finfo(x).max))[ends].all())
         off = off_y + 2.0 ** -149 * 2                        # fp32's own end, of the result and of a sum
         assert_close(torch.where(ends, torch.zeros_like(y), y), lse, (torch.where(ends, 0.0, ry), rl, off, off_l), workspace is not None)
+
+
+def far_scores(n, heads, kv_heads, dim, scale):
+    """Queries and keys of bf16 whose product is up to 10^38, which `scale` brings back."""
+    g = torch.Generator().manual_seed(6)
+    q, k, v = torch.randn(n, heads, dim, generator=g), torch.randn(n, kv_heads, dim, generator=g), torch.randn(n, kv_heads, dim, generator=g)
+    q, k = q * 1e-3, k * 1e-3
+    q[..., 0], k[..., 0] = 1e19, 1e19 * (2.0 * torch.rand(n, kv_heads, generator=g) - 1.0)
+    return q.to(BF16), k.to(BF16), v.to(BF16)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-45, 1e-40, -1e-39, 1e-38, -5e-38, 2e-37])
+def test_scales_next_to_0(ctx, space, scale):
+    """Down to fp32's last numbers the scale counts as it is, and 0 as 0: softmaxes over equal scores."""
+    as_given = float(torch.tensor(scale, dtype=torch.float32))
+    for heads, kv_heads in ((2, 1), (84, 84)):               # waves that share rows, and do not
+        n = 500
+        q, k, v = far_scores(n, heads, kv_heads, 64, scale)
+        for causal in (True, False):
+            y, lse = torch.zeros(q.shape, dtype=BF16, device="cuda"), torch.zeros(q.shape[:2], device="cuda")
+            ctx.attend(q.cuda(), k.cuda(), v.cuda(), y, torch.tensor([0, n], dtype=torch.int32).cuda(), scale, causal=causal, lse=lse, stream=stream())
+            assert_close(y.cpu(), lse.cpu(), attention(q, k, v, as_given, seen_causal(n, n, causal), HALF_STEP[BF16], 0.0), (heads, causal))
+    for kept in (BF16, E4M3):
+        lengths = [400, 1000]
+        pool, refs = Pages(lengths, 2, 16, 64, kept, seed=2), []
+        for i, n in enumerate(lengths):
+            q, k, v = far_scores(n, 4, 2, 64, scale)
+            pool.write(i, k, v, n)
+            k, v, _ = pool.read(i, 0, n)
+            refs.append(attention(q[:1], k, v, as_given, torch.ones(1, n, dtype=torch.bool), 2.0 ** -11, 2.0 ** -35))
+        y, lse = one(ctx, pool, torch.stack([q[0], q[0]]), scale, space)
+        assert_close(y, lse, tuple(torch.cat([r[j] for r in refs]) for j in range(4)), kept)
