@@ -379,7 +379,7 @@ class Cache:
         except OverflowError:
             raise CwError(CW_ERR_UNSUPPORTED, "too large") from None
         self.tensors = (k, v, k_exp, v_exp)
-        self.kv_heads, self.head_dim = kv_heads, head_dim
+        self.device, self.kv_heads, self.head_dim = device, kv_heads, head_dim
         self.address = ctypes.addressof(self._struct)
 
 
@@ -603,7 +603,7 @@ class Context:
     # -- a paged cache of keys and values, and attention
     def cache(self, k, v, k_exp=None, v_exp=None):
         """Names pages: k, v [pages][kv_heads][page][head_dim] in fp16, bf16 or float8_e4m3fn, the last with exponents [pages][kv_heads][page] (uint8).  Kept
-        as long as the pages are; what the library refuses of them the calls that take it tell."""
+        as long as the pages are, for contexts of their GPU; what the library refuses of them the calls that take it tell."""
         return Cache(self._device, k, v, k_exp, v_exp)
 
     def _cache_rows(self, call, cache, k, v, table, lengths, first, stream):
@@ -611,6 +611,8 @@ class Context:
         if len(shape) != 3 or shape[1] != heads or shape[2] != cache.head_dim:
             raise ValueError("k is %s, not (tokens, %d, %d)" % (tuple(shape), heads, cache.head_dim))
         dtype, on, tokens = k.dtype, self._device, shape[0]
+        if cache.device != on:
+            raise ValueError("the cache is not on the context's GPU")
         if dtype is not v.dtype:
             raise TypeError("k and v are of different types")
         kp, ks, kh = _heads(k, "k", on, tokens, heads)
@@ -638,6 +640,8 @@ class Context:
         """y[sequences][heads][head_dim] = attention of q, a token of each sequence, over the lengths[s] tokens (the last `window`) in the pages table[s] of
         `cache`; lse [sequences][heads] fp32 is written if there is one.  workspace: uint8, zeros before its first call."""
         on, dtype, shape = self._device, q.dtype, q.shape
+        if cache.device != on:
+            raise ValueError("the cache is not on the context's GPU")
         tp, ts, sequences, pages = _table(table, on)
         if len(shape) != 3 or shape[0] != sequences or shape[2] != cache.head_dim:
             raise ValueError("q is %s, not (%d, heads, %d)" % (tuple(shape), sequences, cache.head_dim))

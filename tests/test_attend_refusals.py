@@ -234,3 +234,24 @@ def test_scales_at_their_end(ctx):
         for call, kind, defaults, cache in (("cw_attend", cw.cw_attend_args, PROMPT, None), ("cw_attend_one", cw.cw_attend_one_args, ONE, {})):
             st, why = refusal(ctx, call, kind, defaults, dict(scale=scale), cache)
             assert (st, why) == PLANNING if status is None else st == status and (st, why) != PLANNING, (call, scale)
+
+
+class OnGpu1(torch.Tensor):
+    """A tensor that says it is on GPU 1."""
+
+    def get_device(self):
+        return 1
+
+
+def test_binding_refuses_caches_of_another_gpu(ctx):
+    """Pages are named by their addresses: those of another GPU than the context's must not reach it."""
+    half = torch.float16
+    pages = torch.zeros(10, 2, 16, 64, dtype=half).as_subclass(OnGpu1)
+    raises(ValueError, ctx.cache, pages, pages)
+    cache = cw.Cache(1, pages, pages, None, None)            # of a context of GPU 1
+    assert cache.device == 1 and ctx.cache(torch.zeros(1, 2, 16, 64, dtype=half), torch.zeros(1, 2, 16, 64, dtype=half)).device == -1
+    i = lambda *n: torch.zeros(*n, dtype=torch.int32)
+    x, q = torch.zeros(3, 2, 64, dtype=half), torch.zeros(3, 4, 64, dtype=half)
+    for call in (lambda: ctx.cache_write(x, x.clone(), cache, i(3, 5), i(3)), lambda: ctx.cache_read(cache, i(3, 5), i(3), x, x.clone()),
+                 lambda: ctx.attend_one(q, cache, i(3, 5), i(3), q.clone(), 0.1)):
+        assert "the cache is not on the context's GPU" in str(raises(ValueError, call))
