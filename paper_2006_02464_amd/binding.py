@@ -346,27 +346,32 @@ def _on(stream):
     return 0 if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def _strides(t):
+    """Of the dimensions, 0 of those of one element: torch leaves these open."""
+    return tuple(step if n > 1 else 0 for n, step in zip(t.shape, t.stride()))
+
+
 class Cache:
     """Pages of keys and values as the calls over them take them: made by Context.cache, holds the tensors that it names."""
 
     def __init__(self, device, k, v, k_exp, v_exp):
         if k.dim() != 4:
             raise ValueError("k is %s, not (pages, kv_heads, page, head_dim)" % (tuple(k.shape),))
-        if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+        strides = _strides(k)
+        if v.shape != k.shape or _strides(v) != strides or v.dtype != k.dtype:
             raise ValueError("k and v are laid out differently")
         pages, kv_heads, page, head_dim = k.shape
-        strides = k.stride()
         if strides[3] != 1 and head_dim > 1:
             raise ValueError("numbers of a head must be contiguous")
         if (k_exp is None) != (v_exp is None):
             raise ValueError("exponents of both keys and values, or of neither")
         exps = (0, 0, 0)
         if k_exp is not None:
-            if k_exp.shape != k.shape[:3] or v_exp.shape != k.shape[:3] or k_exp.stride() != v_exp.stride():
+            if k_exp.shape != k.shape[:3] or v_exp.shape != k.shape[:3] or _strides(k_exp) != _strides(v_exp):
                 raise ValueError("k_exp and v_exp must be %s and laid out alike" % (tuple(k.shape[:3]),))
             if str(k_exp.dtype) != "torch.uint8" or str(v_exp.dtype) != "torch.uint8":
                 raise TypeError("exponents are bytes")
-            exps = k_exp.stride()
+            exps = _strides(k_exp)
         for t in (k, v, k_exp, v_exp):
             if t is not None and t.get_device() != device:
                 raise ValueError("the cache is not on the context's GPU")

@@ -255,3 +255,24 @@ def test_binding_refuses_caches_of_another_gpu(ctx):
     for call in (lambda: ctx.cache_write(x, x.clone(), cache, i(3, 5), i(3)), lambda: ctx.cache_read(cache, i(3, 5), i(3), x, x.clone()),
                  lambda: ctx.attend_one(q, cache, i(3, 5), i(3), q.clone(), 0.1)):
         assert "the cache is not on the context's GPU" in str(raises(ValueError, call))
+
+
+def test_binding_takes_pages_that_are_laid_out_alike(ctx):
+    """Strides of dimensions of one element, which torch leaves open, say nothing of the layout."""
+    half, code, byte = torch.float16, torch.float8_e4m3fn, torch.uint8
+    view = lambda shape, strides, dtype: torch.zeros(1 << 16, dtype=byte).view(dtype).as_strided(shape, strides)
+    q, i = torch.zeros(3, 4, 64, dtype=half), lambda *n: torch.zeros(*n, dtype=torch.int32)
+
+    def taken(*pages):
+        cache = ctx.cache(*pages)
+        planning(ctx.attend_one, q, cache, i(3, 5), i(3), q.clone(), 0.1)
+        x = torch.zeros(3, cache.kv_heads, 64, dtype=half)
+        planning(ctx.cache_write, x, x.clone(), cache, i(3, 5), i(3))
+    taken(view((1, 2, 16, 64), (2048, 1024, 64, 1), half), view((1, 2, 16, 64), (1, 1024, 64, 1), half))          # one page
+    taken(view((2, 1, 16, 64), (1024, 1024, 64, 1), half), view((2, 1, 16, 64), (1024, 7, 64, 1), half))          # one key head
+    taken(view((2, 2, 1, 64), (128, 64, 64, 1), half), view((2, 2, 1, 64), (128, 64, 3, 1), half))                # one token a page
+    taken(*(view((1, 2, 16, 64), s, code) for s in ((2048, 1024, 64, 1), (5, 1024, 64, 1))), *(view((1, 2, 16), s, byte) for s in ((32, 16, 1), (3, 16, 1))))
+    taken(*(view((2, 1, 16, 64), (1024, 1024, 64, 1), code) for _ in range(2)), *(view((2, 1, 16), s, byte) for s in ((16, 16, 1), (16, 9, 1))))
+    for shape, a, b in (((2, 1, 16, 64), (1024, 0, 64, 1), (2048, 0, 64, 1)), ((1, 2, 16, 64), (0, 1024, 64, 1), (0, 2048, 64, 1)), ((1, 1, 16, 64), (0, 0, 64, 1), (0, 0, 128, 1))):
+        raises(ValueError, ctx.cache, view(shape, a, half), view(shape, b, half))
+    raises(ValueError, ctx.cache, *(view((2, 1, 16, 64), (1024, 0, 64, 1), code) for _ in range(2)), *(view((2, 1, 16), s, byte) for s in ((16, 0, 1), (32, 0, 1))))
