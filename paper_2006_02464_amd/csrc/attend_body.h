@@ -20,8 +20,6 @@ namespace cw {
 // what comes before and behind the tiles: 16 prompts of 33 to 2048 tokens, bf16, in 250 to 262 us, 740 to 780 TFLOP/s.  A third tile under way in LDS is no faster (9 prompts of 1737 to 2121, 40 heads over 5 of 80 352 us and 353, one of 2468 and one head 33 and 42), nor are
 // three waves a SIMD, whose registers spill (44 and 78 us for 60 prompts of 99 to 167, 32 heads over 8 of 80).
 // Where the rows do not fill the GPU, SPLIT waves share 32 of them and take parts of each tile: their results meet in LDS at the end.
-constexpr int kAttendWaves = 4;
-constexpr int attend_rows(int split) { return 32 * kAttendWaves / split; }   // of a workgroup
 constexpr int kAttendKeys = 64;   // of a tile: two of them and their successors fit a CU's LDS up to 128 numbers a head
 template <typename T>
 struct AttendWeights {   // in units of ln 2
@@ -361,16 +359,14 @@ hipError_t launch_attend_as(const AttendArgs &a, hipStream_t s) {
 
 template <typename T, int DP>
 hipError_t launch_attend_dim(const AttendArgs &a, hipStream_t s) {
-    // Waves share rows where there are few workgroups of 128: 500 queries of 32 heads over 8 of 128 bf16 (133 workgroups) 15.0 -> 11.8 us, eight prompts of 290 to 680 behind 215 keys, 8 heads (306)
+    // Waves share rows where there are few workgroups of 128 rows: 500 queries of 32 heads over 8 of 128 bf16 (133 workgroups) 15.0 -> 11.8 us, eight prompts of 290 to 680 behind 215 keys, 8 heads (306)
     // 33.2 -> 27.2; but four of 301 to 1024 behind 2500, 16 heads over 4 of 96 (347) 58 -> 65, 39 of 80 to 149, 8 heads over 4 (434) 13.5 -> 16.4.
-    const int64_t workgroups = (int64_t)a.tokens * a.heads / attend_rows(1) + (int64_t)a.sequences * a.kv_heads;
-    return workgroups <= 320 ? launch_attend_as<T, DP, 2>(a, s) : launch_attend_as<T, DP, 1>(a, s);
+    return attend_workgroups(a) <= 320 ? launch_attend_as<T, DP, 2>(a, s) : launch_attend_as<T, DP, 1>(a, s);
 }
 
 template <typename T>
 hipError_t launch_attend_typed(const AttendArgs &a, hipStream_t s) {
-    if (a.head_dim % 16 != 0 || a.head_dim > kAttendMostDim || (int64_t)a.tokens * a.heads + (int64_t)a.sequences * a.kv_heads > INT32_MAX)
-        return hipErrorInvalidValue;
+    if (a.head_dim % 16 != 0 || a.head_dim > kAttendMostDim || !attend_fits(a)) return hipErrorInvalidValue;
     if (a.head_dim <= 64) return launch_attend_dim<T, 64>(a, s);
     if (a.head_dim <= 96) return launch_attend_dim<T, 96>(a, s);
     if (a.head_dim <= 128) return launch_attend_dim<T, 128>(a, s);

@@ -17,8 +17,6 @@ namespace cw {
 // fp16 ends early, so its weights refer to 2^11 below the maximum: what the type cannot hold of a weight is at most 2^-36 of the largest.
 // 64 sequences of 133 to 8192 tokens, 32 heads over 8 of 128 bf16, take 199 to 204 us, 5.4 TB/s; 200 of up to 4096, 64 heads over 8 in e4m3, 164 to 174; one of 32001 31, 4.2 TB/s, of which about 12 go to the launch, the first
 // bytes and the meeting.  Where the loads are all there is, more of them under way (four steps, smaller ones) gave nothing.
-constexpr int one_tokens(int row_bytes) { return row_bytes > 256 ? 16 : 32; }   // of a step: 16 KB at most
-constexpr int kOneHeads = 16;
 constexpr int kOneMostParts = 64;   // a lane each where they meet
 constexpr int kOneCounters = 65536 / 4;
 
@@ -575,25 +573,21 @@ template <typename T, bool CODES, int RB, int WAVES>
 hipError_t launch_attend_one_as(const AttendOneArgs &a, int64_t items, int64_t steps, int64_t parts, int fewest, int from, bool parts_outer, hipStream_t s) {
     parts = steps < from ? 1 : std::min({parts, (int64_t)kOneMostParts, steps / fewest, one_records(a, items) / items});
     const AttendOneKernel f = one_kernel(a, parts, fewest, from, parts_outer);
-    if (items * f.parts > INT32_MAX) return hipErrorInvalidValue;
+    if (items * f.parts * 64 * WAVES > kMostThreads) return hipErrorInvalidValue;
     attend_one_kernel<T, CODES, RB, WAVES, false><<<dim3((unsigned)(items * f.parts)), 64 * WAVES, 0, s>>>(f);
     return hipGetLastError();
 }
 
 template <typename T, bool CODES, int RB>
-hipError_t launch_attend_one_row(const AttendOneArgs &a, hipStream_t s) {
-    constexpr int TOKENS = one_tokens(RB), WAVES = 4;
-    const int64_t items = (int64_t)a.sequences * ((a.heads / a.cache.kv_heads + kOneHeads - 1) / kOneHeads) * a.cache.kv_heads;
-    int64_t tokens = (int64_t)a.table_pages << a.cache.page_shift;
-    if (a.window > 0) tokens = std::min<int64_t>(tokens, (int64_t)a.window + TOKENS - 1);
-    const int64_t steps = (tokens + TOKENS - 1) / TOKENS;
-    // `slots` workgroups of four waves run at once, as LDS has it.  Up to as many items: parts fill them, of 256 tokens at least (4 sequences of 810 to 1999, 4 heads of 80 bf16 11.4 us, of 512 tokens 15.0; but
+hipError_t launch_attend_one_row(const AttendOneArgs &a, const OneForm &form, hipStream_t s) {
+    constexpr int TOKENS = one_tokens(RB), WAVES = kOneWaves;
+    const int64_t items = form.items, steps = form.steps, slots = form.slots;
+    // Up to as many items as workgroups run at once: parts fill them, of 256 tokens at least (4 sequences of 810 to 1999, 4 heads of 80 bf16 11.4 us, of 512 tokens 15.0; but
     // 2 of 1486 and 5604, 64 heads over 4 in e4m3, 17.3 and 16.8), of sequences from 704 on (one of 600, 32 heads over 8 of 128 fp16, 8.3 us whole, 9.6 in two; one of 1000 11.6 whole, 8.4 in three), an item's behind one another: neighbours go to different XCDs (9 of 100 to 9000, 16 heads of 64 40.5 us, with all items' parts p behind one another 45.2).
-    constexpr int64_t slots = 2 * WAVES * (2 * TOKENS * RB + 256) > 80 * 1024 ? 256 : 512;
     // Parts of the same steps whatever the lengths, no more than run at once, an item's neighbours those of the other heads: 6 of 9661 to 38277, 64 heads over 8 of 256 bf16, 218 us, as many parts of every sequence 240;
     // 5 of 100 to 20000, 32 heads over 8 of 128 42.7 and 50.5, 12 of 30 to 5000 29.7 and 36.2; 14 of 3726 to 4520, 80 over 5 of 256, 73.5 and 71.3. Where a record is large a part is too: 7 of 2441 to 6183, 32 heads over 2 of 128,
     // 23.8 us with parts of 256 tokens, 18.9 of 512.
-    if (items <= slots && a.sequences > 1 && a.sequences <= 64 && tokens >= 704) {
+    if (items <= slots && a.sequences > 1 && a.sequences <= 64 && form.tokens >= 704) {
         const int64_t grid = std::max(items, std::min(slots, one_records(a, items)));
         AttendOneKernel f = one_kernel(a, 1, (std::min(a.heads / a.cache.kv_heads, kOneHeads) * a.cache.head_dim > 1024 ? 512 : 256) / TOKENS, 704 / TOKENS, false);
         f.most = (int)(grid / f.items);
@@ -601,25 +595,24 @@ hipError_t launch_attend_one_row(const AttendOneArgs &a, hipStream_t s) {
         return hipGetLastError();
     }
     if (items <= slots) return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, slots / items, 256 / TOKENS, 704 / TOKENS, false, s);
-    // More, of few tokens, get a wave each: 200 of 30 to 150, 8 heads of 128 18.5 us for 28.8, 150 of 30 to 300 29.5 for 34.1, 40 of 3 to 30 5.0 for 8.2; but 34 of 30 to 300 (272 items) 14.1 for 10.0, 60 of 30 to 400 17.6 for 14.8.
-    if (tokens <= 128 || (tokens <= 320 && items > 2 * slots)) return launch_attend_one_as<T, CODES, RB, 1>(a, items, steps, 1, 1, 0, true, s);
-    // Else what a workgroup spends before its tokens, behind them and on meeting others is made up for by long parts only: 200 of up to 4096 in e4m3, 8 heads, 175 us, in parts of 256 tokens 187; 36 of up to 16000 219, whole
+    if (form.wave_each) return launch_attend_one_as<T, CODES, RB, 1>(a, items, steps, 1, 1, 0, true, s);
+    // Of more items, what a workgroup spends before its tokens, behind them and on meeting others is made up for by long parts only: 200 of up to 4096 in e4m3, 8 heads, 175 us, in parts of 256 tokens 187; 36 of up to 16000 219, whole
     // 239.  All items' first parts come first: of two parts behind one another the second is empty for all but the longest, which leaves every other XCD without work (64 of up to 8192 284 us for 228).
     return launch_attend_one_as<T, CODES, RB, WAVES>(a, items, steps, (4 * slots + items - 1) / items, 2048 / TOKENS, 0, true, s);
 }
 
 template <typename T, bool CODES>
 hipError_t launch_attend_one_typed(const AttendOneArgs &a, hipStream_t s) {
-    const int bytes = a.cache.head_dim * (CODES ? 1 : 2);
+    const OneForm form = one_form(a);
     if (a.cache.head_dim % 16 != 0 || a.cache.head_dim > kAttendMostDim) return hipErrorInvalidValue;
     if constexpr (CODES) {
-        if (bytes <= 64) return launch_attend_one_row<T, CODES, 64>(a, s);
-        if (bytes <= 128) return launch_attend_one_row<T, CODES, 128>(a, s);
-        return launch_attend_one_row<T, CODES, 256>(a, s);
+        if (form.row_bytes == 64) return launch_attend_one_row<T, CODES, 64>(a, form, s);
+        if (form.row_bytes == 128) return launch_attend_one_row<T, CODES, 128>(a, form, s);
+        return launch_attend_one_row<T, CODES, 256>(a, form, s);
     } else {
-        if (bytes <= 128) return launch_attend_one_row<T, CODES, 128>(a, s);
-        if (bytes <= 256) return launch_attend_one_row<T, CODES, 256>(a, s);
-        return launch_attend_one_row<T, CODES, 512>(a, s);
+        if (form.row_bytes == 128) return launch_attend_one_row<T, CODES, 128>(a, form, s);
+        if (form.row_bytes == 256) return launch_attend_one_row<T, CODES, 256>(a, form, s);
+        return launch_attend_one_row<T, CODES, 512>(a, form, s);
     }
 }
 

@@ -1553,7 +1553,10 @@ static int32_t cache_rows(cw_ctx *c, const cw_cache_args *r, void *stream, bool 
     if (r->tokens < 0) return set_err(c, CW_ERR_INVALID, "bad size");
     rc = sequence_checks(c, r->sequences, r->table_pages, r->table_stride, r->table, r->lengths, r->cache->page);
     if (rc != CW_OK) return rc;
-    if (r->tokens > kAttendMostTokens || (int64_t)r->tokens * 2 * a.cache.kv_heads > kCacheMostRows) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
+    a.k = r->k; a.v = r->v; a.first = r->first; a.lengths = r->lengths; a.table = r->table;
+    a.k_stride = r->k_stride; a.k_head_stride = r->k_head_stride; a.v_stride = r->v_stride; a.v_head_stride = r->v_head_stride; a.table_stride = r->table_stride;
+    a.tokens = r->tokens; a.sequences = r->sequences; a.table_pages = r->table_pages; a.dtype = (DType)r->dtype;
+    if (r->tokens > kAttendMostTokens || !cache_fits(a)) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
     if (!r->first && r->tokens != r->sequences) return set_err(c, CW_ERR_INVALID, "without `first` there is a row for every sequence");
     if (!aligned_to(r->first, DT_F32)) return set_err(c, CW_ERR_INVALID, "misaligned pointer");
     if (r->tokens > 0 && r->sequences > 0) {
@@ -1564,9 +1567,6 @@ static int32_t cache_rows(cw_ctx *c, const cw_cache_args *r, void *stream, bool 
     }
     if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
     if (r->tokens == 0 || r->sequences == 0) return CW_OK;
-    a.k = r->k; a.v = r->v; a.first = r->first; a.lengths = r->lengths; a.table = r->table;
-    a.k_stride = r->k_stride; a.k_head_stride = r->k_head_stride; a.v_stride = r->v_stride; a.v_head_stride = r->v_head_stride; a.table_stride = r->table_stride;
-    a.tokens = r->tokens; a.sequences = r->sequences; a.table_pages = r->table_pages; a.dtype = (DType)r->dtype;
     DeviceGuard g(c->device);
     if (!g.ok) return hip_fail(c, hipGetLastError(), "hipSetDevice");
     if (write) CW_HIP(c, launch_cache_write(a, static_cast<hipStream_t>(stream)));
@@ -1604,12 +1604,13 @@ int32_t cw_attend_one(cw_ctx *c, const cw_attend_one_args *r, void *stream) {
         if (why) return set_err(c, CW_ERR_INVALID, why);
         if (!aligned_to(r->lse, DT_F32) || reinterpret_cast<uintptr_t>(r->workspace) % 16 != 0) return set_err(c, CW_ERR_INVALID, "misaligned pointer");
     }
-    if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
-    if (r->sequences == 0) return CW_OK;
     a.q = r->q; a.y = r->y; a.lse = r->lse; a.lengths = r->lengths; a.table = r->table;
     a.workspace = r->workspace; a.workspace_bytes = r->workspace ? r->workspace_bytes : 0;
     a.q_stride = r->q_stride; a.q_head_stride = r->q_head_stride; a.y_stride = r->y_stride; a.y_head_stride = r->y_head_stride; a.table_stride = r->table_stride;
     a.sequences = r->sequences; a.heads = r->heads; a.table_pages = r->table_pages; a.window = r->window; a.dtype = (DType)r->dtype; a.scale = r->scale;
+    if (!attend_one_fits(a)) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
+    if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
+    if (r->sequences == 0) return CW_OK;
     DeviceGuard g(c->device);
     if (!g.ok) return hip_fail(c, hipGetLastError(), "hipSetDevice");
     CW_HIP(c, launch_attend_one(a, static_cast<hipStream_t>(stream)));
@@ -1635,12 +1636,11 @@ int32_t cw_attend(cw_ctx *c, const cw_attend_args *r, void *stream) {
         if (!why && (!aligned_to(r->lse, DT_F32) || !aligned_to(r->first, DT_F32) || !aligned_to(r->first_k, DT_F32))) why = "misaligned pointer";
         if (why) return set_err(c, CW_ERR_INVALID, why);
     }
-    if ((r->keys > 1 && (r->k_stride > kAttendMostStride || r->v_stride > kAttendMostStride)) || (int64_t)r->tokens * r->heads + (int64_t)r->sequences * r->kv_heads > INT32_MAX)
-        return set_err(c, CW_ERR_UNSUPPORTED, "too large");
-    if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
-    if (r->tokens == 0 || r->sequences == 0) return CW_OK;
     AttendArgs a{r->q, r->k, r->v, r->y, r->lse, r->first, r->first_k ? r->first_k : r->first, r->q_stride, r->q_head_stride, r->k_stride, r->k_head_stride, r->v_stride, r->v_head_stride,
                  r->y_stride, r->y_head_stride, r->tokens, r->keys, r->sequences, r->heads, r->kv_heads, r->head_dim, r->causal, r->window < r->keys ? r->window : 0, (DType)r->dtype, r->scale};   // no sequence has more keys
+    if ((r->keys > 1 && (r->k_stride > kAttendMostStride || r->v_stride > kAttendMostStride)) || !attend_fits(a)) return set_err(c, CW_ERR_UNSUPPORTED, "too large");
+    if (c->device < 0) return set_err(c, CW_ERR_INVALID, "planning-only context has no device");
+    if (r->tokens == 0 || r->sequences == 0) return CW_OK;
     DeviceGuard g(c->device);
     if (!g.ok) return hip_fail(c, hipGetLastError(), "hipSetDevice");
     CW_HIP(c, launch_attend(a, static_cast<hipStream_t>(stream)));

@@ -557,6 +557,10 @@ hipError_t launch_fc4(const Fc4Args &a, hipStream_t s);
 void fc4_grid(const Fc4Args &a, dim3 *grid, int *block);   // of that launch
 hipError_t launch_answer(const AnswerArgs &a, hipStream_t s);
 size_t answer_workspace_bytes();
+constexpr int64_t kMostThreads = UINT32_MAX;   // of a launch
+bool cache_fits(const CacheArgs &a);           // a launch, for arguments that are checked otherwise; attend_fits and attend_one_fits as well
+bool attend_one_fits(const AttendOneArgs &a);
+bool attend_fits(const AttendArgs &a);
 hipError_t launch_cache_write(const CacheArgs &a, hipStream_t s);
 hipError_t launch_cache_read(const CacheArgs &a, hipStream_t s);
 hipError_t launch_attend_one(const AttendOneArgs &a, hipStream_t s);

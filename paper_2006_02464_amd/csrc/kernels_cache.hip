@@ -218,8 +218,8 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_kernel(const CacheKern
     }
 }
 
-template <typename T, bool WRITE>
-static hipError_t launch_cache_as(const CacheArgs &a, hipStream_t s) {
+// The kernel's arguments, and its workgroups.
+static CacheKernel cache_form(const CacheArgs &a, int64_t *workgroups) {
     CacheKernel f{a, make_fast_div((uint32_t)(2 * a.cache.kv_heads)), 2, 1, 1};
     while (f.lanes * 8 < a.cache.head_dim) {
         f.lanes *= 2;
@@ -230,7 +230,21 @@ static hipError_t launch_cache_as(const CacheArgs &a, hipStream_t s) {
     const int64_t each = 64 / f.lanes, rows = (int64_t)a.tokens * 2 * a.cache.kv_heads, all = (rows + each - 1) / each;
     f.passes = (int)std::max<int64_t>(1, std::min({all / 2048, (int64_t)kCacheBatch, 62 * 2 * a.cache.kv_heads / each}));
     const int64_t waves = (all + f.passes - 1) / f.passes;
-    const dim3 grid((unsigned)((waves + kCacheWaves - 1) / kCacheWaves));
+    *workgroups = (waves + kCacheWaves - 1) / kCacheWaves;
+    return f;
+}
+
+bool cache_fits(const CacheArgs &a) {
+    int64_t workgroups;
+    cache_form(a, &workgroups);
+    return (int64_t)a.tokens * 2 * a.cache.kv_heads <= kCacheMostRows && workgroups * 64 * kCacheWaves <= kMostThreads;
+}
+
+template <typename T, bool WRITE>
+static hipError_t launch_cache_as(const CacheArgs &a, hipStream_t s) {
+    int64_t workgroups;
+    const CacheKernel f = cache_form(a, &workgroups);
+    const dim3 grid((unsigned)workgroups);
     if (a.cache.dtype == DT_E4M3) cache_kernel<T, unsigned char, WRITE><<<grid, 64 * kCacheWaves, 0, s>>>(f);
     else if (a.cache.dtype == DT_F16) cache_kernel<T, f16, WRITE><<<grid, 64 * kCacheWaves, 0, s>>>(f);
     else cache_kernel<T, bf16, WRITE><<<grid, 64 * kCacheWaves, 0, s>>>(f);
@@ -239,7 +253,7 @@ static hipError_t launch_cache_as(const CacheArgs &a, hipStream_t s) {
 
 template <bool WRITE>
 static hipError_t launch_cache(const CacheArgs &a, hipStream_t s) {
-    if (a.tokens < 1 || a.sequences < 1 || a.cache.head_dim % 16 != 0 || a.cache.head_dim > kAttendMostDim || (int64_t)a.tokens * 2 * a.cache.kv_heads > kCacheMostRows) return hipErrorInvalidValue;
+    if (a.tokens < 1 || a.sequences < 1 || a.cache.head_dim % 16 != 0 || a.cache.head_dim > kAttendMostDim || !cache_fits(a)) return hipErrorInvalidValue;
     if (a.dtype == DT_F32) return launch_cache_as<float, WRITE>(a, s);
     return a.dtype == DT_F16 ? launch_cache_as<f16, WRITE>(a, s) : launch_cache_as<bf16, WRITE>(a, s);
 }

@@ -276,3 +276,28 @@ def test_binding_takes_pages_that_are_laid_out_alike(ctx):
     for shape, a, b in (((2, 1, 16, 64), (1024, 0, 64, 1), (2048, 0, 64, 1)), ((1, 2, 16, 64), (0, 1024, 64, 1), (0, 2048, 64, 1)), ((1, 1, 16, 64), (0, 0, 64, 1), (0, 0, 128, 1))):
         raises(ValueError, ctx.cache, view(shape, a, half), view(shape, b, half))
     raises(ValueError, ctx.cache, *(view((2, 1, 16, 64), (1024, 0, 64, 1), code) for _ in range(2)), *(view((2, 1, 16), s, byte) for s in ((16, 0, 1), (32, 0, 1))))
+
+
+def test_launches_of_more_than_32_bits_of_threads(ctx):
+    """A launch's threads are counted in 32 bits: calls of more are "too large" before the GPU is asked."""
+    def both(call, kind, defaults, fits, beyond, cache=None):
+        assert refusal(ctx, call, kind, dict(defaults, **fits), {}, cache) == PLANNING, (call, fits)
+        st, why = refusal(ctx, call, kind, dict(defaults, **beyond), {}, cache)
+        assert (st, why) == (UNSUPPORTED, "too large"), (call, beyond, why)
+    # rows of 256 numbers, two a wave's pass, four passes: 32 a workgroup of 256
+    wide = dict(kv_heads=16, head_dim=256, token_stride=256, head_stride=16 * 256, page_stride=16 * 16 * 256)
+    rows = dict(ROWS, k_stride=4096, k_head_stride=256, v_stride=4096, v_head_stride=256)
+    for call in ("cw_cache_write", "cw_cache_read"):
+        both(call, cw.cw_cache_args, rows, dict(tokens=(1 << 24) - 1), dict(tokens=1 << 24), wide)
+    # a workgroup of 256 for every sequence and key head
+    prompt = dict(PROMPT, heads=16, kv_heads=16, q_stride=1024, y_stride=1024, k_stride=1024, v_stride=1024)
+    both("cw_attend", cw.cw_attend_args, prompt, dict(sequences=(1 << 20) - 1), dict(sequences=1 << 20))
+    both("cw_attend", cw.cw_attend_args, dict(prompt, sequences=1), dict(tokens=(1 << 24) - 200, heads=128, kv_heads=1, y_stride=8192), dict(tokens=1 << 24, heads=128, kv_heads=1, y_stride=8192))
+    one = dict(ONE, heads=16, q_stride=1024, y_stride=1024)
+    many = dict(kv_heads=16, page_stride=16 * 16 * 64)
+    both("cw_attend_one", cw.cw_attend_one_args, dict(one, table_pages=100), dict(sequences=(1 << 20) - 1), dict(sequences=1 << 20), many)
+    # of few tokens one of 64
+    more = dict(kv_heads=64, page_stride=64 * 16 * 64)
+    for few in (dict(table_pages=8), dict(table_pages=20), dict(table_pages=100, window=200)):
+        both("cw_attend_one", cw.cw_attend_one_args, dict(one, heads=64, y_stride=4096, **few), dict(sequences=(1 << 20) - 1), dict(sequences=1 << 20), more)
+        assert refusal(ctx, "cw_attend_one", cw.cw_attend_one_args, dict(one, sequences=1 << 20, **few), {}, many) == PLANNING
