@@ -408,7 +408,7 @@ typedef struct {
     float scale;                /* finite, 2^127 in magnitude at most */
 } cw_attend_one_args;
 int32_t cw_attend_one(cw_ctx *ctx, const cw_attend_one_args *args, void *stream);
-/* Workspace that serves every call (32 MiB). */
+/* Workspace that serves every call (32 MiB): more changes nothing. */
 size_t cw_attend_one_workspace_bytes(void);
 
 /* Attention of whole prompts, or of parts of them behind their histories, packed one behind the other: queries first[s]..first[s + 1] - 1 see keys

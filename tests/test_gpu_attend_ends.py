@@ -113,3 +113,23 @@ def test_scales_next_to_0(ctx, space, scale):
             refs.append(attention(q[:1], k, v, as_given, torch.ones(1, n, dtype=torch.bool), 2.0 ** -11, 2.0 ** -35))
         y, lse = one(ctx, pool, torch.stack([q[0], q[0]]), scale, space)
         assert_close(y, lse, tuple(torch.cat([r[j] for r in refs]) for j in range(4)), kept)
+
+
+@pytest.mark.parametrize("sequences", [252, 254, 255])
+def test_the_workspace_that_serves_every_call(ctx, sequences):
+    """More than attend_one_workspace_bytes() changes nothing: not a bit of the results, and what lies behind them stays."""
+    lengths = [i * 13 % 50 for i in range(sequences)]
+    lengths[0], lengths[100], lengths[sequences - 1] = 4096, 4000, 4096
+    pool = Pages(lengths, 8, 64, 128, E4M3, seed=2).fill(5)
+    handle, gpu = pool.cuda(ctx)
+    table, lens = pool.table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda()
+    q = torch.randn(sequences, 128, 128, generator=torch.Generator().manual_seed(3)).half().cuda()
+    most, out = ctx.attend_one_workspace_bytes(), []
+    for size in (most, 3 * most):
+        space = torch.full((size,), 0x5a, dtype=torch.uint8, device="cuda")
+        space[:cw.CW_ATTEND_COUNTERS] = 0
+        y, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+        ctx.attend_one(q, handle, table, lens, y, 0.08, lse=lse, workspace=space, stream=stream())
+        assert bool((space[most:] == 0x5a).all())
+        out.append((y, lse))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
