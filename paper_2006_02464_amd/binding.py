@@ -643,7 +643,8 @@ class Context:
 
     def attend_one(self, q, cache, table, lengths, y, scale, window=0, lse=None, workspace=None, stream=None):
         """y[sequences][heads][head_dim] = attention of q, a token of each sequence, over the lengths[s] tokens (the last `window`) in the pages table[s] of
-        `cache`; lse [sequences][heads] fp32 is written if there is one.  workspace: uint8, zeros before its first call."""
+        `cache`; lse [sequences][heads] fp32 is written if there is one.  workspace: uint8, zeros before its first call.  A table is best as wide as the
+        longest sequence needs: how sequences are shared goes by its width."""
         on, dtype, shape = self._device, q.dtype, q.shape
         if cache.device != on:
             raise ValueError("the cache is not on the context's GPU")

@@ -16,8 +16,9 @@ namespace cw {
 // of each, which leaves the result about a quarter further from the formula than its own rounding does: weights of two parts take half as many matrix instructions again and a third more time (8192 tokens of 32 heads over
 // 8 of 128 fp16 564 us and 757, 16 prompts of 33 to 2048 bf16 267 and 338).  fp16 ends early, so its weights refer to kShift below the maximum: the largest is 2^11 to 2^15, and what the type cannot hold
 // of a weight is at most 2^-36 of the largest, where it would be 2^-25 with the maximum itself.
-// The matrix cores and the card's power bound it: 8192 tokens of 32 heads over 8 of 128 fp16, causal, in 540 to 560 us, 980 to 1020 TFLOP/s at 1.7 GHz, where a library's product of 8192^3 reaches 1093; short prompts
-// what comes before and behind the tiles: 16 prompts of 33 to 2048 tokens, bf16, in 250 to 262 us, 740 to 780 TFLOP/s.  A third tile under way in LDS is no faster (9 prompts of 1737 to 2121, 40 heads over 5 of 80 352 us and 353, one of 2468 and one head 33 and 42), nor are
+// The matrix cores and the card's power bound it: 8192 tokens of 32 heads over 8 of 128 fp16, causal, in 530 to 565 us, 970 to 1040 TFLOP/s at 1.5 to 1.8 GHz, where a library's product of 8192^3 random numbers reaches 1365, with its
+// right operand transposed 1600; short prompts what comes before and behind the tiles: 16 prompts of 33 to 2048 tokens, bf16, in 246 to 265 us, 725 to 780 TFLOP/s.  Heads beyond 192 numbers do not fit a wave's registers where tiles
+// have masks: 132 bytes a lane lie in scratch, 76 where waves share rows, and nine prompts of three tokens, 16 heads of 256, take 11 us, of 64 numbers 4.7.  A third tile under way in LDS is no faster (9 prompts of 1737 to 2121, 40 heads over 5 of 80 352 us and 353, one of 2468 and one head 33 and 42), nor are
 // three waves a SIMD, whose registers spill (44 and 78 us for 60 prompts of 99 to 167, 32 heads over 8 of 80).
 // Where the rows do not fill the GPU, SPLIT waves share 32 of them and take parts of each tile: their results meet in LDS at the end.
 constexpr int kAttendKeys = 64;   // of a tile: two of them and their successors fit a CU's LDS up to 128 numbers a head

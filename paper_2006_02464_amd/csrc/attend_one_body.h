@@ -15,8 +15,8 @@ namespace cw {
 // weights refer to a maximum of their own, which follows where one is 2^kSlack times above it.  bf16 weights go into the second product in two parts, 15 bits, which their loads hide; fp16 weights in one of 11 bits: a second
 // one leaves an error that is a tenth less and costs a call 8 to 18 % where little is read (one sequence of 1000 tokens, 32 heads over 8 of 128 fp16, 8.4 us and 9.3, of 300 6.2 and 7.3), 200 of up to 4096 in e4m3 173 us and 177.
 // fp16 ends early, so its weights refer to 2^11 below the maximum: what the type cannot hold of a weight is at most 2^-36 of the largest.
-// 64 sequences of 133 to 8192 tokens, 32 heads over 8 of 128 bf16, take 199 to 204 us, 5.4 TB/s; 200 of up to 4096, 64 heads over 8 in e4m3, 164 to 174; one of 32001 31, 4.2 TB/s, of which about 12 go to the launch, the first
-// bytes and the meeting.  Where the loads are all there is, more of them under way (four steps, smaller ones) gave nothing.
+// 64 sequences of 133 to 8192 tokens, 32 heads over 8 of 128 bf16, take 196 to 204 us, 5.4 TB/s, where reading GiBs and nothing else reaches 7.1; 200 of up to 4096, 64 heads over 8 in e4m3, 164 to 176; one of 32001 31, 4.2 TB/s, of
+// which about 12 go to the launch, the first bytes and the meeting.  More loads under way (four steps, smaller ones) gave nothing.
 constexpr int kOneMostParts = 64;   // a lane each where they meet
 constexpr int kOneCounters = 65536 / 4;
 
@@ -421,7 +421,7 @@ __device__ static __forceinline__ void attend_one_part(const AttendOneKernel &f,
     };
     // A trip to memory takes longer than all the arithmetic: where a head's results are fewer than the threads, groups of these take every so manieth part, and the first
     // four of each thread are under way while the parts' weights are made, a lane a part.  Eight at a time load more than there is where the parts are few, past the L2 and so slowly, and their code is longer: one sequence of 1000,
-    // 32 heads over 8 of 128, 9.0 us for 8.4, 25 of 100 to 4000 26.5 for 25.4; but one of 65000, 64 heads over 4 in e4m3 (64 parts), 36.3 for 39.7.
+    // 32 heads over 8 of 128, 8.6 us for 8.2, 25 of 100 to 4000 25.7 for 25.1; but one of 65000, 64 heads over 4 in e4m3 (64 parts), 33.3 for 37.5.
     constexpr int BATCH = 4;
     const int groups = items < THREADS ? (int)((THREADS + 0.5f) * __builtin_amdgcn_rcpf((float)items)) : 1;
     const int g = groups > 1 ? (int)((tid + 0.5f) * __builtin_amdgcn_rcpf((float)items)) : 0, i0 = tid - g * items * (groups > 1);
@@ -585,7 +585,7 @@ hipError_t launch_attend_one_row(const AttendOneArgs &a, const OneForm &form, hi
     constexpr int TOKENS = one_tokens(RB), WAVES = kOneWaves;
     const int64_t items = form.items, steps = form.steps, slots = form.slots;
     // Up to as many items as workgroups run at once: parts fill them, of 256 tokens at least (4 sequences of 810 to 1999, 4 heads of 80 bf16 11.4 us, of 512 tokens 15.0; but
-    // 2 of 1486 and 5604, 64 heads over 4 in e4m3, 17.3 and 16.8), of sequences from 704 on (one of 600, 32 heads over 8 of 128 fp16, 8.3 us whole, 9.6 in two; one of 1000 11.6 whole, 8.4 in three), an item's behind one another: neighbours go to different XCDs (9 of 100 to 9000, 16 heads of 64 40.5 us, with all items' parts p behind one another 45.2).
+    // 2 of 1486 and 5604, 64 heads over 4 in e4m3, 17.3 and 16.8), of sequences from 704 on (one of 600, 32 heads over 8 of 128 fp16, 8.3 us whole, 9.6 in two; one of 1000 11.6 whole, 8.2 in three), an item's behind one another: neighbours go to different XCDs (9 of 100 to 9000, 16 heads of 64 40.5 us, with all items' parts p behind one another 45.2).
     // Parts of the same steps whatever the lengths, no more than run at once, an item's neighbours those of the other heads: 6 of 9661 to 38277, 64 heads over 8 of 256 bf16, 218 us, as many parts of every sequence 240;
     // 5 of 100 to 20000, 32 heads over 8 of 128 42.7 and 50.5, 12 of 30 to 5000 29.7 and 36.2; 14 of 3726 to 4520, 80 over 5 of 256, 73.5 and 71.3. Where a record is large a part is too: 7 of 2441 to 6183, 32 heads over 2 of 128,
     // 23.8 us with parts of 256 tokens, 18.9 of 512.

@@ -8,8 +8,9 @@ namespace cw {
 
 // Nothing but moving bytes.  A row is a token's keys or values of one head; its lanes are a power of two, 8 numbers each, so that its largest magnitude is a few exchanges
 // away.  A wave takes a run of rows, kCacheBatch times 64 lanes of them under way at once: first a lane for each of its tokens finds the token's sequence, page and place, which takes trips to
-// memory that wait for one another, then the rows follow one another.  HBM bounds it: 34 k tokens of 8 heads of 128 fp16 to e4m3 in 43 us (4.9 TB/s; a copy of 1 GiB reaches 5.1), back in 37 (5.6, some of it from the last
-// level's cache), a row at a time 49 and 49.  Stores go past the caches: what they would keep there is what the reads need.
+// memory that wait for one another, then the rows follow one another.  HBM bounds it: 34 k tokens of 8 heads of 128 fp16 to e4m3 in 43.5 us (4.9 TB/s; a copy of 1 GiB reaches 5.1), of 16 bits to 16 bits in 52 either way
+// (5.4); back from e4m3 in 59 to 61 (3.5 TB/s), or 38 where what is read and written lies in the last level's cache.  fp32 rows: to e4m3 78 us (4.5 TB/s; 168 registers a lane where 16-bit rows take 64), to 16 bits 76, back 91 and 93.  A row at a time was
+// slower: 49 for 43.  Stores go past the caches: what they would keep there is what the reads need (back from e4m3 64 us otherwise, from 16 bits 56).
 constexpr int kCacheWaves = 4, kCacheBatch = 4;
 
 struct CacheKernel {
@@ -226,7 +227,7 @@ static CacheKernel cache_form(const CacheArgs &a, int64_t *workgroups) {
         ++f.lane_shift;
     }
     // A batch, or fewer where that leaves a CU less than eight waves; at most 62 tokens.  Longer runs leave the waves that are at work at the same time further apart in memory: 34 k tokens
-    // of 8 heads of 128 fp16 read from e4m3 38.5 us, and 46 for 36 where heads are two of 64.
+    // of 8 heads of 128 fp16 read from e4m3 38.5 us out of the last level's cache, and 46 for 36 where heads are two of 64.
     const int64_t each = 64 / f.lanes, rows = (int64_t)a.tokens * 2 * a.cache.kv_heads, all = (rows + each - 1) / each;
     f.passes = (int)std::max<int64_t>(1, std::min({all / 2048, (int64_t)kCacheBatch, 62 * 2 * a.cache.kv_heads / each}));
     const int64_t waves = (all + f.passes - 1) / f.passes;
