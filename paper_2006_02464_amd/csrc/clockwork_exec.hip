@@ -1517,7 +1517,7 @@ static int32_t cache_view(cw_ctx *c, const cw_cache *r, bool written, CacheView 
         return set_err(c, CW_ERR_INVALID, "bad stride of the cache");
     if (codes && (r->exp_page_stride < 0 || r->exp_head_stride < 0 || r->exp_token_stride < 0 || r->exp_page_stride > kMostStride || r->exp_head_stride > kMostStride || r->exp_token_stride > kMostStride))
         return set_err(c, CW_ERR_INVALID, "bad stride of the cache's exponents");
-    if (codes != (r->k_exp != nullptr) || codes != (r->v_exp != nullptr)) return set_err(c, CW_ERR_INVALID, "a cache has exponents with CW_DTYPE_E4M3, and only then");
+    if (codes ? r->pages > 0 && (!r->k_exp || !r->v_exp) : r->k_exp || r->v_exp) return set_err(c, CW_ERR_INVALID, "a cache has exponents with CW_DTYPE_E4M3, and only then");
     if (r->pages > 0) {
         if (!r->k || !r->v) return set_err(c, CW_ERR_INVALID, "null pointer in the cache");
         if (reinterpret_cast<uintptr_t>(r->k) % 16 != 0 || reinterpret_cast<uintptr_t>(r->v) % 16 != 0) return set_err(c, CW_ERR_INVALID, "misaligned pointer in the cache");

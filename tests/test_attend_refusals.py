@@ -301,3 +301,19 @@ def test_launches_of_more_than_32_bits_of_threads(ctx):
     for few in (dict(table_pages=8), dict(table_pages=20), dict(table_pages=100, window=200)):
         both("cw_attend_one", cw.cw_attend_one_args, dict(one, heads=64, y_stride=4096, **few), dict(sequences=(1 << 20) - 1), dict(sequences=1 << 20), more)
         assert refusal(ctx, "cw_attend_one", cw.cw_attend_one_args, dict(one, sequences=1 << 20, **few), {}, many) == PLANNING
+
+
+def test_pools_of_no_pages(ctx):
+    """They have no addresses: those of 8 bits none of exponents either."""
+    none = dict(pages=0, k=None, v=None)
+    for call, kind, defaults in OVER_A_CACHE:
+        for cache in (none, dict(CODES, **none), dict(CODES, **none, k_exp=None, v_exp=None)):
+            assert refusal(ctx, call, kind, defaults, {}, cache) == PLANNING, (call, cache)
+        st, why = refusal(ctx, call, kind, defaults, {}, dict(none, k_exp=4096, v_exp=4096))
+        assert st == INVALID and (st, why) != PLANNING
+    i, half = lambda *n: torch.zeros(*n, dtype=torch.int32), torch.float16
+    codes, exps = torch.zeros(0, 2, 16, 64, dtype=torch.float8_e4m3fn), torch.zeros(0, 2, 16, dtype=torch.uint8)
+    x, q = torch.zeros(3, 2, 64, dtype=half), torch.zeros(3, 4, 64, dtype=half)
+    for cache in (ctx.cache(codes, codes, exps, exps), ctx.cache(codes.to(half), codes.to(half))):
+        planning(ctx.cache_write, x, x.clone(), cache, i(3, 5), i(3))
+        planning(ctx.attend_one, q, cache, i(3, 5), i(3), q.clone(), 0.1)

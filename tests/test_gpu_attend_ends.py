@@ -133,3 +133,21 @@ def test_the_workspace_that_serves_every_call(ctx, sequences):
         assert bool((space[most:] == 0x5a).all())
         out.append((y, lse))
     assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+
+
+@pytest.mark.parametrize("kept", [F16, E4M3])
+def test_pools_of_no_pages(ctx, space, kept):
+    """Nothing is written, zeros are read, rows see nothing."""
+    k = torch.zeros(0, 2, 16, 64, dtype=kept, device="cuda")
+    exps = [torch.zeros(0, 2, 16, dtype=torch.uint8, device="cuda") if kept == E4M3 else None for _ in range(2)]
+    cache = ctx.cache(k, k.clone(), *exps)
+    table, lens = torch.zeros(3, 2, dtype=torch.int32, device="cuda"), torch.tensor([0, 5, 20], dtype=torch.int32).cuda()
+    x = torch.ones(3, 2, 64, dtype=F16, device="cuda")
+    z = x.clone()
+    ctx.cache_write(x, z, cache, table, lens, stream=stream())
+    ctx.cache_read(cache, table, lens, x, z, stream=stream())
+    assert not bool(x.any()) and not bool(z.any())
+    q, y = (torch.ones(3, 4, 64, dtype=F16, device="cuda") for _ in range(2))
+    lse = torch.ones(3, 4, device="cuda")
+    ctx.attend_one(q, cache, table, lens, y, 0.1, lse=lse, workspace=space, stream=stream())
+    assert not bool(y.any()) and bool((lse == -INF).all())
