@@ -44,7 +44,7 @@ def sink(n, heads, kv_heads, dim, dtype, depth, at, queries):
 def test_prompts(ctx, dtype, depth, heads, kv_heads, dim, n):
     """A weight is rounded to the values' type: half a step, 2^-36 of the largest where fp16 ends (least)."""
     few = 64 if heads < 40 else n
-    for at in (0, n // 2, n - few):
+    for at in sorted({0, n // 2, n - few}):
         q, k, v = sink(n, heads, kv_heads, dim, dtype, depth, at, few)
         first, first_k = (torch.tensor([0, x], dtype=torch.int32).cuda() for x in (few, n))
         y, lse = torch.zeros(q.shape, dtype=dtype, device="cuda"), torch.zeros(q.shape[:2], device="cuda")
@@ -59,7 +59,7 @@ def test_single_tokens(ctx, x, kept, depth, heads, kv_heads, dim, lengths):
     """Of fp16 and of codes a weight has 11 bits, half a step 2^-11, and where fp16 ends half a step of 2^-25 beside a largest of 2^11 or more: 2^-36; with codes of the largest weight times its value's power
     of two, and those differ by 2 here at most, which may be either way: 2^-34.  Of bf16 it has two parts, the second at most 2^-7 of the first and off by 2^-8 of itself."""
     sequences, space = len(lengths), torch.zeros(ctx.attend_one_workspace_bytes(), dtype=torch.uint8, device="cuda")
-    for place in (0.0, 0.5, 1.0):
+    for place in (0.0, 0.5, 1.0) if sequences < 64 else (0.5,):
         pool, refs = Pages(lengths, kv_heads, 16, dim, kept, seed=depth), []
         q = torch.zeros(sequences, heads, dim, dtype=x)
         for i, n in enumerate(lengths):
